@@ -17,6 +17,8 @@
  *   cmc_two_tier_decode  decode attention over [selected rows || window]
  *   cmc_decode_step      append + decode fused into one launch (every step)
  *   *_ragged             the same with per-sequence sizes (ragged batches)
+ *   *_q8                 the gather, append and decode on a cache of 8-bit codes,
+ *                        and cmc_cache_read_q8, which reads such a cache back
  *   cmc_locate_window    CME-guided Tier-2 window placement (once per question)
  *   cmc_denoise          graph-based context denoising before compression
  *                        (Sec. 2.1, once per context)
@@ -70,7 +72,9 @@ typedef enum cmc_status CMC_ENUM_INT {
 
 typedef enum cmc_dtype CMC_ENUM_INT {
     CMC_F32 = 0,
-    CMC_BF16 = 1
+    CMC_BF16 = 1,
+    CMC_E4M3 = 2,   /* 8-bit cache codes only: OCP e4m3 (float8_e4m3fn) */
+    CMC_I8 = 3      /* 8-bit cache codes only: two's complement */
 } cmc_dtype;
 
 /* ------------------------------------------------------------------------ */
@@ -467,6 +471,136 @@ cmc_status cmc_decode_step_noalloc(const float *q,
                                    const void *new_k, const void *new_v, int T_new,
                                    cmc_dtype kv_dtype, int B, int Hq, int Hkv, int Dh, int N,
                                    float scale, float *out, void *stream);
+
+/* ------------------------------------------------------------------------ */
+/* 8-bit cache.                                                             */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * The two-tier cache in 8 bits: half the bytes of bf16 per decode step.  A
+ * K or V array of R rows is held as
+ *   codes   [B][Hkv][R][Dh]               CMC_E4M3 or CMC_I8
+ *   scales  [B][Hkv][ceil(R / block)] fp32  one for each `block` consecutive
+ *                                         rows of a head, block in {32, 64, 128}
+ * and an element's value is code * scale.  With a the largest finite
+ * magnitude among a block's live rows and M the codes' largest magnitude (448;
+ * 127), the library writes
+ *   scale = 2^e, e the least integer >= -126 with a <= M 2^e
+ *   code  = x / scale rounded to nearest even (e4m3: error at most 2^-4 of the
+ *           value, or 2^-10 scale below 2^-6 scale; int8: scale / 2)
+ * with infinities stored as +-M and NaN as the NaN code (int8 has none: 0).
+ * The power of two keeps old rows whole when a block's scale changes: their
+ * codes are multiplied by old scale / new scale and rounded, which is exact
+ * when the scale falls; when it grows e4m3 loses only what falls below its
+ * normal range, and int8 at most half of the new scale.  The decode and the
+ * read-back take any finite scales, e.g. of a cache made elsewhere.
+ *
+ * Common limits: Hkv >= 1, B and Hkv <= 65535, Dh in {64, 128, 256}, at most
+ * 2^26 rows an array, else CMC_ERR_UNSUPPORTED.
+ */
+
+/*
+ * cmc_gather_tier1 into an 8-bit block: row j < k_b of out is the code row of
+ * pool row idx[b][j], scales over blocks of output rows.
+ *
+ *   cme_k/v, kv_dtype, idx, k_len, idx_stride: as cmc_gather_tier1 (fp32 or bf16)
+ *   out_k/v    [B][Hkv][k][Dh] codes; out_ks/vs [B][Hkv][ceil(k / block)]
+ *
+ * Rows j >= k_b, and the scales of blocks without a row below k_b, are left as
+ * they were.
+ */
+cmc_status cmc_gather_tier1_q8(const void *cme_k, const void *cme_v, cmc_dtype kv_dtype,
+                               const int32_t *idx, const int32_t *k_len, int idx_stride,
+                               int B, int Hkv, int N, int k, int Dh, cmc_dtype code, int block,
+                               void *out_k, void *out_v, float *out_ks, float *out_vs,
+                               void *stream);
+
+/*
+ * cmc_window_append on an 8-bit ring (win_k/v [B][Hkv][W][Dh] codes, win_ks/vs
+ * [B][Hkv][ceil(W / block)], blocks of slots): new_k/v [B][Hkv][T_new][Dh] in
+ * new_dtype (fp32 or bf16), row t to slot (count_b + t) mod W, then count_b +=
+ * T_new.  Every block with an appended slot gets the scale of its live rows
+ * after the append (slots below min(count_b + T_new, W)): the appended rows, and
+ * the others as their codes held them; where that differs from the old scale
+ * the other rows' codes follow it.  Rows appended in one call or in several may
+ * so differ by the roundings in between.  Slots that hold no row, and the
+ * scales of blocks without one, may hold anything; they are left as they were.
+ *
+ * Limits: 1 <= T_new <= W, count_b >= 0 and count_b + T_new < 2^31.  W == 0 is a
+ * no-op.
+ */
+cmc_status cmc_window_append_q8(void *win_k, void *win_v, float *win_ks, float *win_vs,
+                                cmc_dtype code, int block, int32_t *win_count,
+                                const void *new_k, const void *new_v, cmc_dtype new_dtype,
+                                int B, int Hkv, int W, int Dh, int T_new, void *stream);
+
+/*
+ * Reads an 8-bit cache back, in the order its rows were written: with n =
+ * min(count_b, R) rows, out[b][h][r] for r < n is the value of row
+ * (first + r) mod R, where first = count_b mod R if count_b > R and 0 otherwise.
+ * For a ring that is oldest row first; for a Tier-1 block, whose count is at
+ * most R, the rows as they stand.
+ *
+ *   k8, v8     [B][Hkv][R][Dh] codes; ks, vs [B][Hkv][ceil(R / block)]
+ *   count      [B] int32: win_count, or the k_len of a Tier-1 block; NULL: R
+ *   out_k/v    [B][Hkv][R][Dh] fp32 or bf16 (exact for the scales that the
+ *              library writes, but for results below the type's normal range,
+ *              which are rounded); rows r >= n are left as they were
+ */
+cmc_status cmc_cache_read_q8(const void *k8, const void *v8, const float *ks, const float *vs,
+                             cmc_dtype code, int block, const int32_t *count,
+                             int B, int Hkv, int R, int Dh, cmc_dtype out_dtype,
+                             void *out_k, void *out_v, void *stream);
+
+/* Bytes of workspace cmc_two_tier_decode_q8 and cmc_decode_step_q8 need; 0 for
+ * invalid sizes.  To be zero-filled before its first use and kept as
+ * cmc_decode_workspace_bytes says. */
+size_t cmc_decode_q8_workspace_bytes(int B, int Hq, int Hkv, int Dh, int k, int W);
+
+/*
+ * cmc_two_tier_decode on the 8-bit cache: softmax(scale q K^T) V over Tier-1
+ * rows 0 .. k_b - 1 and the valid ring slots.
+ *
+ *   cme_k/v    [B][Hkv][N][Dh] codes; cme_ks/vs [B][Hkv][ceil(N / block)]
+ *              (cmc_gather_tier1_q8's output; there is no index list)
+ *   k_len      [B] int32 (device): k_b = k_len[b] clamped into [0, k], or NULL
+ *              for all k
+ *   win_*      the ring as cmc_window_append_q8 keeps it
+ *   q, win_count, scale, out, workspace: as cmc_two_tier_decode, the workspace
+ *              of cmc_decode_q8_workspace_bytes
+ *
+ * A head with an empty key list gets zeros; one that attends to a NaN gets NaN.
+ * Limits: Hq / Hkv in {1, 2, 4, 8}, 0 <= k <= N, k + W >= 1.
+ * Arithmetic: q and the softmax weights enter the products with 22 bits (two
+ * fp16 parts), the codes as they are, fp32 sums in a fixed order (run-to-run
+ * bit-identical); weights below 2^-16 of the largest keep fewer bits, to 2^-38 of
+ * the largest.
+ */
+cmc_status cmc_two_tier_decode_q8(const float *q, const void *cme_k, const void *cme_v,
+                                  const float *cme_ks, const float *cme_vs,
+                                  const int32_t *k_len, int k,
+                                  const void *win_k, const void *win_v,
+                                  const float *win_ks, const float *win_vs,
+                                  const int32_t *win_count, int W, cmc_dtype code, int block,
+                                  int B, int Hq, int Hkv, int Dh, int N, float scale, float *out,
+                                  void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * One decode step in a single launch: cmc_window_append_q8 (T_new <= 65535),
+ * then cmc_two_tier_decode_q8 over the updated cache.  The ring's codes, scales
+ * and counts are those of the two calls; out is the same attention over the
+ * same keys, up to the order of the sums.  With W == 0 there is no Tier-2 and the
+ * new rows are ignored.
+ */
+cmc_status cmc_decode_step_q8(const float *q, const void *cme_k, const void *cme_v,
+                              const float *cme_ks, const float *cme_vs,
+                              const int32_t *k_len, int k,
+                              void *win_k, void *win_v, float *win_ks, float *win_vs,
+                              int32_t *win_count, int W,
+                              const void *new_k, const void *new_v, int T_new, cmc_dtype new_dtype,
+                              cmc_dtype code, int block,
+                              int B, int Hq, int Hkv, int Dh, int N, float scale, float *out,
+                              void *workspace, size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------ */
 /* Diagnostics.                                                             */

@@ -28,6 +28,8 @@ CMC_ERR_WORKSPACE_TOO_SMALL = 3
 CMC_ERR_HIP = 4
 CMC_F32 = 0
 CMC_BF16 = 1
+CMC_E4M3 = 2
+CMC_I8 = 3
 
 EXPORTED = [
     "cmc_select_workspace_bytes", "cmc_select_cmes", "cmc_select_cmes_ragged", "cmc_gather_tier1",
@@ -35,7 +37,8 @@ EXPORTED = [
     "cmc_window_start", "cmc_decode_workspace_bytes", "cmc_two_tier_decode", "cmc_decode_step",
     "cmc_two_tier_decode_ragged", "cmc_decode_step_ragged", "cmc_locate_window", "cmc_denoise_workspace_bytes",
     "cmc_denoise", "cmc_bridge_workspace_bytes", "cmc_memory_bridge", "cmc_status_string", "cmc_last_error",
-    "cmc_version", "cmc_decode_step_noalloc",
+    "cmc_version", "cmc_decode_step_noalloc", "cmc_gather_tier1_q8", "cmc_window_append_q8", "cmc_cache_read_q8",
+    "cmc_decode_q8_workspace_bytes", "cmc_two_tier_decode_q8", "cmc_decode_step_q8",
 ]
 
 
@@ -98,6 +101,20 @@ def lib() -> ctypes.CDLL:
         L.cmc_decode_step_noalloc.argtypes = [P, P, P, P, I, P, P, P, I, P, P, I, I, I, I, I, I, I,
                                               ctypes.c_float, P, P]
         L.cmc_decode_step_noalloc.restype = I
+        L.cmc_gather_tier1_q8.argtypes = [P, P, I, P, P, I, I, I, I, I, I, I, I, P, P, P, P, P]
+        L.cmc_gather_tier1_q8.restype = I
+        L.cmc_window_append_q8.argtypes = [P, P, P, P, I, I, P, P, P, I, I, I, I, I, I, P]
+        L.cmc_window_append_q8.restype = I
+        L.cmc_cache_read_q8.argtypes = [P, P, P, P, I, I, P, I, I, I, I, I, P, P, P]
+        L.cmc_cache_read_q8.restype = I
+        L.cmc_decode_q8_workspace_bytes.argtypes = [I, I, I, I, I, I]
+        L.cmc_decode_q8_workspace_bytes.restype = SZ
+        L.cmc_two_tier_decode_q8.argtypes = [P, P, P, P, P, P, I, P, P, P, P, P, I, I, I, I, I, I, I, I,
+                                             ctypes.c_float, P, P, SZ, P]
+        L.cmc_two_tier_decode_q8.restype = I
+        L.cmc_decode_step_q8.argtypes = [P, P, P, P, P, P, I, P, P, P, P, P, I, P, P, I, I, I, I, I, I, I, I, I,
+                                         ctypes.c_float, P, P, SZ, P]
+        L.cmc_decode_step_q8.restype = I
         L.cmc_status_string.argtypes = [I]
         L.cmc_status_string.restype = ctypes.c_char_p
         L.cmc_last_error.argtypes = []
@@ -573,3 +590,213 @@ def cmc_decode_step_noalloc(q, cme_k, cme_v, idx, k: int, win_k, win_v, win_coun
                                        float(scale), _ptr(a["out"]), _stream(stream))
     _check(rc)
     return a["out"]
+
+
+# ----------------------------------------------------------- 8-bit cache
+
+def _code_dtype(t) -> int:
+    torch = _torch or _load_torch()
+    d = t.dtype
+    if d is torch.float8_e4m3fn:
+        return CMC_E4M3
+    if d is torch.int8:
+        return CMC_I8
+    raise TypeError(f"expected float8_e4m3fn or int8 codes, got {d}")
+
+
+def _ptrs(*tensors):
+    """Device addresses of tensors (None passes through) that all lie on the
+    current device, whose stream the call runs on."""
+    if _torch is None:
+        _load_torch()
+    dev = _device_index()
+    out = []
+    for t in tensors:
+        if t is None:
+            out.append(None)
+            continue
+        if t.get_device() != dev:
+            if not t.is_cuda:
+                _on_host(t)
+            raise ValueError(f"cmc: tensor of shape {tuple(t.shape)} is on {t.device}, not on the current device cuda:{dev}")
+        out.append(t.data_ptr())
+    return out
+
+
+def _cache_args(name, codes_k, codes_v, scales_k, scales_v, block):
+    """Checks of one 8-bit cache array pair; returns its (B, Hkv, R, Dh)."""
+    torch = _torch or _load_torch()
+    s = codes_k.shape
+    if not (len(s) == 4 and codes_v.shape == s and codes_v.dtype is codes_k.dtype):
+        raise ValueError(f"{name}_k/v must be matching codes [B][Hkv][rows][Dh]")
+    n = (s[0], s[1], -(-s[2] // block) if block > 0 else 0)
+    if not (scales_k.shape == n and scales_v.shape == n and scales_k.dtype is torch.float32
+            and scales_v.dtype is torch.float32):
+        raise ValueError(f"{name}_ks/vs must be fp32 [B][Hkv][ceil(rows / block)]")
+    if not (codes_k.is_contiguous() and codes_v.is_contiguous() and scales_k.is_contiguous()
+            and scales_v.is_contiguous()):
+        raise ValueError(f"{name}: codes and scales must be contiguous")
+    return s
+
+
+def cmc_gather_tier1_q8(cme_k, cme_v, idx, k: int, block: int, k_len=None, dtype=None, out_k=None, out_v=None,
+                        out_ks=None, out_vs=None, stream=None):
+    """cmc_gather_tier1 into 8-bit codes with a power-of-two scale for every
+    `block` rows of a head.  cme_* [B][Hkv][N][Dh] fp32 or bf16; `dtype`
+    (float8_e4m3fn unless said otherwise, or int8) is the codes' type where out_k
+    is not given.  Returns (out_k, out_v [B][Hkv][k][Dh], out_ks, out_vs
+    [B][Hkv][ceil(k / block)] fp32)."""
+    torch = _torch or _load_torch()
+    _need(cme_k.dim() == 4 and cme_k.is_contiguous() and cme_v.is_contiguous() and cme_v.shape == cme_k.shape
+          and cme_v.dtype == cme_k.dtype, "cme_k/v [B][Hkv][N][Dh]")
+    B, Hkv, N, Dh = cme_k.shape
+    _need(block > 0, "block must be positive")
+    stride = 0
+    if idx is not None:
+        _need(idx.dim() == 2 and idx.shape[0] == B and idx.dtype == torch.int32 and idx.is_contiguous(),
+              "idx [B][idx_stride] int32")
+        stride = int(idx.shape[1])
+    if k_len is not None:
+        _need(k_len.shape == (B,) and k_len.dtype == torch.int32 and k_len.is_contiguous(), "k_len [B] int32")
+    dev = cme_k.device
+    if out_k is None:
+        out_k = torch.empty((B, Hkv, k, Dh), dtype=dtype or torch.float8_e4m3fn, device=dev)
+    if out_v is None:
+        out_v = torch.empty((B, Hkv, k, Dh), dtype=out_k.dtype, device=dev)
+    n = -(-k // block)
+    if out_ks is None:
+        out_ks = torch.empty((B, Hkv, n), dtype=torch.float32, device=dev)
+    if out_vs is None:
+        out_vs = torch.empty((B, Hkv, n), dtype=torch.float32, device=dev)
+    _need(_cache_args("out", out_k, out_v, out_ks, out_vs, block) == (B, Hkv, k, Dh), "out_k/v [B][Hkv][k][Dh]")
+    pk, pv, pi, pl, ok, ov, oks, ovs = _ptrs(cme_k, cme_v, idx, k_len, out_k, out_v, out_ks, out_vs)
+    rc = lib().cmc_gather_tier1_q8(pk, pv, _kv_dtype(cme_k), pi, pl, stride, B, Hkv, N, int(k), Dh, _code_dtype(out_k),
+                                   int(block), ok, ov, oks, ovs, _stream(stream))
+    _check(rc)
+    return out_k, out_v, out_ks, out_vs
+
+
+def cmc_window_append_q8(win_k, win_v, win_ks, win_vs, win_count, new_k, new_v, block: int, stream=None) -> None:
+    """Append to an 8-bit ring in place.  win_k/v [B][Hkv][W][Dh] codes,
+    win_ks/vs [B][Hkv][ceil(W / block)] fp32, win_count [B] int32, new_*
+    [B][Hkv][T][Dh] fp32 or bf16."""
+    torch = _torch or _load_torch()
+    B, Hkv, W, Dh = _cache_args("win", win_k, win_v, win_ks, win_vs, block)
+    _need(new_k.dim() == 4 and new_k.shape[:2] == (B, Hkv) and new_k.shape[3] == Dh, "new_k [B][Hkv][T][Dh]")
+    _need(new_v.shape == new_k.shape and new_v.dtype == new_k.dtype, "new_k/v must match")
+    _need(new_k.is_contiguous() and new_v.is_contiguous(), "new_k/v must be contiguous")
+    _need(win_count.shape == (B,) and win_count.dtype == torch.int32 and win_count.is_contiguous(),
+          "win_count [B] int32")
+    wk, wv, wks, wvs, wc, nk, nv = _ptrs(win_k, win_v, win_ks, win_vs, win_count, new_k, new_v)
+    rc = lib().cmc_window_append_q8(wk, wv, wks, wvs, _code_dtype(win_k), int(block), wc, nk, nv, _kv_dtype(new_k), B,
+                                    Hkv, W, Dh, int(new_k.shape[2]), _stream(stream))
+    _check(rc)
+
+
+def cmc_cache_read_q8(k8, v8, ks, vs, block: int, count=None, dtype=None, out_k=None, out_v=None, stream=None):
+    """Values of an 8-bit cache in the order its rows were written (a ring's
+    oldest row first): rows r < min(count, R) of out_k/v [B][Hkv][R][Dh], fp32
+    or bf16 (`dtype`, bf16 unless said otherwise, where out_k is not given).
+    count [B] int32, or None for R rows.  Returns (out_k, out_v)."""
+    torch = _torch or _load_torch()
+    B, Hkv, R, Dh = _cache_args("cache", k8, v8, ks, vs, block)
+    if count is not None:
+        _need(count.shape == (B,) and count.dtype == torch.int32 and count.is_contiguous(), "count [B] int32")
+    if out_k is None:
+        out_k = torch.empty((B, Hkv, R, Dh), dtype=dtype or torch.bfloat16, device=k8.device)
+    if out_v is None:
+        out_v = torch.empty((B, Hkv, R, Dh), dtype=out_k.dtype, device=k8.device)
+    _need(out_k.shape == (B, Hkv, R, Dh) and out_v.shape == out_k.shape and out_v.dtype == out_k.dtype
+          and out_k.is_contiguous() and out_v.is_contiguous(), "out_k/v [B][Hkv][R][Dh]")
+    ck, cv, sk, sv, n, ok, ov = _ptrs(k8, v8, ks, vs, count, out_k, out_v)
+    rc = lib().cmc_cache_read_q8(ck, cv, sk, sv, _code_dtype(k8), int(block), n, B, Hkv, R, Dh, _kv_dtype(out_k), ok, ov,
+                                 _stream(stream))
+    _check(rc)
+    return out_k, out_v
+
+
+def cmc_decode_q8_workspace_bytes(B: int, Hq: int, Hkv: int, Dh: int, k: int, W: int) -> int:
+    return int(lib().cmc_decode_q8_workspace_bytes(int(B), int(Hq), int(Hkv), int(Dh), int(k), int(W)))
+
+
+def decode_workspace_q8(B: int, Hq: int, Hkv: int, Dh: int, k: int, W: int, device):
+    """A zero-filled workspace of the 8-bit decode calls (the library keeps it
+    zeroed)."""
+    import torch
+    return torch.zeros(max(1, cmc_decode_q8_workspace_bytes(B, Hq, Hkv, Dh, k, W)), dtype=torch.uint8, device=device)
+
+
+def _decode_q8_args(q, cme_k, cme_v, cme_ks, cme_vs, k, win_k, win_v, win_ks, win_vs, win_count, block, k_len, out,
+                    workspace):
+    """Checks shared by the 8-bit decode wrappers; returns (B, Hq, Hkv, Dh, N,
+    W, out, workspace, its bytes)."""
+    torch = _torch or _load_torch()
+    f32, i32 = torch.float32, torch.int32
+    qs = q.shape
+    if not (len(qs) == 3 and q.dtype is f32 and q.is_contiguous()):
+        raise ValueError("q must be contiguous fp32 [B][Hq][Dh]")
+    B, Hq, Dh = qs
+    _, Hkv, N, _ = s = _cache_args("cme", cme_k, cme_v, cme_ks, cme_vs, block)
+    if not (s[0] == B and s[3] == Dh):
+        raise ValueError("cme_k/v [B][Hkv][N][Dh]")
+    W = 0
+    if win_k is not None:
+        s = _cache_args("win", win_k, win_v, win_ks, win_vs, block)
+        W = s[2]
+        if not (s == (B, Hkv, W, Dh) and win_k.dtype is cme_k.dtype):
+            raise ValueError("win_k/v [B][Hkv][W][Dh], codes as cme_k/v")
+        if not (win_count is not None and win_count.shape == (B,) and win_count.dtype is i32
+                and win_count.is_contiguous()):
+            raise ValueError("win_count [B] int32")
+    if k_len is not None and not (k_len.shape == (B,) and k_len.dtype is i32 and k_len.is_contiguous()):
+        raise ValueError("k_len [B] int32")
+    if out is None:
+        out = torch.empty((B, Hq, Dh), dtype=f32, device=q.device)
+    elif not (out.shape == qs and out.dtype is f32 and out.is_contiguous()):
+        raise ValueError("out [B][Hq][Dh] fp32")
+    if workspace is None:
+        workspace = decode_workspace_q8(B, Hq, Hkv, Dh, k, W, q.device)
+    return B, Hq, Hkv, Dh, N, W, out, workspace, workspace.numel() * workspace.element_size()
+
+
+def cmc_two_tier_decode_q8(q, cme_k, cme_v, cme_ks, cme_vs, k: int, win_k, win_v, win_ks, win_vs, win_count,
+                           scale: float, block: int, k_len=None, out=None, workspace=None, stream=None):
+    """cmc_two_tier_decode over the 8-bit cache: rows 0 .. k - 1 (k_len[b] - 1)
+    of cme_k/v [B][Hkv][N][Dh] codes, then the ring (None: no Tier-2); scales
+    [B][Hkv][ceil(rows / block)] fp32.  Returns out [B][Hq][Dh] fp32."""
+    B, Hq, Hkv, Dh, N, W, out, workspace, ws_bytes = _decode_q8_args(
+        q, cme_k, cme_v, cme_ks, cme_vs, k, win_k, win_v, win_ks, win_vs, win_count, block, k_len, out, workspace)
+    if W == 0:
+        win_k = win_v = win_ks = win_vs = win_count = None
+    pq, po, pw, *cache = _ptrs(q, out, workspace, cme_k, cme_v, cme_ks, cme_vs, k_len, win_k, win_v, win_ks, win_vs,
+                               win_count)
+    rc = lib().cmc_two_tier_decode_q8(pq, *cache[:5], int(k), *cache[5:], W, _code_dtype(cme_k), int(block), B, Hq, Hkv,
+                                      Dh, N, float(scale), po, pw, ws_bytes, _stream(stream))
+    _check(rc)
+    return out
+
+
+def cmc_decode_step_q8(q, cme_k, cme_v, cme_ks, cme_vs, k: int, win_k, win_v, win_ks, win_vs, win_count, new_k, new_v,
+                       scale: float, block: int, k_len=None, out=None, workspace=None, stream=None):
+    """cmc_window_append_q8 of new_k/new_v [B][Hkv][T][Dh] (fp32 or bf16), then
+    cmc_two_tier_decode_q8, in one launch.  Returns out [B][Hq][Dh] fp32."""
+    B, Hq, Hkv, Dh, N, W, out, workspace, ws_bytes = _decode_q8_args(
+        q, cme_k, cme_v, cme_ks, cme_vs, k, win_k, win_v, win_ks, win_vs, win_count, block, k_len, out, workspace)
+    T, new_dtype = 0, CMC_F32
+    if W > 0:
+        ns = new_k.shape
+        if not (len(ns) == 4 and ns[0] == B and ns[1] == Hkv and ns[3] == Dh):
+            raise ValueError("new_k [B][Hkv][T][Dh]")
+        if not (new_v.shape == ns and new_v.dtype is new_k.dtype):
+            raise ValueError("new_k/v must match")
+        if not (new_k.is_contiguous() and new_v.is_contiguous()):
+            raise ValueError("new_k/v must be contiguous")
+        T, new_dtype = ns[2], _kv_dtype(new_k)
+    else:
+        new_k = new_v = win_k = win_v = win_ks = win_vs = win_count = None
+    pq, po, pw, nk, nv, *cache = _ptrs(q, out, workspace, new_k, new_v, cme_k, cme_v, cme_ks, cme_vs, k_len, win_k,
+                                       win_v, win_ks, win_vs, win_count)
+    rc = lib().cmc_decode_step_q8(pq, *cache[:5], int(k), *cache[5:], W, nk, nv, T, new_dtype, _code_dtype(cme_k),
+                                  int(block), B, Hq, Hkv, Dh, N, float(scale), po, pw, ws_bytes, _stream(stream))
+    _check(rc)
+    return out

@@ -1,0 +1,243 @@
+// Writing the 8-bit cache and reading it back (the format: cache8.hpp).
+//
+// The Tier-1 gather and a prefill's ring append take one workgroup per block
+// of rows, for K and V together: half of its threads hold the block's K in
+// registers, half its V, so every row is read once; the block's largest
+// magnitude is reduced over the half, and the codes go out as 16-byte stores.
+// A decode step's append (a few rows) takes one workgroup per sequence, a wave
+// per (kv head, K or V, block), and advances the count itself.  All of it is
+// bound by memory, the small calls by latency.
+#include <algorithm>
+
+#include "cache8.hpp"
+#include "kernels.hpp"
+
+namespace cmc {
+
+namespace {
+
+// One block of rows of one (sequence, kv head): the rows of a Tier-1 block,
+// read from the pool through the index list, or (RING) a ring block that the
+// appended rows touch, its other live rows read back from their codes.  NP:
+// 16-element words per thread, for blockDim.x / 2 threads on each of K and V.
+template <typename T, class F, bool RING, int NP>
+__global__ __launch_bounds__(1024) void write_blocks_kernel(Write8Params p) {
+    const int h = blockIdx.y, b = blockIdx.z;
+    const size_t head = (size_t)b * p.Hkv + h;
+    const int half = (int)(blockDim.x >> 1);  // whole waves
+    const bool is_v = (int)threadIdx.x >= half;
+    const int t0 = (int)threadIdx.x - (is_v ? half : 0);
+    const int shift = p.row_shift, lb = p.log2_block;
+    int j = blockIdx.x, slot0 = 0, live;
+    if constexpr (RING) {
+        const int count = max(p.count[b], 0);
+        slot0 = count % p.R;
+        TouchedBlocks tb;
+        tb.set(slot0, p.T_new, p.R, lb);
+        if (j >= tb.count) return;  // uniform
+        j = tb.block(j);
+        live = (int)min((long long)count + p.T_new, (long long)p.R) - (j << lb);
+    } else {
+        live = (p.count ? min(max(p.count[b], 0), p.R) : p.R) - (j << lb);
+        if (live <= 0) return;  // uniform
+    }
+    const int s0 = j << lb;
+    const int words = min(live, 1 << lb) << shift;
+    const T *src = static_cast<const T *>(is_v ? p.src_v : p.src_k) + ((head * p.src_rows) << shift) * 16;
+    uint4 *dst = static_cast<uint4 *>(is_v ? p.v : p.k) + ((head * p.R + s0) << shift);
+    float *scale_at = (is_v ? p.vs : p.ks) + head * p.blocks + j;
+    float old_scale = 0.f;
+    if constexpr (RING) old_scale = *scale_at;
+
+    // A word holds elements to be rounded (fresh) or a ring's old codes.
+    Raw16<T> raw[NP];
+    uint4 code[RING ? NP : 1];
+    bool fresh[NP];
+#pragma unroll
+    for (int u = 0; u < NP; ++u) {
+        const int i = t0 + u * half;
+        int row = s0 + (i >> shift);
+        bool in = i < words;
+        raw[u].clear();
+        if constexpr (RING) {
+            row -= slot0;
+            row += row < 0 ? p.R : 0;
+            fresh[u] = in && row < p.T_new;
+            code[u] = make_uint4(0, 0, 0, 0);
+            if (in && !fresh[u]) code[u] = dst[i];
+        } else {
+            fresh[u] = in;
+            if (in && p.idx) row = min(max(p.idx[(size_t)b * p.idx_stride + row], 0), p.src_rows - 1);
+        }
+        if (fresh[u]) raw[u].load(src + (((size_t)row << shift) + (i & ((1 << shift) - 1))) * 16);
+    }
+    uint32_t top = 0, old = 0;
+#pragma unroll
+    for (int u = 0; u < NP; ++u) top = max(top, raw[u].top());
+    if constexpr (RING) {
+        float t = 0.f;
+#pragma unroll
+        for (int u = 0; u < NP; ++u) t = fmaxf(t, codes_top<F>(code[u]));
+        old = old_mag(t, old_scale);
+    }
+    __shared__ uint32_t s_top[2][2][8];
+    const int wave = t0 >> 6, waves = half >> 6;
+    top = wave_umax(max(top, old));
+    if ((threadIdx.x & 63) == 0) s_top[0][is_v][wave] = top;
+    __syncthreads();
+    for (int w = 0; w < waves; ++w) top = max(top, s_top[0][is_v][w]);
+    // Infinities or NaN in the block, known to the whole half: the maximum is
+    // taken anew without them.
+    const bool plain = top < kInfBits;
+    if (!plain) {
+        top = old;
+#pragma unroll
+        for (int u = 0; u < NP; ++u) top = max(top, raw[u].finite_top());
+        top = wave_umax(top);
+        if ((threadIdx.x & 63) == 0) s_top[1][is_v][wave] = top;
+    }
+    __syncthreads();
+    if (!plain) {
+        for (int w = 0; w < waves; ++w) top = max(top, s_top[1][is_v][w]);
+    }
+    const int e = scale_exp<F>(top);
+    const float scale = exp_scale(e), inv = exp_inverse(e);
+    if (t0 == 0) *scale_at = scale;
+#pragma unroll
+    for (int u = 0; u < NP; ++u) {
+        const int i = t0 + u * half;
+        if (fresh[u]) {
+            float x[16];
+            raw[u].widen(x);
+            st16_nt(&dst[i], pack16<F>(x, inv, plain));
+        } else if constexpr (RING) {
+            if (i < words && scale != old_scale) st16_nt(&dst[i], repack16<F>(code[u], old_scale, inv));
+        }
+    }
+}
+
+// A few rows appended: one workgroup per sequence.
+template <typename T, class F>
+__global__ __launch_bounds__(1024) void append_rows_kernel(Write8Params p) {
+    const int b = blockIdx.x;
+    const int count = max(p.count[b], 0);
+    const int slot0 = count % p.R;
+    const int filled = (int)min((long long)count + p.T_new, (long long)p.R);
+    TouchedBlocks tb;
+    tb.set(slot0, p.T_new, p.R, p.log2_block);
+    const int items = 2 * p.Hkv * tb.count;  // small: see append_one_wg
+    for (int w = threadIdx.x >> 6; w < items; w += (int)(blockDim.x >> 6)) {
+        const bool is_v = w & 1;
+        const size_t head = (size_t)b * p.Hkv + (w >> 1) % p.Hkv;
+        append_block<T, F>(static_cast<const T *>(is_v ? p.src_v : p.src_k) + ((head * p.T_new) << p.row_shift) * 16,
+                           static_cast<uint8_t *>(is_v ? p.v : p.k) + ((head * p.R) << p.row_shift) * 16,
+                           (is_v ? p.vs : p.ks) + head * p.blocks, tb.block((w >> 1) / p.Hkv), p.log2_block,
+                           p.row_shift, p.R, slot0, filled, p.T_new);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) p.count[b] = count + p.T_new;
+}
+
+// Rows r < min(count, R) of the cache in the order they were written, oldest
+// first: row (first + r) mod R, first = count mod R where the ring has
+// wrapped.  A thread widens sixteen codes of K and sixteen of V.
+template <typename T>
+__device__ __forceinline__ void put16(T *p, const float (&x)[16]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            st16_nt(reinterpret_cast<uint4 *>(p) + i,
+                    make_uint4(__float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]),
+                               __float_as_uint(x[4 * i + 3])));
+    } else {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x[2 * i], (__bf16)x[2 * i + 1]});
+        st16_nt(reinterpret_cast<uint4 *>(p), make_uint4(w[0], w[1], w[2], w[3]));
+        st16_nt(reinterpret_cast<uint4 *>(p) + 1, make_uint4(w[4], w[5], w[6], w[7]));
+    }
+}
+
+template <typename T, class F>
+__global__ __launch_bounds__(256) void read_kernel(Read8Params p) {
+    const int h = blockIdx.y, b = blockIdx.z;
+    const size_t head = (size_t)b * p.Hkv + h;
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    const int count = p.count ? p.count[b] : p.R;
+    const long long r = i >> p.row_shift;
+    if (r >= min(count, p.R)) return;
+    long long row = r + (count > p.R ? count % p.R : 0);
+    row -= row >= p.R ? p.R : 0;
+    const size_t from = ((head * p.R + row) << p.row_shift) + (i & ((1 << p.row_shift) - 1));
+    const size_t to = (((head * p.R + r) << p.row_shift) + (i & ((1 << p.row_shift) - 1))) * 16;
+    const size_t at = head * p.blocks + (row >> p.log2_block);
+    const uint4 ck = static_cast<const uint4 *>(p.k)[from], cv = static_cast<const uint4 *>(p.v)[from];
+    const float ks = p.ks[at], vs = p.vs[at];
+    float x[16];
+    widen16<F>(ck, x);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] *= ks;
+    put16<T>(static_cast<T *>(p.out_k) + to, x);
+    widen16<F>(cv, x);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] *= vs;
+    put16<T>(static_cast<T *>(p.out_v) + to, x);
+}
+
+template <typename T, class F, bool RING>
+hipError_t launch_blocks(const Write8Params &p, int items, hipStream_t stream) {
+    const int words = 1 << (p.log2_block + p.row_shift);  // of a whole block: 128 to 2048
+    const int half = std::min(words, 512);
+    const dim3 grid(items, p.Hkv, p.B);
+    switch (words / half) {
+        case 1: write_blocks_kernel<T, F, RING, 1><<<grid, 2 * half, 0, stream>>>(p); break;
+        case 2: write_blocks_kernel<T, F, RING, 2><<<grid, 2 * half, 0, stream>>>(p); break;
+        case 4: write_blocks_kernel<T, F, RING, 4><<<grid, 2 * half, 0, stream>>>(p); break;
+        default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
+// Ring blocks that an append of T rows can touch at most: two that it fills
+// in part and a short last block on the way.
+int touched_most(int T, int blocks, int log2_block) {
+    return std::min(blocks, ((T - 1) >> log2_block) + 3);
+}
+
+template <typename T, class F>
+hipError_t launch_append(const Write8Params &p, hipStream_t stream) {
+    const int most = touched_most(p.T_new, p.blocks, p.log2_block);
+    if (p.T_new <= kAppend8OneWg) {
+        append_rows_kernel<T, F><<<p.B, 1024, 0, stream>>>(p);
+        return hipGetLastError();
+    }
+    if (hipError_t e = launch_blocks<T, F, true>(p, most, stream); e != hipSuccess) return e;
+    return launch_window_count(p.count, p.B, p.T_new, stream);
+}
+
+}  // namespace
+
+hipError_t launch_gather8(const Write8Params &p, bool bf16, bool e4m3, hipStream_t stream) {
+    if (bf16) return e4m3 ? launch_blocks<uint16_t, CodeE4M3, false>(p, p.blocks, stream)
+                          : launch_blocks<uint16_t, CodeI8, false>(p, p.blocks, stream);
+    return e4m3 ? launch_blocks<float, CodeE4M3, false>(p, p.blocks, stream)
+                : launch_blocks<float, CodeI8, false>(p, p.blocks, stream);
+}
+
+hipError_t launch_append8(const Write8Params &p, bool bf16, bool e4m3, hipStream_t stream) {
+    if (bf16) return e4m3 ? launch_append<uint16_t, CodeE4M3>(p, stream) : launch_append<uint16_t, CodeI8>(p, stream);
+    return e4m3 ? launch_append<float, CodeE4M3>(p, stream) : launch_append<float, CodeI8>(p, stream);
+}
+
+hipError_t launch_read8(const Read8Params &p, bool bf16, bool e4m3, hipStream_t stream) {
+    const long long words = (long long)p.R << p.row_shift;
+    const dim3 grid((unsigned)((words + 255) / 256), p.Hkv, p.B);
+    if (bf16 && e4m3) read_kernel<uint16_t, CodeE4M3><<<grid, 256, 0, stream>>>(p);
+    else if (bf16) read_kernel<uint16_t, CodeI8><<<grid, 256, 0, stream>>>(p);
+    else if (e4m3) read_kernel<float, CodeE4M3><<<grid, 256, 0, stream>>>(p);
+    else read_kernel<float, CodeI8><<<grid, 256, 0, stream>>>(p);
+    return hipGetLastError();
+}
+
+}  // namespace cmc

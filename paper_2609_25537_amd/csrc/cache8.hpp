@@ -1,0 +1,302 @@
+// The 8-bit cache format (device side), shared by the kernels that write,
+// read and attend over it.
+//
+// A (sequence, kv head)'s rows are held as 8-bit codes, with one fp32 scale
+// for each block of `block` consecutive rows; an element's value is code *
+// scale.  With a the largest finite magnitude of the block's live rows and M
+// the codes' largest magnitude, scale = 2^e with e the least integer >= -126
+// for which a <= M 2^e, and code = x / scale rounded to nearest even.
+//
+// The scale is a power of two so that dividing by it is exact: the code's
+// rounding is the only one (e4m3: half a step of 2^-3 of the value's binade,
+// so at most 2^-4 of the value above 2^-6 scale; int8: scale / 2).  And when a
+// block's scale changes because a row was appended, the old rows' codes move
+// by whole binades: a falling scale is exact for both codes, a growing one
+// costs e4m3 bits only where a code becomes subnormal, and int8 half of the new
+// step per binade, one step in all at the largest scale a row has lived
+// through.  A scale fitted to a itself would round every old row anew
+// each time the maximum moved.
+#pragma once
+
+#include "device_common.hpp"
+
+namespace cmc {
+
+typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+
+// e4m3 (OCP: no infinities, 0x7f and 0xff are NaN).
+struct CodeE4M3 {
+    static constexpr float kMost = 448.f;
+    static constexpr int kTopExp = 8;               // 448 = 1.75 * 2^8
+    static constexpr uint32_t kTopFrac = 0x600000;  // .75
+    static constexpr bool kHasNaN = true;
+    // Four values (within [-kMost, kMost] or NaN) to a word of codes.
+    __device__ __forceinline__ static uint32_t pack4(float a, float b, float c, float d) {
+        const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+    }
+    __device__ __forceinline__ static void widen4(uint32_t w, float (&f)[4]) {
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
+        const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+        f[0] = lo[0]; f[1] = lo[1]; f[2] = hi[0]; f[3] = hi[1];
+    }
+    // Four codes as fp16, which holds every code exactly.
+    __device__ __forceinline__ static void half4(uint32_t w, uint32_t &lo, uint32_t &hi) {
+        lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.f, false));
+        hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.f, true));
+    }
+};
+
+struct CodeI8 {
+    static constexpr float kMost = 127.f;
+    static constexpr int kTopExp = 6;               // 127 = 1.984375 * 2^6
+    static constexpr uint32_t kTopFrac = 0x7e0000;  // .984375
+    static constexpr bool kHasNaN = false;
+    // Adding 1.5 * 2^23 rounds to an integer (nearest even), whose two's
+    // complement the low bits then hold.
+    __device__ __forceinline__ static uint32_t pack4(float a, float b, float c, float d) {
+        constexpr float kMagic = 12582912.f;
+        const uint32_t ab = __builtin_amdgcn_perm(__float_as_uint(b + kMagic), __float_as_uint(a + kMagic), 0x0c0c0400);
+        const uint32_t cd = __builtin_amdgcn_perm(__float_as_uint(d + kMagic), __float_as_uint(c + kMagic), 0x0c0c0400);
+        return __builtin_amdgcn_perm(cd, ab, 0x05040100);
+    }
+    __device__ __forceinline__ static void widen4(uint32_t w, float (&f)[4]) {
+        f[0] = (float)(int8_t)w;
+        f[1] = (float)(int8_t)(w >> 8);
+        f[2] = (float)(int8_t)(w >> 16);
+        f[3] = (float)((int32_t)w >> 24);
+    }
+    // fp16 with the bits 0x6400 | u is 1024 + u for u < 1024, and u = code +
+    // 128 is the code with its sign bit flipped: subtracting 1152 is exact.
+    __device__ __forceinline__ static void half4(uint32_t w, uint32_t &lo, uint32_t &hi) {
+        const uint32_t u = w ^ 0x80808080u;
+        const halfx2 k = {(_Float16)1152.f, (_Float16)1152.f};
+        lo = __builtin_bit_cast(uint32_t, __builtin_bit_cast(halfx2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400)) - k);
+        hi = __builtin_bit_cast(uint32_t, __builtin_bit_cast(halfx2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402)) - k);
+    }
+};
+
+// e of the scale 2^e for the largest magnitude whose fp32 bits are `a` (finite).
+template <class F>
+__device__ __forceinline__ int scale_exp(uint32_t a) {
+    const int e = (int)(a >> 23) - 127 - F::kTopExp + ((a & 0x7fffffu) > F::kTopFrac ? 1 : 0);
+    return e < -126 ? -126 : e;
+}
+__device__ __forceinline__ float exp_scale(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+// 2^-e: e is at most 122, so this is normal too.
+__device__ __forceinline__ float exp_inverse(int e) { return __uint_as_float((uint32_t)(127 - e) << 23); }
+
+constexpr uint32_t kInfBits = 0x7f800000u;
+
+// The magnitude bits of x, 0 if it is not finite.
+__device__ __forceinline__ uint32_t finite_mag(float x) {
+    const uint32_t u = __float_as_uint(x) & 0x7fffffffu;
+    return u < kInfBits ? u : 0u;
+}
+
+__device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));   // ^1
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));   // ^2
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, true));  // ^7
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xF, 0xF, true));  // ^15
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max((uint32_t)a[0], (uint32_t)a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return max((uint32_t)b[0], (uint32_t)b[1]);
+}
+
+// Code of x / scale with inv = 1 / scale, for any x: infinities take the
+// largest code, NaN the NaN code (int8, which has none: 0).
+template <class F>
+__device__ __forceinline__ float to_code_range(float x, float inv) {
+    const float y = __builtin_amdgcn_fmed3f(x * inv, -F::kMost, F::kMost);
+    return x == x ? y : (F::kHasNaN ? x : 0.f);
+}
+
+// Sixteen consecutive elements of a row as loaded: 32 bytes of bf16, 64 of fp32.
+template <typename T>
+struct Raw16 {
+    static constexpr int M = Vec16<T>::N, N = 16 / M;
+    uint4 r[N];
+    __device__ __forceinline__ void load(const T *p) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) r[i] = reinterpret_cast<const uint4 *>(p)[i];
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < N; ++i) r[i] = make_uint4(0, 0, 0, 0);
+    }
+    __device__ __forceinline__ void widen(float (&x)[16]) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float f[M];
+            Vec16<T>::widen(r[i], f);
+#pragma unroll
+            for (int j = 0; j < M; ++j) x[M * i + j] = f[j];
+        }
+    }
+    // The largest magnitude's fp32 bits, infinities and NaN counting.
+    __device__ __forceinline__ uint32_t top() const {
+        uint32_t m = 0;
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                m = max(max(m, max(r[i].x & 0x7fffffffu, r[i].y & 0x7fffffffu)),
+                        max(r[i].z & 0x7fffffffu, r[i].w & 0x7fffffffu));
+        } else {
+            typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+            u16x2 t = {0, 0};
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const uint32_t w[4] = {r[i].x, r[i].y, r[i].z, r[i].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    t = __builtin_elementwise_max(t, __builtin_bit_cast(u16x2, w[e] & 0x7fff7fffu));
+            }
+            m = (uint32_t)(t[0] > t[1] ? t[0] : t[1]) << 16;
+        }
+        return m;
+    }
+    // The same of the finite elements alone.
+    __device__ __forceinline__ uint32_t finite_top() const {
+        float x[16];
+        widen(x);
+        uint32_t m = 0;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) m = max(m, finite_mag(x[e]));
+        return m;
+    }
+};
+
+template <class F>
+__device__ __forceinline__ void widen16(const uint4 &c, float (&x)[16]) {
+    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        float f[4];
+        F::widen4(w[q], f);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[4 * q + e] = f[e];
+    }
+}
+
+// The largest magnitude of sixteen codes; NaN codes do not count.
+template <class F>
+__device__ __forceinline__ float codes_top(const uint4 &c) {
+    float x[16], m = 0.f;
+    widen16<F>(c, x);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) m = fmaxf(m, fabsf(x[e]));
+    return m;
+}
+// That magnitude's share in the block's maximum.  A top of 0 (no live old row,
+// or only zeros) counts for nothing, whatever the old scale holds.
+__device__ __forceinline__ uint32_t old_mag(float codes_top, float old_scale) {
+    return codes_top > 0.f ? finite_mag(codes_top * old_scale) : 0u;
+}
+
+// Codes of sixteen elements.  plain: all of them are finite, so that none
+// passes the largest code.
+template <class F>
+__device__ __forceinline__ uint4 pack16(const float (&x)[16], float inv, bool plain) {
+    uint32_t w[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = plain ? x[4 * q + e] * inv : to_code_range<F>(x[4 * q + e], inv);
+        w[q] = F::pack4(y[0], y[1], y[2], y[3]);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Codes under a new scale of sixteen codes under an old one.
+template <class F>
+__device__ __forceinline__ uint4 repack16(const uint4 &c, float old_scale, float inv) {
+    float x[16];
+    widen16<F>(c, x);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] *= old_scale;
+    return pack16<F>(x, inv, false);
+}
+
+// The ring blocks that an append of T_new rows at slot0 writes: consecutive
+// from first, round the ring's nb blocks.
+struct TouchedBlocks {
+    int first, count, nb;
+    __device__ __forceinline__ void set(int slot0, int T_new, int W, int log2_block) {
+        nb = (int)(((unsigned)W + (1u << log2_block) - 1u) >> log2_block);
+        first = slot0 >> log2_block;
+        const int room = W - slot0;  // slots up to the ring's end
+        if (T_new <= room) count = ((slot0 + T_new - 1) >> log2_block) - first + 1;
+        else count = min(nb, nb - first + ((T_new - room - 1) >> log2_block) + 1);
+    }
+    __device__ __forceinline__ int block(int i) const { return first + i < nb ? first + i : first + i - nb; }
+    __device__ __forceinline__ bool has(int j) const {
+        const int d = j - first;
+        return (d < 0 ? d + nb : d) < count;
+    }
+};
+
+// One wave brings one ring block of K or V of one (sequence, kv head) up to
+// date with the rows appended at slot0: the scale from the new rows and the
+// live old ones, then the codes.  Where the scale stays, only the new rows are
+// written.  row_shift: log2 of a row's 16-code words; filled: slots that are
+// live after the append.
+template <typename T, class F>
+__device__ __forceinline__ void append_block(const T *rows, uint8_t *codes, float *scales, int j, int log2_block,
+                                             int row_shift, int W, int slot0, int filled, int T_new) {
+    const int lane = threadIdx.x & 63;
+    const int s0 = j << log2_block;
+    const int live = min(1 << log2_block, filled - s0);
+    const int words = live << row_shift;
+    uint4 *base = reinterpret_cast<uint4 *>(codes) + ((size_t)s0 << row_shift);
+    // appended row that word i belongs to; T_new or more: an old row
+    const auto row_of = [&](int i) {
+        const int t = s0 + (i >> row_shift) - slot0;
+        return t < 0 ? t + W : t;
+    };
+    const auto new_word = [&](int t, int i) {
+        return rows + (((size_t)t << row_shift) + (i & ((1 << row_shift) - 1))) * 16;
+    };
+    const float old_scale = scales[j];
+    uint32_t top = 0;
+    float old_top = 0.f;
+    constexpr int kTrip = 4;  // words a lane requests before it looks at the first
+    for (int i0 = lane; i0 < words; i0 += kWave * kTrip) {
+        uint4 c[kTrip];
+#pragma unroll
+        for (int u = 0; u < kTrip; ++u) c[u] = base[min(i0 + u * kWave, words - 1)];
+#pragma unroll
+        for (int u = 0; u < kTrip; ++u) {
+            const int i = i0 + u * kWave;
+            if (i >= words) continue;
+            const int t = row_of(i);
+            if (t < T_new) {
+                Raw16<T> r;
+                r.load(new_word(t, i));
+                top = max(top, r.finite_top());
+            } else {
+                old_top = fmaxf(old_top, codes_top<F>(c[u]));
+            }
+        }
+    }
+    const int e = scale_exp<F>(wave_umax(max(top, old_mag(old_top, old_scale))));
+    const float scale = exp_scale(e), inv = exp_inverse(e);
+    const bool same = scale == old_scale;
+    for (int i = lane; i < words; i += kWave) {
+        const int t = row_of(i);
+        if (t < T_new) {
+            Raw16<T> r;
+            float x[16];
+            r.load(new_word(t, i));
+            r.widen(x);
+            base[i] = pack16<F>(x, inv, false);
+        } else if (!same) {
+            base[i] = repack16<F>(base[i], old_scale, inv);
+        }
+    }
+    if (lane == 0 && !same) scales[j] = scale;
+}
+
+}  // namespace cmc

@@ -172,6 +172,31 @@ DecodePlan plan_decode(int B, int Hq, int Hkv, int Dh, int k, int W, int T_new) 
     return pl;
 }
 
+// Split plan of the decode over the 8-bit cache, in units of kUnit8 rows.  Four
+// 4-wave workgroups are resident per CU (two for heads of 256), so `slots` =
+// 1024 (512) of them fill the 256 CUs in one round.
+DecodePlan plan_decode8(int B, int Hq, int Hkv, int Dh, int k, int W, int T_new) {
+    constexpr long long kWaves = 4, kMaxSplits = 127;
+    DecodePlan pl;
+    const long long pairs = (long long)B * Hkv;
+    const long long units = ((long long)k + kUnit8 - 1) / kUnit8 + ((long long)W + kUnit8 - 1) / kUnit8;
+    if (units <= 0 || pairs <= 0) return pl;
+    const int G = Hq / Hkv;
+    const long long slots = Dh > 128 ? 512 : 1024;
+    const long long target = std::min(std::max(1LL, slots / pairs), kMaxSplits);
+    long long chunk = (units + target - 1) / target;
+    chunk = (chunk + kWaves - 1) / kWaves * kWaves;
+    pl.S = (int)((units + chunk - 1) / chunk);
+    pl.chunk = (int)chunk;
+    pl.own_append = pl.S > 1 && T_new > 0 && W > 0;
+    const long long parts = pl.S > 1 ? pl.S + 1 : 1;
+    pl.counter_bytes = align256((size_t)(B + pairs) * sizeof(unsigned));
+    pl.ml_bytes = parts > 1 ? align256((size_t)(pairs * parts * G * 2) * sizeof(float)) : 0;
+    pl.acc_bytes = parts > 1 ? align256((size_t)(pairs * parts * G * Dh) * sizeof(float)) : 0;
+    pl.total = pl.counter_bytes + pl.ml_bytes + pl.acc_bytes;
+    return pl;
+}
+
 }  // namespace cmc
 
 extern "C" {
@@ -662,6 +687,243 @@ cmc_status cmc_decode_step_ragged(const float *q, const void *cme_k, const void 
                     T_new, W);
     return decode_impl("decode_step_ragged", q, cme_k, cme_v, idx, k_len, k, win_k, win_v, win_count, W, new_k,
                        new_v, T_new, kv_dtype, B, Hq, Hkv, Dh, N, scale, out, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"
+
+// ----------------------------------------------------------- 8-bit cache
+
+namespace {
+
+// Checks shared by the calls on an 8-bit cache array of R rows a head.
+cmc_status check_cache8(const char *fn, cmc_dtype code, int block, int B, int Hkv, int Dh, const char *rows, int R) {
+    if (code != CMC_E4M3 && code != CMC_I8) return fail(CMC_ERR_UNSUPPORTED, "%s: unknown code type %d", fn, (int)code);
+    if (block != 32 && block != 64 && block != 128)
+        return fail(CMC_ERR_UNSUPPORTED, "%s: block=%d not in {32,64,128}", fn, block);
+    if (B < 0 || Hkv < 1 || R < 0)
+        return fail(CMC_ERR_INVALID_ARGUMENT, "%s: need B, %s >= 0 and Hkv >= 1 (got B=%d %s=%d Hkv=%d)", fn, rows, B, rows,
+                    R, Hkv);
+    if (!supported_dh(Dh)) return fail(CMC_ERR_UNSUPPORTED, "%s: Dh=%d not in {64,128,256}", fn, Dh);
+    if (B > 65535 || Hkv > 65535) return fail(CMC_ERR_UNSUPPORTED, "%s: B and Hkv must be <= 65535", fn);
+    if (R > cmc::kCache8MaxRows)
+        return fail(CMC_ERR_UNSUPPORTED, "%s: %s=%d exceeds %d", fn, rows, R, cmc::kCache8MaxRows);
+    return CMC_OK;
+}
+
+cmc_status check_float(const char *fn, cmc_dtype t) {
+    if (t != CMC_F32 && t != CMC_BF16) return fail(CMC_ERR_UNSUPPORTED, "%s: unknown element type %d", fn, (int)t);
+    return CMC_OK;
+}
+
+int log2_of(int n) { return __builtin_ctz((unsigned)n); }
+
+int blocks_of(int rows, int block) { return (int)(((long long)rows + block - 1) / block); }
+
+cmc_status decode8_impl(const char *fn, const float *q, const void *cme_k, const void *cme_v, const float *cme_ks,
+                        const float *cme_vs, const int32_t *k_len, int k, void *win_k, void *win_v, float *win_ks,
+                        float *win_vs, int32_t *win_count, int W, const void *new_k, const void *new_v, int T_new,
+                        cmc_dtype new_dtype, cmc_dtype code, int block, int B, int Hq, int Hkv, int Dh, int N,
+                        float scale, float *out, void *workspace, size_t workspace_bytes, void *stream) {
+    if (cmc_status st = check_cache8(fn, code, block, B, Hkv, Dh, "W", W)) return st;
+    if (cmc_status st = check_cache8(fn, code, block, B, Hkv, Dh, "N", N)) return st;
+    if (Hq < 1 || k < 0) return fail(CMC_ERR_INVALID_ARGUMENT, "%s: need Hq >= 1 and k >= 0", fn);
+    if (Hq % Hkv != 0) return fail(CMC_ERR_INVALID_ARGUMENT, "%s: Hq=%d not a multiple of Hkv=%d", fn, Hq, Hkv);
+    const int G = Hq / Hkv;
+    if (G != 1 && G != 2 && G != 4 && G != 8)
+        return fail(CMC_ERR_UNSUPPORTED, "%s: Hq/Hkv=%d not in {1,2,4,8}", fn, G);
+    if ((long long)k + W < 1) return fail(CMC_ERR_INVALID_ARGUMENT, "%s: empty cache (k + W = 0)", fn);
+    if (k > N) return fail(CMC_ERR_INVALID_ARGUMENT, "%s: k=%d exceeds N=%d", fn, k, N);
+    if (!(scale == scale) || isinf(scale)) return fail(CMC_ERR_INVALID_ARGUMENT, "%s: scale must be finite", fn);
+    if (T_new < 0 || (W > 0 && T_new > W))
+        return fail(CMC_ERR_INVALID_ARGUMENT, "%s: need 0 <= T_new <= W (got T_new=%d W=%d)", fn, T_new, W);
+    if (W == 0) T_new = 0;  // no Tier-2: appending is a no-op
+    if (T_new > cmc::kMaxAppendRows)
+        return fail(CMC_ERR_UNSUPPORTED, "%s: T_new=%d exceeds %d rows per call", fn, T_new, cmc::kMaxAppendRows);
+    if (T_new > 0) {
+        if (cmc_status st = check_float(fn, new_dtype)) return st;
+    }
+    if (B == 0) return ok();
+    if (!q || !out) return fail(CMC_ERR_INVALID_ARGUMENT, "%s: q and out must be non-null", fn);
+    if (k > 0 && (!cme_k || !cme_v || !cme_ks || !cme_vs))
+        return fail(CMC_ERR_INVALID_ARGUMENT, "%s: null Tier-1 codes or scales", fn);
+    if (W > 0 && (!win_k || !win_v || !win_ks || !win_vs || !win_count))
+        return fail(CMC_ERR_INVALID_ARGUMENT, "%s: null Tier-2 window", fn);
+    if (T_new > 0 && (!new_k || !new_v)) return fail(CMC_ERR_INVALID_ARGUMENT, "%s: null new rows", fn);
+    if (misaligned(q) || misaligned(cme_k) || misaligned(cme_v) || misaligned(cme_ks) || misaligned(cme_vs) ||
+        misaligned(k_len) || misaligned(win_k) || misaligned(win_v) || misaligned(win_ks) || misaligned(win_vs) ||
+        misaligned(win_count) || misaligned(out) || misaligned(workspace) || misaligned(new_k) || misaligned(new_v))
+        return fail(CMC_ERR_UNSUPPORTED, "%s: every pointer must be 16-byte aligned", fn);
+    const cmc::DecodePlan pl = cmc::plan_decode8(B, Hq, Hkv, Dh, k, W, T_new);
+    const size_t need = cmc_decode_q8_workspace_bytes(B, Hq, Hkv, Dh, k, W);
+    if (!workspace || workspace_bytes < need)
+        return fail(CMC_ERR_WORKSPACE_TOO_SMALL, "%s: workspace of %zu bytes needed, %zu given", fn, need,
+                    workspace ? workspace_bytes : (size_t)0);
+    cmc::Decode8Params p{};
+    char *const counters = static_cast<char *>(workspace);
+    char *const partials = counters + pl.counter_bytes;
+    p.q = q;
+    p.cme_k = cme_k;
+    p.cme_v = cme_v;
+    p.cme_ks = cme_ks;
+    p.cme_vs = cme_vs;
+    p.k_len = k_len;
+    p.win_k = win_k;
+    p.win_v = win_v;
+    p.win_ks = win_ks;
+    p.win_vs = win_vs;
+    p.win_count = W > 0 ? win_count : nullptr;
+    p.new_k = new_k;
+    p.new_v = new_v;
+    p.new_bf16 = new_dtype == CMC_BF16;
+    p.out = out;
+    p.seq_counter = reinterpret_cast<unsigned *>(counters);
+    p.pair_counter = reinterpret_cast<unsigned *>(counters) + B;
+    p.part_ml = reinterpret_cast<float *>(partials);
+    p.part_acc = reinterpret_cast<float *>(partials + pl.ml_bytes);
+    p.k = k;
+    p.W = W;
+    p.B = B;
+    p.Hq = Hq;
+    p.Hkv = Hkv;
+    p.N = N;
+    p.T_new = T_new;
+    p.new_split = pl.own_append ? 1 : 0;
+    p.S = pl.S + p.new_split;
+    p.chunk = pl.chunk;
+    p.waves = pl.waves;
+    p.qscale = cmc::decode_qscale(scale);
+    p.pool_blocks = blocks_of(N, block);
+    p.ring_blocks = blocks_of(W, block);
+    p.log2_block = log2_of(block);
+    hipError_t e = cmc::launch_decode8(p, code == CMC_E4M3, G, Dh, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "decode launch");
+    return ok();
+}
+
+}  // namespace
+
+extern "C" {
+
+cmc_status cmc_gather_tier1_q8(const void *cme_k, const void *cme_v, cmc_dtype kv_dtype, const int32_t *idx,
+                               const int32_t *k_len, int idx_stride, int B, int Hkv, int N, int k, int Dh,
+                               cmc_dtype code, int block, void *out_k, void *out_v, float *out_ks, float *out_vs,
+                               void *stream) {
+    if (cmc_status st = check_float("gather_q8", kv_dtype)) return st;
+    if (cmc_status st = check_cache8("gather_q8", code, block, B, Hkv, Dh, "k", k)) return st;
+    if (N < 0) return fail(CMC_ERR_INVALID_ARGUMENT, "gather_q8: need N >= 0 (got N=%d)", N);
+    if (idx && idx_stride < k)
+        return fail(CMC_ERR_INVALID_ARGUMENT, "gather_q8: idx_stride=%d is below k=%d", idx_stride, k);
+    if (!idx && k > N) return fail(CMC_ERR_INVALID_ARGUMENT, "gather_q8: k=%d exceeds N=%d with idx == NULL", k, N);
+    if (k > 0 && N < 1) return fail(CMC_ERR_INVALID_ARGUMENT, "gather_q8: k=%d rows from an empty pool", k);
+    if (B == 0 || k == 0) return ok();
+    if (!cme_k || !cme_v || !out_k || !out_v || !out_ks || !out_vs)
+        return fail(CMC_ERR_INVALID_ARGUMENT, "gather_q8: null pointer");
+    if (misaligned(cme_k) || misaligned(cme_v) || misaligned(idx) || misaligned(k_len) || misaligned(out_k) ||
+        misaligned(out_v) || misaligned(out_ks) || misaligned(out_vs))
+        return fail(CMC_ERR_UNSUPPORTED, "gather_q8: every pointer must be 16-byte aligned");
+    cmc::Write8Params p{};
+    p.src_k = cme_k;
+    p.src_v = cme_v;
+    p.idx = idx;
+    p.count = const_cast<int32_t *>(k_len);  // read only
+    p.k = out_k;
+    p.v = out_v;
+    p.ks = out_ks;
+    p.vs = out_vs;
+    p.B = B;
+    p.Hkv = Hkv;
+    p.R = k;
+    p.blocks = blocks_of(k, block);
+    p.src_rows = N;
+    p.idx_stride = idx_stride;
+    p.row_shift = log2_of(Dh / 16);
+    p.log2_block = log2_of(block);
+    hipError_t e = cmc::launch_gather8(p, kv_dtype == CMC_BF16, code == CMC_E4M3, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "gather_q8 launch");
+    return ok();
+}
+
+cmc_status cmc_window_append_q8(void *win_k, void *win_v, float *win_ks, float *win_vs, cmc_dtype code, int block,
+                                int32_t *win_count, const void *new_k, const void *new_v, cmc_dtype new_dtype, int B,
+                                int Hkv, int W, int Dh, int T_new, void *stream) {
+    if (cmc_status st = check_float("append_q8", new_dtype)) return st;
+    if (cmc_status st = check_cache8("append_q8", code, block, B, Hkv, Dh, "W", W)) return st;
+    if (W == 0 || B == 0) return ok();
+    if (T_new < 1 || T_new > W)
+        return fail(CMC_ERR_INVALID_ARGUMENT, "append_q8: need 1 <= T_new <= W (got T_new=%d W=%d)", T_new, W);
+    if (!win_k || !win_v || !win_ks || !win_vs || !win_count || !new_k || !new_v)
+        return fail(CMC_ERR_INVALID_ARGUMENT, "append_q8: null pointer");
+    if (misaligned(win_k) || misaligned(win_v) || misaligned(win_ks) || misaligned(win_vs) || misaligned(win_count) ||
+        misaligned(new_k) || misaligned(new_v))
+        return fail(CMC_ERR_UNSUPPORTED, "append_q8: every pointer must be 16-byte aligned");
+    cmc::Write8Params p{};
+    p.src_k = new_k;
+    p.src_v = new_v;
+    p.count = win_count;
+    p.k = win_k;
+    p.v = win_v;
+    p.ks = win_ks;
+    p.vs = win_vs;
+    p.B = B;
+    p.Hkv = Hkv;
+    p.R = W;
+    p.blocks = blocks_of(W, block);
+    p.src_rows = T_new;
+    p.T_new = T_new;
+    p.row_shift = log2_of(Dh / 16);
+    p.log2_block = log2_of(block);
+    hipError_t e = cmc::launch_append8(p, new_dtype == CMC_BF16, code == CMC_E4M3, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "append_q8 launch");
+    return ok();
+}
+
+cmc_status cmc_cache_read_q8(const void *k8, const void *v8, const float *ks, const float *vs, cmc_dtype code, int block,
+                             const int32_t *count, int B, int Hkv, int R, int Dh, cmc_dtype out_dtype, void *out_k,
+                             void *out_v, void *stream) {
+    if (cmc_status st = check_float("cache_read_q8", out_dtype)) return st;
+    if (cmc_status st = check_cache8("cache_read_q8", code, block, B, Hkv, Dh, "R", R)) return st;
+    if (B == 0 || R == 0) return ok();
+    if (!k8 || !v8 || !ks || !vs || !out_k || !out_v)
+        return fail(CMC_ERR_INVALID_ARGUMENT, "cache_read_q8: null pointer");
+    if (misaligned(k8) || misaligned(v8) || misaligned(ks) || misaligned(vs) || misaligned(count) ||
+        misaligned(out_k) || misaligned(out_v))
+        return fail(CMC_ERR_UNSUPPORTED, "cache_read_q8: every pointer must be 16-byte aligned");
+    cmc::Read8Params p{k8, v8, ks, vs, count, out_k, out_v, B, Hkv, R, blocks_of(R, block), log2_of(Dh / 16),
+                       log2_of(block)};
+    hipError_t e = cmc::launch_read8(p, out_dtype == CMC_BF16, code == CMC_E4M3, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "cache_read_q8 launch");
+    return ok();
+}
+
+size_t cmc_decode_q8_workspace_bytes(int B, int Hq, int Hkv, int Dh, int k, int W) {
+    if (B < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || k < 0 || W < 0 || !supported_dh(Dh)) return 0;
+    return std::max(cmc::plan_decode8(B, Hq, Hkv, Dh, k, W, 0).total, cmc::plan_decode8(B, Hq, Hkv, Dh, k, W, 1).total);
+}
+
+cmc_status cmc_two_tier_decode_q8(const float *q, const void *cme_k, const void *cme_v, const float *cme_ks,
+                                  const float *cme_vs, const int32_t *k_len, int k, const void *win_k,
+                                  const void *win_v, const float *win_ks, const float *win_vs,
+                                  const int32_t *win_count, int W, cmc_dtype code, int block, int B, int Hq, int Hkv,
+                                  int Dh, int N, float scale, float *out, void *workspace, size_t workspace_bytes,
+                                  void *stream) {
+    // Nothing is appended (T_new = 0), so the window is only read.
+    return decode8_impl("decode_q8", q, cme_k, cme_v, cme_ks, cme_vs, k_len, k, const_cast<void *>(win_k),
+                        const_cast<void *>(win_v), const_cast<float *>(win_ks), const_cast<float *>(win_vs),
+                        const_cast<int32_t *>(win_count), W, nullptr, nullptr, 0, CMC_F32, code, block, B, Hq, Hkv, Dh,
+                        N, scale, out, workspace, workspace_bytes, stream);
+}
+
+cmc_status cmc_decode_step_q8(const float *q, const void *cme_k, const void *cme_v, const float *cme_ks,
+                              const float *cme_vs, const int32_t *k_len, int k, void *win_k, void *win_v,
+                              float *win_ks, float *win_vs, int32_t *win_count, int W, const void *new_k,
+                              const void *new_v, int T_new, cmc_dtype new_dtype, cmc_dtype code, int block, int B,
+                              int Hq, int Hkv, int Dh, int N, float scale, float *out, void *workspace,
+                              size_t workspace_bytes, void *stream) {
+    if (W > 0 && T_new < 1)
+        return fail(CMC_ERR_INVALID_ARGUMENT, "decode_step_q8: need 1 <= T_new <= W (got T_new=%d W=%d)", T_new, W);
+    return decode8_impl("decode_step_q8", q, cme_k, cme_v, cme_ks, cme_vs, k_len, k, win_k, win_v, win_ks, win_vs,
+                        win_count, W, new_k, new_v, T_new, new_dtype, code, block, B, Hq, Hkv, Dh, N, scale, out,
+                        workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -78,6 +78,53 @@ struct GatherParams {
 };
 hipError_t launch_gather(const GatherParams &p, hipStream_t stream);
 
+// Advances every sequence's count by T_new (negative counts from 0).
+hipError_t launch_window_count(int32_t *win_count, int B, int T_new, hipStream_t stream);
+
+// The 8-bit cache (format: cache8.hpp).  Rows of Dh codes are counted in
+// 16-code words: row_shift = log2(Dh / 16).
+struct Write8Params {
+    const void *src_k, *src_v;  // gather: [B][Hkv][src_rows][Dh] pool; append: [B][Hkv][T_new][Dh] rows
+    const int32_t *idx;         // gather: [B][idx_stride] pool rows, or nullptr: rows 0..R-1
+    int32_t *count;             // gather: [B] rows written, or nullptr: all R; append: [B] ring counts, advanced by T_new
+    void *k, *v;                // [B][Hkv][R][Dh] codes
+    float *ks, *vs;             // [B][Hkv][blocks] scales
+    int B, Hkv, R, blocks, src_rows, idx_stride, T_new;
+    int row_shift, log2_block;
+};
+hipError_t launch_gather8(const Write8Params &p, bool bf16, bool e4m3, hipStream_t stream);
+hipError_t launch_append8(const Write8Params &p, bool bf16, bool e4m3, hipStream_t stream);
+
+struct Read8Params {
+    const void *k, *v;        // [B][Hkv][R][Dh] codes
+    const float *ks, *vs;     // [B][Hkv][blocks] scales
+    const int32_t *count;     // [B] rows ever written, or nullptr: R
+    void *out_k, *out_v;      // [B][Hkv][R][Dh] fp32 or bf16
+    int B, Hkv, R, blocks;
+    int row_shift, log2_block;
+};
+// Rows of a cache array: row and word indices of one (sequence, kv head) stay
+// within 32 bits.
+constexpr int kCache8MaxRows = 1 << 26;
+hipError_t launch_read8(const Read8Params &p, bool bf16, bool e4m3, hipStream_t stream);
+
+// Decode over the 8-bit cache.  cme_k/v and win_k/v hold codes; the pool is
+// read in row order (idx is not used) and N counts its rows.
+struct Decode8Params : DecodeParams {
+    const float *cme_ks, *cme_vs;  // [B][Hkv][pool_blocks]
+    float *win_ks, *win_vs;        // [B][Hkv][ring_blocks]; written only for blocks that this call appends to
+    int pool_blocks, ring_blocks, log2_block;
+    bool new_bf16;                 // type of new_k/v
+};
+// Rows a wave takes at a time; chunk and the plan count in these.
+constexpr int kUnit8 = 32;
+DecodePlan plan_decode8(int B, int Hq, int Hkv, int Dh, int k, int W, int T_new);
+hipError_t launch_decode8(const Decode8Params &p, bool e4m3, int G, int Dh, hipStream_t stream);
+
+// Most appended rows that one workgroup per sequence takes (see
+// launch_append in cache8.hip).
+constexpr int kAppend8OneWg = 4;
+
 struct SelectParams {
     const void *sel_keys;     // [B][N][D] fp32 or bf16 (keys_bf16)
     const float *q_vec;       // [B][D]

@@ -176,7 +176,11 @@ hipError_t launch_window_append(const AppendParams &p, hipStream_t stream) {
     window_copy_kernel<<<dim3(grid, p.B), 256, 0, stream>>>(p, row_shift, groups, head_vecs);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    window_count_kernel<<<(p.B + 255) / 256, 256, 0, stream>>>(p.win_count, p.B, p.T_new);
+    return launch_window_count(p.win_count, p.B, p.T_new, stream);
+}
+
+hipError_t launch_window_count(int32_t *win_count, int B, int T_new, hipStream_t stream) {
+    window_count_kernel<<<(B + 255) / 256, 256, 0, stream>>>(win_count, B, T_new);
     return hipGetLastError();
 }
 
