@@ -604,34 +604,40 @@ def _code_dtype(t) -> int:
     raise TypeError(f"expected float8_e4m3fn or int8 codes, got {d}")
 
 
-def _ptrs(*tensors):
-    """Device addresses of tensors (None passes through) that all lie on the
-    current device, whose stream the call runs on."""
-    if _torch is None:
-        _load_torch()
-    dev = _device_index()
-    out = []
+# The checks below are written out, with few calls and each attribute fetched
+# once: a wrapper that goes through helpers per tensor takes longer on the host
+# than a small call on the GPU.
+_q8_calls = None
+
+
+def _load_q8():
+    """The C functions of the 8-bit cache, looked up once."""
+    global _q8_calls
+    L = lib()
+    _q8_calls = (L.cmc_gather_tier1_q8, L.cmc_window_append_q8, L.cmc_cache_read_q8, L.cmc_two_tier_decode_q8,
+                 L.cmc_decode_step_q8)
+    return _q8_calls
+
+
+def _elsewhere(dev, *tensors):
+    """Raises for the first tensor that is not on the current device, whose
+    stream the call would run on."""
     for t in tensors:
-        if t is None:
-            out.append(None)
-            continue
-        if t.get_device() != dev:
+        if t is not None and t.get_device() != dev:
             if not t.is_cuda:
                 _on_host(t)
             raise ValueError(f"cmc: tensor of shape {tuple(t.shape)} is on {t.device}, not on the current device cuda:{dev}")
-        out.append(t.data_ptr())
-    return out
 
 
 def _cache_args(name, codes_k, codes_v, scales_k, scales_v, block):
     """Checks of one 8-bit cache array pair; returns its (B, Hkv, R, Dh)."""
-    torch = _torch or _load_torch()
+    f32 = _torch.float32
     s = codes_k.shape
     if not (len(s) == 4 and codes_v.shape == s and codes_v.dtype is codes_k.dtype):
         raise ValueError(f"{name}_k/v must be matching codes [B][Hkv][rows][Dh]")
-    n = (s[0], s[1], -(-s[2] // block) if block > 0 else 0)
-    if not (scales_k.shape == n and scales_v.shape == n and scales_k.dtype is torch.float32
-            and scales_v.dtype is torch.float32):
+    B, Hkv, R, _ = s
+    n = (B, Hkv, -(-R // block) if block > 0 else -1)
+    if not (scales_k.shape == n and scales_v.shape == n and scales_k.dtype is f32 and scales_v.dtype is f32):
         raise ValueError(f"{name}_ks/vs must be fp32 [B][Hkv][ceil(rows / block)]")
     if not (codes_k.is_contiguous() and codes_v.is_contiguous() and scales_k.is_contiguous()
             and scales_v.is_contiguous()):
@@ -647,33 +653,57 @@ def cmc_gather_tier1_q8(cme_k, cme_v, idx, k: int, block: int, k_len=None, dtype
     is not given.  Returns (out_k, out_v [B][Hkv][k][Dh], out_ks, out_vs
     [B][Hkv][ceil(k / block)] fp32)."""
     torch = _torch or _load_torch()
-    _need(cme_k.dim() == 4 and cme_k.is_contiguous() and cme_v.is_contiguous() and cme_v.shape == cme_k.shape
-          and cme_v.dtype == cme_k.dtype, "cme_k/v [B][Hkv][N][Dh]")
-    B, Hkv, N, Dh = cme_k.shape
-    _need(block > 0, "block must be positive")
+    k, block = int(k), int(block)
+    ps = cme_k.shape
+    if not (len(ps) == 4 and cme_v.shape == ps and cme_v.dtype is cme_k.dtype and cme_k.is_contiguous()
+            and cme_v.is_contiguous()):
+        raise ValueError("cme_k/v [B][Hkv][N][Dh]")
+    B, Hkv, N, Dh = ps
+    if block < 1 or k < 0:
+        raise ValueError("block must be positive and k at least 0")
     stride = 0
     if idx is not None:
-        _need(idx.dim() == 2 and idx.shape[0] == B and idx.dtype == torch.int32 and idx.is_contiguous(),
-              "idx [B][idx_stride] int32")
-        stride = int(idx.shape[1])
-    if k_len is not None:
-        _need(k_len.shape == (B,) and k_len.dtype == torch.int32 and k_len.is_contiguous(), "k_len [B] int32")
-    dev = cme_k.device
+        i = idx.shape
+        if not (len(i) == 2 and i[0] == B and idx.dtype is torch.int32 and idx.is_contiguous()):
+            raise ValueError("idx [B][idx_stride] int32")
+        stride = i[1]
+    if k_len is not None and not (k_len.shape == (B,) and k_len.dtype is torch.int32 and k_len.is_contiguous()):
+        raise ValueError("k_len [B] int32")
     if out_k is None:
-        out_k = torch.empty((B, Hkv, k, Dh), dtype=dtype or torch.float8_e4m3fn, device=dev)
+        out_k = torch.empty((B, Hkv, k, Dh), dtype=dtype or torch.float8_e4m3fn, device=cme_k.device)
     if out_v is None:
-        out_v = torch.empty((B, Hkv, k, Dh), dtype=out_k.dtype, device=dev)
-    n = -(-k // block)
+        out_v = torch.empty_like(out_k)
     if out_ks is None:
-        out_ks = torch.empty((B, Hkv, n), dtype=torch.float32, device=dev)
+        out_ks = torch.empty((B, Hkv, -(-k // block)), dtype=torch.float32, device=cme_k.device)
     if out_vs is None:
-        out_vs = torch.empty((B, Hkv, n), dtype=torch.float32, device=dev)
-    _need(_cache_args("out", out_k, out_v, out_ks, out_vs, block) == (B, Hkv, k, Dh), "out_k/v [B][Hkv][k][Dh]")
-    pk, pv, pi, pl, ok, ov, oks, ovs = _ptrs(cme_k, cme_v, idx, k_len, out_k, out_v, out_ks, out_vs)
-    rc = lib().cmc_gather_tier1_q8(pk, pv, _kv_dtype(cme_k), pi, pl, stride, B, Hkv, N, int(k), Dh, _code_dtype(out_k),
-                                   int(block), ok, ov, oks, ovs, _stream(stream))
-    _check(rc)
+        out_vs = torch.empty_like(out_ks)
+    if _cache_args("out", out_k, out_v, out_ks, out_vs, block) != (B, Hkv, k, Dh):
+        raise ValueError("out_k/v [B][Hkv][k][Dh]")
+    dev = _device_index()
+    if (cme_k.get_device() != dev or cme_v.get_device() != dev or out_k.get_device() != dev or out_v.get_device() != dev
+            or out_ks.get_device() != dev or out_vs.get_device() != dev
+            or (idx is not None and idx.get_device() != dev) or (k_len is not None and k_len.get_device() != dev)):
+        _elsewhere(dev, cme_k, cme_v, idx, k_len, out_k, out_v, out_ks, out_vs)
+    rc = (_q8_calls or _load_q8())[0](
+        cme_k.data_ptr(), cme_v.data_ptr(), _kv_dtype(cme_k), None if idx is None else idx.data_ptr(),
+        None if k_len is None else k_len.data_ptr(), stride, B, Hkv, N, k, Dh, _code_dtype(out_k), block,
+        out_k.data_ptr(), out_v.data_ptr(), out_ks.data_ptr(), out_vs.data_ptr(),
+        _raw_stream(dev) if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
     return out_k, out_v, out_ks, out_vs
+
+
+def _new_rows(new_k, new_v, B, Hkv, Dh):
+    """Checks of the rows to append; returns their number."""
+    s = new_k.shape
+    if not (len(s) == 4 and s[0] == B and s[1] == Hkv and s[3] == Dh):
+        raise ValueError("new_k [B][Hkv][T][Dh]")
+    if not (new_v.shape == s and new_v.dtype is new_k.dtype):
+        raise ValueError("new_k/v must match")
+    if not (new_k.is_contiguous() and new_v.is_contiguous()):
+        raise ValueError("new_k/v must be contiguous")
+    return s[2]
 
 
 def cmc_window_append_q8(win_k, win_v, win_ks, win_vs, win_count, new_k, new_v, block: int, stream=None) -> None:
@@ -681,16 +711,22 @@ def cmc_window_append_q8(win_k, win_v, win_ks, win_vs, win_count, new_k, new_v, 
     win_ks/vs [B][Hkv][ceil(W / block)] fp32, win_count [B] int32, new_*
     [B][Hkv][T][Dh] fp32 or bf16."""
     torch = _torch or _load_torch()
+    block = int(block)
     B, Hkv, W, Dh = _cache_args("win", win_k, win_v, win_ks, win_vs, block)
-    _need(new_k.dim() == 4 and new_k.shape[:2] == (B, Hkv) and new_k.shape[3] == Dh, "new_k [B][Hkv][T][Dh]")
-    _need(new_v.shape == new_k.shape and new_v.dtype == new_k.dtype, "new_k/v must match")
-    _need(new_k.is_contiguous() and new_v.is_contiguous(), "new_k/v must be contiguous")
-    _need(win_count.shape == (B,) and win_count.dtype == torch.int32 and win_count.is_contiguous(),
-          "win_count [B] int32")
-    wk, wv, wks, wvs, wc, nk, nv = _ptrs(win_k, win_v, win_ks, win_vs, win_count, new_k, new_v)
-    rc = lib().cmc_window_append_q8(wk, wv, wks, wvs, _code_dtype(win_k), int(block), wc, nk, nv, _kv_dtype(new_k), B,
-                                    Hkv, W, Dh, int(new_k.shape[2]), _stream(stream))
-    _check(rc)
+    T = _new_rows(new_k, new_v, B, Hkv, Dh)
+    if not (win_count.shape == (B,) and win_count.dtype is torch.int32 and win_count.is_contiguous()):
+        raise ValueError("win_count [B] int32")
+    dev = _device_index()
+    if (win_k.get_device() != dev or win_v.get_device() != dev or win_ks.get_device() != dev
+            or win_vs.get_device() != dev or win_count.get_device() != dev or new_k.get_device() != dev
+            or new_v.get_device() != dev):
+        _elsewhere(dev, win_k, win_v, win_ks, win_vs, win_count, new_k, new_v)
+    rc = (_q8_calls or _load_q8())[1](
+        win_k.data_ptr(), win_v.data_ptr(), win_ks.data_ptr(), win_vs.data_ptr(), _code_dtype(win_k), block,
+        win_count.data_ptr(), new_k.data_ptr(), new_v.data_ptr(), _kv_dtype(new_k), B, Hkv, W, Dh, T,
+        _raw_stream(dev) if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
 
 
 def cmc_cache_read_q8(k8, v8, ks, vs, block: int, count=None, dtype=None, out_k=None, out_v=None, stream=None):
@@ -699,19 +735,29 @@ def cmc_cache_read_q8(k8, v8, ks, vs, block: int, count=None, dtype=None, out_k=
     or bf16 (`dtype`, bf16 unless said otherwise, where out_k is not given).
     count [B] int32, or None for R rows.  Returns (out_k, out_v)."""
     torch = _torch or _load_torch()
-    B, Hkv, R, Dh = _cache_args("cache", k8, v8, ks, vs, block)
-    if count is not None:
-        _need(count.shape == (B,) and count.dtype == torch.int32 and count.is_contiguous(), "count [B] int32")
+    block = int(block)
+    s = _cache_args("cache", k8, v8, ks, vs, block)
+    B, Hkv, R, Dh = s
+    if count is not None and not (count.shape == (B,) and count.dtype is torch.int32 and count.is_contiguous()):
+        raise ValueError("count [B] int32")
     if out_k is None:
-        out_k = torch.empty((B, Hkv, R, Dh), dtype=dtype or torch.bfloat16, device=k8.device)
+        out_k = torch.empty(s, dtype=dtype or torch.bfloat16, device=k8.device)
     if out_v is None:
-        out_v = torch.empty((B, Hkv, R, Dh), dtype=out_k.dtype, device=k8.device)
-    _need(out_k.shape == (B, Hkv, R, Dh) and out_v.shape == out_k.shape and out_v.dtype == out_k.dtype
-          and out_k.is_contiguous() and out_v.is_contiguous(), "out_k/v [B][Hkv][R][Dh]")
-    ck, cv, sk, sv, n, ok, ov = _ptrs(k8, v8, ks, vs, count, out_k, out_v)
-    rc = lib().cmc_cache_read_q8(ck, cv, sk, sv, _code_dtype(k8), int(block), n, B, Hkv, R, Dh, _kv_dtype(out_k), ok, ov,
-                                 _stream(stream))
-    _check(rc)
+        out_v = torch.empty_like(out_k)
+    if not (out_k.shape == s and out_v.shape == s and out_v.dtype is out_k.dtype and out_k.is_contiguous()
+            and out_v.is_contiguous()):
+        raise ValueError("out_k/v [B][Hkv][R][Dh]")
+    dev = _device_index()
+    if (k8.get_device() != dev or v8.get_device() != dev or ks.get_device() != dev or vs.get_device() != dev
+            or out_k.get_device() != dev or out_v.get_device() != dev
+            or (count is not None and count.get_device() != dev)):
+        _elsewhere(dev, k8, v8, ks, vs, count, out_k, out_v)
+    rc = (_q8_calls or _load_q8())[2](
+        k8.data_ptr(), v8.data_ptr(), ks.data_ptr(), vs.data_ptr(), _code_dtype(k8), block,
+        None if count is None else count.data_ptr(), B, Hkv, R, Dh, _kv_dtype(out_k), out_k.data_ptr(), out_v.data_ptr(),
+        _raw_stream(dev) if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
     return out_k, out_v
 
 
@@ -726,37 +772,73 @@ def decode_workspace_q8(B: int, Hq: int, Hkv: int, Dh: int, k: int, W: int, devi
     return torch.zeros(max(1, cmc_decode_q8_workspace_bytes(B, Hq, Hkv, Dh, k, W)), dtype=torch.uint8, device=device)
 
 
-def _decode_q8_args(q, cme_k, cme_v, cme_ks, cme_vs, k, win_k, win_v, win_ks, win_vs, win_count, block, k_len, out,
-                    workspace):
-    """Checks shared by the 8-bit decode wrappers; returns (B, Hq, Hkv, Dh, N,
-    W, out, workspace, its bytes)."""
+def _decode_q8(step, q, cme_k, cme_v, cme_ks, cme_vs, k, win_k, win_v, win_ks, win_vs, win_count, new_k, new_v, scale,
+               block, k_len, out, workspace, stream):
+    """Both decode calls: the checks, then the C call."""
     torch = _torch or _load_torch()
     f32, i32 = torch.float32, torch.int32
+    k, block = int(k), int(block)
     qs = q.shape
     if not (len(qs) == 3 and q.dtype is f32 and q.is_contiguous()):
         raise ValueError("q must be contiguous fp32 [B][Hq][Dh]")
     B, Hq, Dh = qs
-    _, Hkv, N, _ = s = _cache_args("cme", cme_k, cme_v, cme_ks, cme_vs, block)
+    s = _cache_args("cme", cme_k, cme_v, cme_ks, cme_vs, block)
+    _, Hkv, N, _ = s
     if not (s[0] == B and s[3] == Dh):
         raise ValueError("cme_k/v [B][Hkv][N][Dh]")
-    W = 0
+    code = cme_k.dtype
+    W = T = 0
     if win_k is not None:
         s = _cache_args("win", win_k, win_v, win_ks, win_vs, block)
         W = s[2]
-        if not (s == (B, Hkv, W, Dh) and win_k.dtype is cme_k.dtype):
+        if not (s == (B, Hkv, W, Dh) and win_k.dtype is code):
             raise ValueError("win_k/v [B][Hkv][W][Dh], codes as cme_k/v")
         if not (win_count is not None and win_count.shape == (B,) and win_count.dtype is i32
                 and win_count.is_contiguous()):
             raise ValueError("win_count [B] int32")
+        if step and W > 0:
+            T = _new_rows(new_k, new_v, B, Hkv, Dh)
     if k_len is not None and not (k_len.shape == (B,) and k_len.dtype is i32 and k_len.is_contiguous()):
         raise ValueError("k_len [B] int32")
     if out is None:
-        out = torch.empty((B, Hq, Dh), dtype=f32, device=q.device)
+        out = torch.empty(qs, dtype=f32, device=q.device)
     elif not (out.shape == qs and out.dtype is f32 and out.is_contiguous()):
         raise ValueError("out [B][Hq][Dh] fp32")
     if workspace is None:
         workspace = decode_workspace_q8(B, Hq, Hkv, Dh, k, W, q.device)
-    return B, Hq, Hkv, Dh, N, W, out, workspace, workspace.numel() * workspace.element_size()
+    dev = _device_index()
+    if (q.get_device() != dev or out.get_device() != dev or workspace.get_device() != dev or cme_k.get_device() != dev
+            or cme_v.get_device() != dev or cme_ks.get_device() != dev or cme_vs.get_device() != dev
+            or (k_len is not None and k_len.get_device() != dev)):
+        _elsewhere(dev, q, out, workspace, cme_k, cme_v, cme_ks, cme_vs, k_len)
+    wk = wv = wks = wvs = wc = nk = nv = None
+    if W > 0:
+        if (win_k.get_device() != dev or win_v.get_device() != dev or win_ks.get_device() != dev
+                or win_vs.get_device() != dev or win_count.get_device() != dev):
+            _elsewhere(dev, win_k, win_v, win_ks, win_vs, win_count)
+        wk, wv, wks, wvs, wc = (win_k.data_ptr(), win_v.data_ptr(), win_ks.data_ptr(), win_vs.data_ptr(),
+                                win_count.data_ptr())
+    kl = None if k_len is None else k_len.data_ptr()
+    c = CMC_E4M3 if code is torch.float8_e4m3fn else _code_dtype(cme_k)
+    ws_bytes = workspace.numel() * workspace.element_size()
+    st = _raw_stream(dev) if stream is None else _stream(stream)
+    calls = _q8_calls or _load_q8()
+    if step:
+        new_dtype = CMC_F32
+        if T > 0:
+            if new_k.get_device() != dev or new_v.get_device() != dev:
+                _elsewhere(dev, new_k, new_v)
+            nk, nv, new_dtype = new_k.data_ptr(), new_v.data_ptr(), _kv_dtype(new_k)
+        rc = calls[4](q.data_ptr(), cme_k.data_ptr(), cme_v.data_ptr(), cme_ks.data_ptr(), cme_vs.data_ptr(), kl, k, wk, wv,
+                      wks, wvs, wc, W, nk, nv, T, new_dtype, c, block, B, Hq, Hkv, Dh, N, scale, out.data_ptr(),
+                      workspace.data_ptr(), ws_bytes, st)
+    else:
+        rc = calls[3](q.data_ptr(), cme_k.data_ptr(), cme_v.data_ptr(), cme_ks.data_ptr(), cme_vs.data_ptr(), kl, k, wk, wv,
+                      wks, wvs, wc, W, c, block, B, Hq, Hkv, Dh, N, scale, out.data_ptr(), workspace.data_ptr(), ws_bytes,
+                      st)
+    if rc:
+        _check(rc)
+    return out
 
 
 def cmc_two_tier_decode_q8(q, cme_k, cme_v, cme_ks, cme_vs, k: int, win_k, win_v, win_ks, win_vs, win_count,
@@ -764,39 +846,13 @@ def cmc_two_tier_decode_q8(q, cme_k, cme_v, cme_ks, cme_vs, k: int, win_k, win_v
     """cmc_two_tier_decode over the 8-bit cache: rows 0 .. k - 1 (k_len[b] - 1)
     of cme_k/v [B][Hkv][N][Dh] codes, then the ring (None: no Tier-2); scales
     [B][Hkv][ceil(rows / block)] fp32.  Returns out [B][Hq][Dh] fp32."""
-    B, Hq, Hkv, Dh, N, W, out, workspace, ws_bytes = _decode_q8_args(
-        q, cme_k, cme_v, cme_ks, cme_vs, k, win_k, win_v, win_ks, win_vs, win_count, block, k_len, out, workspace)
-    if W == 0:
-        win_k = win_v = win_ks = win_vs = win_count = None
-    pq, po, pw, *cache = _ptrs(q, out, workspace, cme_k, cme_v, cme_ks, cme_vs, k_len, win_k, win_v, win_ks, win_vs,
-                               win_count)
-    rc = lib().cmc_two_tier_decode_q8(pq, *cache[:5], int(k), *cache[5:], W, _code_dtype(cme_k), int(block), B, Hq, Hkv,
-                                      Dh, N, float(scale), po, pw, ws_bytes, _stream(stream))
-    _check(rc)
-    return out
+    return _decode_q8(False, q, cme_k, cme_v, cme_ks, cme_vs, k, win_k, win_v, win_ks, win_vs, win_count, None, None, scale,
+                      block, k_len, out, workspace, stream)
 
 
 def cmc_decode_step_q8(q, cme_k, cme_v, cme_ks, cme_vs, k: int, win_k, win_v, win_ks, win_vs, win_count, new_k, new_v,
                        scale: float, block: int, k_len=None, out=None, workspace=None, stream=None):
     """cmc_window_append_q8 of new_k/new_v [B][Hkv][T][Dh] (fp32 or bf16), then
     cmc_two_tier_decode_q8, in one launch.  Returns out [B][Hq][Dh] fp32."""
-    B, Hq, Hkv, Dh, N, W, out, workspace, ws_bytes = _decode_q8_args(
-        q, cme_k, cme_v, cme_ks, cme_vs, k, win_k, win_v, win_ks, win_vs, win_count, block, k_len, out, workspace)
-    T, new_dtype = 0, CMC_F32
-    if W > 0:
-        ns = new_k.shape
-        if not (len(ns) == 4 and ns[0] == B and ns[1] == Hkv and ns[3] == Dh):
-            raise ValueError("new_k [B][Hkv][T][Dh]")
-        if not (new_v.shape == ns and new_v.dtype is new_k.dtype):
-            raise ValueError("new_k/v must match")
-        if not (new_k.is_contiguous() and new_v.is_contiguous()):
-            raise ValueError("new_k/v must be contiguous")
-        T, new_dtype = ns[2], _kv_dtype(new_k)
-    else:
-        new_k = new_v = win_k = win_v = win_ks = win_vs = win_count = None
-    pq, po, pw, nk, nv, *cache = _ptrs(q, out, workspace, new_k, new_v, cme_k, cme_v, cme_ks, cme_vs, k_len, win_k,
-                                       win_v, win_ks, win_vs, win_count)
-    rc = lib().cmc_decode_step_q8(pq, *cache[:5], int(k), *cache[5:], W, nk, nv, T, new_dtype, _code_dtype(cme_k),
-                                  int(block), B, Hq, Hkv, Dh, N, float(scale), po, pw, ws_bytes, _stream(stream))
-    _check(rc)
-    return out
+    return _decode_q8(True, q, cme_k, cme_v, cme_ks, cme_vs, k, win_k, win_v, win_ks, win_vs, win_count, new_k, new_v, scale,
+                      block, k_len, out, workspace, stream)

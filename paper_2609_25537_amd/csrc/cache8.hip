@@ -5,7 +5,7 @@
 // registers, half its V, so every row is read once; the block's largest
 // magnitude is reduced over the half, and the codes go out as 16-byte stores.
 // A decode step's append (a few rows) takes one workgroup per sequence, a wave
-// per (kv head, K or V, block), and advances the count itself.  All of it is
+// per (kv head, block), and advances the count itself.  All of it is
 // bound by memory, the small calls by latency.
 #include <algorithm>
 
@@ -77,7 +77,7 @@ __global__ __launch_bounds__(1024) void write_blocks_kernel(Write8Params p) {
     if constexpr (RING) {
         float t = 0.f;
 #pragma unroll
-        for (int u = 0; u < NP; ++u) t = fmaxf(t, codes_top<F>(code[u]));
+        for (int u = 0; u < NP; ++u) t = fmaxf(t, F::top16(code[u]));
         old = old_mag(t, old_scale);
     }
     __shared__ uint32_t s_top[2][2][8];
@@ -125,14 +125,14 @@ __global__ __launch_bounds__(1024) void append_rows_kernel(Write8Params p) {
     const int filled = (int)min((long long)count + p.T_new, (long long)p.R);
     TouchedBlocks tb;
     tb.set(slot0, p.T_new, p.R, p.log2_block);
-    const int items = 2 * p.Hkv * tb.count;  // small: see append_one_wg
+    const int items = p.Hkv * tb.count;  // small: see launch_append
     for (int w = threadIdx.x >> 6; w < items; w += (int)(blockDim.x >> 6)) {
-        const bool is_v = w & 1;
-        const size_t head = (size_t)b * p.Hkv + (w >> 1) % p.Hkv;
-        append_block<T, F>(static_cast<const T *>(is_v ? p.src_v : p.src_k) + ((head * p.T_new) << p.row_shift) * 16,
-                           static_cast<uint8_t *>(is_v ? p.v : p.k) + ((head * p.R) << p.row_shift) * 16,
-                           (is_v ? p.vs : p.ks) + head * p.blocks, tb.block((w >> 1) / p.Hkv), p.log2_block,
-                           p.row_shift, p.R, slot0, filled, p.T_new);
+        const size_t head = (size_t)b * p.Hkv + w % p.Hkv;
+        const size_t src = ((head * p.T_new) << p.row_shift) * 16, dst = ((head * p.R) << p.row_shift) * 16;
+        append_block<T, F, kWave>({static_cast<const T *>(p.src_k) + src, static_cast<const T *>(p.src_v) + src},
+                              {static_cast<uint8_t *>(p.k) + dst, static_cast<uint8_t *>(p.v) + dst},
+                              {p.ks + head * p.blocks, p.vs + head * p.blocks}, tb.block(w / p.Hkv), p.log2_block,
+                              p.row_shift, p.R, slot0, filled, p.T_new, nullptr);
     }
     __syncthreads();
     if (threadIdx.x == 0) p.count[b] = count + p.T_new;

@@ -22,6 +22,7 @@
 
 namespace cmc {
 
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
 typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 
@@ -31,6 +32,27 @@ struct CodeE4M3 {
     static constexpr int kTopExp = 8;               // 448 = 1.75 * 2^8
     static constexpr uint32_t kTopFrac = 0x600000;  // .75
     static constexpr bool kHasNaN = true;
+    // The largest magnitude of sixteen codes, as a float; NaN codes do not
+    // count.  Magnitudes order as their codes do, two to a 32-bit operation.
+    __device__ __forceinline__ static float top16(const uint4 &c) {
+        u16x2 t = {0, 0};
+        const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            t = __builtin_elementwise_max(t, __builtin_bit_cast(u16x2, w[i] & 0x007f007fu));
+            t = __builtin_elementwise_max(t, __builtin_bit_cast(u16x2, (w[i] >> 8) & 0x007f007fu));
+        }
+        uint32_t m = t[0] > t[1] ? t[0] : t[1];
+        if (m == 0x7f) {  // a NaN among them
+            m = 0;
+            for (int i = 0; i < 4; ++i)
+                for (int b = 0; b < 32; b += 8) {
+                    const uint32_t x = (w[i] >> b) & 0x7f;
+                    m = x != 0x7f && x > m ? x : m;
+                }
+        }
+        return __builtin_amdgcn_cvt_pk_f32_fp8((int)m, false)[0];
+    }
     // Four values (within [-kMost, kMost] or NaN) to a word of codes.
     __device__ __forceinline__ static uint32_t pack4(float a, float b, float c, float d) {
         const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
@@ -53,6 +75,19 @@ struct CodeI8 {
     static constexpr int kTopExp = 6;               // 127 = 1.984375 * 2^6
     static constexpr uint32_t kTopFrac = 0x7e0000;  // .984375
     static constexpr bool kHasNaN = false;
+    __device__ __forceinline__ static float top16(const uint4 &c) {
+        typedef short s16x2 __attribute__((ext_vector_type(2)));
+        s16x2 hi = {0, 0}, lo = {0, 0};
+        const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const s16x2 odd = __builtin_bit_cast(s16x2, w[i]) >> 8, even = __builtin_bit_cast(s16x2, w[i] << 8) >> 8;
+            hi = __builtin_elementwise_max(hi, __builtin_elementwise_max(odd, even));
+            lo = __builtin_elementwise_min(lo, __builtin_elementwise_min(odd, even));
+        }
+        const int h = hi[0] > hi[1] ? hi[0] : hi[1], l = lo[0] < lo[1] ? lo[0] : lo[1];
+        return (float)(h > -l ? h : -l);
+    }
     // Adding 1.5 * 2^23 rounds to an integer (nearest even), whose two's
     // complement the low bits then hold.
     __device__ __forceinline__ static uint32_t pack4(float a, float b, float c, float d) {
@@ -145,7 +180,6 @@ struct Raw16 {
                 m = max(max(m, max(r[i].x & 0x7fffffffu, r[i].y & 0x7fffffffu)),
                         max(r[i].z & 0x7fffffffu, r[i].w & 0x7fffffffu));
         } else {
-            typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
             u16x2 t = {0, 0};
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -181,16 +215,8 @@ __device__ __forceinline__ void widen16(const uint4 &c, float (&x)[16]) {
     }
 }
 
-// The largest magnitude of sixteen codes; NaN codes do not count.
-template <class F>
-__device__ __forceinline__ float codes_top(const uint4 &c) {
-    float x[16], m = 0.f;
-    widen16<F>(c, x);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) m = fmaxf(m, fabsf(x[e]));
-    return m;
-}
-// That magnitude's share in the block's maximum.  A top of 0 (no live old row,
+// The largest magnitude of a block's old codes as a part of its new maximum.  A
+// top of 0 (no live old row,
 // or only zeros) counts for nothing, whatever the old scale holds.
 __device__ __forceinline__ uint32_t old_mag(float codes_top, float old_scale) {
     return codes_top > 0.f ? finite_mag(codes_top * old_scale) : 0u;
@@ -238,65 +264,114 @@ struct TouchedBlocks {
     }
 };
 
-// One wave brings one ring block of K or V of one (sequence, kv head) up to
-// date with the rows appended at slot0: the scale from the new rows and the
-// live old ones, then the codes.  Where the scale stays, only the new rows are
-// written.  row_shift: log2 of a row's 16-code words; filled: slots that are
-// live after the append.
-template <typename T, class F>
-__device__ __forceinline__ void append_block(const T *rows, uint8_t *codes, float *scales, int j, int log2_block,
-                                             int row_shift, int W, int slot0, int filled, int T_new) {
-    const int lane = threadIdx.x & 63;
+// NT threads (a wave, or a workgroup of NT / 64) bring a ring block of K and V of
+// one (sequence, kv head) up to date with the rows appended at slot0: the
+// scales from the new rows and the live old ones, then the codes.  Where no
+// scale moves, only the new rows are written.  row_shift: log2 of a row's
+// 16-code words; filled: slots that are live after the append.  A workgroup
+// needs s_top[2][NT / 64] in LDS, and a barrier before anyone reads the block or
+// another block is begun.
+template <typename T, class F, int NT>
+__device__ __forceinline__ void append_block(const T *const (&rows)[2], uint8_t *const (&codes)[2], float *const (&scales)[2],
+                                             int j, int log2_block, int row_shift, int W, int slot0, int filled, int T_new,
+                                             uint32_t (*s_top)[NT / 64]) {
+    const int me = NT == kWave ? threadIdx.x & 63 : threadIdx.x;
     const int s0 = j << log2_block;
-    const int live = min(1 << log2_block, filled - s0);
-    const int words = live << row_shift;
-    uint4 *base = reinterpret_cast<uint4 *>(codes) + ((size_t)s0 << row_shift);
+    const int words = min(1 << log2_block, filled - s0) << row_shift;
+    uint4 *base[2];
+    float old_scale[2], old_top[2] = {0.f, 0.f};
+    uint32_t top[2] = {0, 0};
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        base[x] = reinterpret_cast<uint4 *>(codes[x]) + ((size_t)s0 << row_shift);
+        old_scale[x] = scales[x][j];
+    }
     // appended row that word i belongs to; T_new or more: an old row
     const auto row_of = [&](int i) {
         const int t = s0 + (i >> row_shift) - slot0;
         return t < 0 ? t + W : t;
     };
-    const auto new_word = [&](int t, int i) {
-        return rows + (((size_t)t << row_shift) + (i & ((1 << row_shift) - 1))) * 16;
+    const auto new_word = [&](int x, int t, int i) {
+        return rows[x] + (((size_t)t << row_shift) + (i & ((1 << row_shift) - 1))) * 16;
     };
-    const float old_scale = scales[j];
-    uint32_t top = 0;
-    float old_top = 0.f;
-    constexpr int kTrip = 4;  // words a lane requests before it looks at the first
-    for (int i0 = lane; i0 < words; i0 += kWave * kTrip) {
-        uint4 c[kTrip];
+    bool plain = true;  // this thread's new words are finite
+    constexpr int kTrip = NT == kWave ? 4 : 2;  // words of each array that a thread requests before it looks at the first
+#pragma unroll 1
+    for (int i0 = me; i0 < words; i0 += NT * kTrip) {
+        uint4 c[2][kTrip];
 #pragma unroll
-        for (int u = 0; u < kTrip; ++u) c[u] = base[min(i0 + u * kWave, words - 1)];
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int u = 0; u < kTrip; ++u) c[x][u] = base[x][min(i0 + u * NT, words - 1)];
 #pragma unroll
         for (int u = 0; u < kTrip; ++u) {
-            const int i = i0 + u * kWave;
+            const int i = i0 + u * NT;
             if (i >= words) continue;
             const int t = row_of(i);
             if (t < T_new) {
-                Raw16<T> r;
-                r.load(new_word(t, i));
-                top = max(top, r.finite_top());
+                Raw16<T> r[2];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) r[x].load(new_word(x, t, i));
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    uint32_t m = r[x].top();
+                    if (m >= kInfBits) {
+                        m = r[x].finite_top();
+                        plain = false;
+                    }
+                    top[x] = max(top[x], m);
+                }
             } else {
-                old_top = fmaxf(old_top, codes_top<F>(c[u]));
+#pragma unroll
+                for (int x = 0; x < 2; ++x) old_top[x] = fmaxf(old_top[x], F::top16(c[x][u]));
             }
         }
     }
-    const int e = scale_exp<F>(wave_umax(max(top, old_mag(old_top, old_scale))));
-    const float scale = exp_scale(e), inv = exp_inverse(e);
-    const bool same = scale == old_scale;
-    for (int i = lane; i < words; i += kWave) {
-        const int t = row_of(i);
-        if (t < T_new) {
-            Raw16<T> r;
-            float x[16];
-            r.load(new_word(t, i));
-            r.widen(x);
-            base[i] = pack16<F>(x, inv, false);
-        } else if (!same) {
-            base[i] = repack16<F>(base[i], old_scale, inv);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) top[x] = wave_umax(max(top[x], old_mag(old_top[x], old_scale[x])));
+    if constexpr (NT > kWave) {
+        if ((me & 63) == 0) {
+            s_top[0][me >> 6] = top[0];
+            s_top[1][me >> 6] = top[1];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < NT / 64; ++w) {
+            top[0] = max(top[0], s_top[0][w]);
+            top[1] = max(top[1], s_top[1][w]);
         }
     }
-    if (lane == 0 && !same) scales[j] = scale;
+    float scale[2], inv[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const int e = scale_exp<F>(top[x]);
+        scale[x] = exp_scale(e);
+        inv[x] = exp_inverse(e);
+    }
+    // Old rows are passed by where no scale moved (where one did, codes of the
+    // other array come out as they were).
+    const bool same = scale[0] == old_scale[0] && scale[1] == old_scale[1];
+#pragma unroll 1
+    for (int i = me; i < words; i += NT) {
+        const int t = row_of(i);
+        if (t < T_new) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                Raw16<T> r;
+                float v[16];
+                r.load(new_word(x, t, i));
+                r.widen(v);
+                base[x][i] = plain ? pack16<F>(v, inv[x], true) : pack16<F>(v, inv[x], false);
+            }
+        } else if (!same) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) base[x][i] = repack16<F>(base[x][i], old_scale[x], inv[x]);
+        }
+    }
+    if (me == 0) {
+        scales[0][j] = scale[0];
+        scales[1][j] = scale[1];
+    }
 }
 
 }  // namespace cmc

@@ -172,24 +172,87 @@ DecodePlan plan_decode(int B, int Hq, int Hkv, int Dh, int k, int W, int T_new) 
     return pl;
 }
 
-// Split plan of the decode over the 8-bit cache, in units of kUnit8 rows.  Four
-// 4-wave workgroups are resident per CU (two for heads of 256), so `slots` =
-// 1024 (512) of them fill the 256 CUs in one round.
-DecodePlan plan_decode8(int B, int Hq, int Hkv, int Dh, int k, int W, int T_new) {
-    constexpr long long kWaves = 4, kMaxSplits = 127;
+// Split plan of the decode over the 8-bit cache, in units of kUnit8 rows; times in
+// us of a launch that appends a row, G = 4, Dh = 128 unless said otherwise.
+// Two 4-wave workgroups or one of 8 waves are resident per CU, so 512 (256) fill
+// the chip.
+//   - Up to 64 (sequence, kv head) pairs: 256 workgroups at most, one of each
+//     pair's for the block that is appended to, and no more splits than about
+//     the root of the units, since the last split to arrive reads all of their
+//     partials.  8 pairs, 6144 keys in 8 / 12 / 24 splits and one: 12.5 / 11.6 /
+//     12.3; 24576 keys in 16 / 24: 18.4 / 16.6; 64 pairs, 1536 keys in 2 / 3 / 5:
+//     12.9 / 12.2 / 13.7.  On long lists of more than 32 pairs the appended
+//     block's workgroups are missed elsewhere: 64 pairs, 24576 keys, 3 and one
+//     71.3, 4 of 8 waves 68.6.
+//   - Up to 128 pairs: 512 workgroups in the same way (128 pairs, 1536 keys: 3 and
+//     one 16.2, 2 of 8 waves 18.0, one 18.1); on lists from 4096 keys without one
+//     for the append, and of 8 waves where that is as many waves (128 pairs, 6144
+//     keys: 3 and one 41.8, 4 42.4, 2 of 8 waves 38.8; 96 pairs: 4 and one 34.0,
+//     5 31.9, 2 of 8 waves 33.5).  Where nothing is appended short lists stay
+//     whole: 128 pairs, 400 keys in 1 / 2: 8.4 / 9.2, 1536 keys 14.3 / 13.4.
+//   - Up to 170 pairs: 2 and one, or 3 on long lists (160 pairs, 768 keys: 1 / 2 and
+//     one 14.8 / 14.3; 6144 keys: 1 of 8 waves 52.4, 2 and one 53.0, 3 48.7).
+//   - Up to 256 pairs: one workgroup per pair, of 8 waves where each has work for
+//     some turns (256 pairs, 768 keys: 4 / 8 waves 15.8 / 16.4; 1536 keys 24.2 /
+//     22.4; Dh = 64, 400 keys 11.4 / 10.7).
+//   - More: one workgroup of 4 waves per pair, but two up to 384 pairs of long
+//     lists, whose second round would be half empty (384 pairs, 1536 keys: 35.0
+//     / 34.6; 6144 keys: 114 / 99.6; 512 pairs: 128 / 130).
+//   - Eight heads of 256 spend more on partials: above 64 pairs they take short
+//     lists whole (128 pairs, 400 keys: 1 / 2 and one 16.9 / 18.7; 1536 keys: 1 / 3
+//     and one 34.3 / 28.7).
+DecodePlan plan_decode8(int B, int Hq, int Hkv, int Dh, int k, int W, bool append) {
+    constexpr long long kMaxSplits = 127;
     DecodePlan pl;
     const long long pairs = (long long)B * Hkv;
     const long long units = ((long long)k + kUnit8 - 1) / kUnit8 + ((long long)W + kUnit8 - 1) / kUnit8;
     if (units <= 0 || pairs <= 0) return pl;
     const int G = Hq / Hkv;
-    const long long slots = Dh > 128 ? 512 : 1024;
-    const long long target = std::min(std::max(1LL, slots / pairs), kMaxSplits);
-    long long chunk = (units + target - 1) / target;
-    chunk = (chunk + kWaves - 1) / kWaves * kWaves;
-    pl.S = (int)((units + chunk - 1) / chunk);
+    const bool heavy = G * Dh > 1024;
+    append = append && W > 0;
+    long long S = 1;
+    bool own = false;
+    if (pairs <= 64) {
+        if (pairs > 32 && units >= 512) {
+            S = 256 / pairs;
+            pl.waves = 8;
+        } else {
+            own = append;
+            S = std::min(256 / pairs - (append ? 1 : 0), (long long)ceil(0.875 * sqrt((double)units)));
+        }
+    } else if (pairs <= 128) {
+        if (units >= 128) {
+            S = 512 / pairs;
+            if (S == 2 * (256 / pairs)) {
+                S /= 2;
+                pl.waves = 8;
+            }
+        } else if (append) {
+            own = units >= 24 || !heavy;
+            S = own ? 512 / pairs - 1 : 1;
+        } else {
+            S = units >= 32 ? 256 / pairs : 1;
+        }
+    } else if (pairs <= 170) {
+        if (units >= (append && !heavy ? 64 : 48)) {
+            S = 3;
+        } else if (append && !heavy) {
+            S = 2;
+            own = true;
+        }
+    } else if (pairs <= 256) {
+        if (units >= (Dh == 64 ? 12 : 32)) pl.waves = 8;
+    } else if (pairs <= 384) {
+        if (units >= 96) S = 2;
+    }
+    S = std::min(std::max(S, 1LL), kMaxSplits);
+    long long chunk = (units + S - 1) / S;
+    chunk = (chunk + pl.waves - 1) / pl.waves * pl.waves;
+    S = (units + chunk - 1) / chunk;
+    pl.S = (int)S;
     pl.chunk = (int)chunk;
-    pl.own_append = pl.S > 1 && T_new > 0 && W > 0;
-    const long long parts = pl.S > 1 ? pl.S + 1 : 1;
+    pl.own_append = own && S > 1;
+    const long long parts = S + (pl.own_append ? 1 : 0);
     pl.counter_bytes = align256((size_t)(B + pairs) * sizeof(unsigned));
     pl.ml_bytes = parts > 1 ? align256((size_t)(pairs * parts * G * 2) * sizeof(float)) : 0;
     pl.acc_bytes = parts > 1 ? align256((size_t)(pairs * parts * G * Dh) * sizeof(float)) : 0;
@@ -737,8 +800,6 @@ cmc_status decode8_impl(const char *fn, const float *q, const void *cme_k, const
     if (T_new < 0 || (W > 0 && T_new > W))
         return fail(CMC_ERR_INVALID_ARGUMENT, "%s: need 0 <= T_new <= W (got T_new=%d W=%d)", fn, T_new, W);
     if (W == 0) T_new = 0;  // no Tier-2: appending is a no-op
-    if (T_new > cmc::kMaxAppendRows)
-        return fail(CMC_ERR_UNSUPPORTED, "%s: T_new=%d exceeds %d rows per call", fn, T_new, cmc::kMaxAppendRows);
     if (T_new > 0) {
         if (cmc_status st = check_float(fn, new_dtype)) return st;
     }
@@ -753,11 +814,18 @@ cmc_status decode8_impl(const char *fn, const float *q, const void *cme_k, const
         misaligned(k_len) || misaligned(win_k) || misaligned(win_v) || misaligned(win_ks) || misaligned(win_vs) ||
         misaligned(win_count) || misaligned(out) || misaligned(workspace) || misaligned(new_k) || misaligned(new_v))
         return fail(CMC_ERR_UNSUPPORTED, "%s: every pointer must be 16-byte aligned", fn);
-    const cmc::DecodePlan pl = cmc::plan_decode8(B, Hq, Hkv, Dh, k, W, T_new);
+    const bool fused = T_new > 0 && T_new <= cmc::kFusedRows8;
+    const cmc::DecodePlan pl = cmc::plan_decode8(B, Hq, Hkv, Dh, k, W, fused);
     const size_t need = cmc_decode_q8_workspace_bytes(B, Hq, Hkv, Dh, k, W);
     if (!workspace || workspace_bytes < need)
         return fail(CMC_ERR_WORKSPACE_TOO_SMALL, "%s: workspace of %zu bytes needed, %zu given", fn, need,
                     workspace ? workspace_bytes : (size_t)0);
+    if (T_new > 0 && !fused) {
+        if (cmc_status st = cmc_window_append_q8(win_k, win_v, win_ks, win_vs, code, block, win_count, new_k, new_v,
+                                                 new_dtype, B, Hkv, W, Dh, T_new, stream))
+            return st;
+        T_new = 0;
+    }
     cmc::Decode8Params p{};
     char *const counters = static_cast<char *>(workspace);
     char *const partials = counters + pl.counter_bytes;
@@ -897,7 +965,8 @@ cmc_status cmc_cache_read_q8(const void *k8, const void *v8, const float *ks, co
 
 size_t cmc_decode_q8_workspace_bytes(int B, int Hq, int Hkv, int Dh, int k, int W) {
     if (B < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || k < 0 || W < 0 || !supported_dh(Dh)) return 0;
-    return std::max(cmc::plan_decode8(B, Hq, Hkv, Dh, k, W, 0).total, cmc::plan_decode8(B, Hq, Hkv, Dh, k, W, 1).total);
+    return std::max(cmc::plan_decode8(B, Hq, Hkv, Dh, k, W, false).total,
+                    cmc::plan_decode8(B, Hq, Hkv, Dh, k, W, true).total);
 }
 
 cmc_status cmc_two_tier_decode_q8(const float *q, const void *cme_k, const void *cme_v, const float *cme_ks,

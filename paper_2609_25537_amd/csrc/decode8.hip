@@ -30,10 +30,12 @@
 // lanes.  The next unit's K is requested when this unit's scores are done,
 // its V when this unit's P V is.
 //
-// Fused append: the last split (its own where the list is split) brings the
-// ring blocks that the appended rows touch up to date (append_block), then
-// attends over them; every other split leaves those blocks out.  Publication,
-// merge and the count's advance are decode.hip's.
+// Fused append: the last split (one of its own where the plan says so) brings
+// the ring blocks that the appended rows touch up to date (append_block), then
+// attends over them; every other split leaves them out.  Publication, merge and
+// the count's advance are decode.hip's.
+#include <stddef.h>
+
 #include "cache8.hpp"
 #include "decode_common.hpp"
 
@@ -44,13 +46,28 @@ namespace {
 constexpr int kWeightExp = 13;   // p is held times 2^13
 constexpr float kMaxSlack = 2.f; // how far a score may pass the running maximum
 
+// Keeps loads after this point from being issued before it, and arithmetic on
+// the registers they go to from being moved behind it.
+__device__ __forceinline__ void in_order() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+template <int DH>
+constexpr int kSets8 = DH == 256 ? 1 : 2;
+
 template <int NW, class F, int DH, int G>
 struct Walk8 {
     static constexpr int SL = DH / 64;  // 16-byte words of a K row per lane; words of a V row per lane
     static constexpr int D = DH / 16;   // output dims per lane
-    uint4 kr[2][SL];
-    uint32_t vr[8][SL];
-    float ks, vs;
+    static constexpr int NS = kSets8<DH>;
+    // Units on their way or being worked on, each in registers of its own.
+    struct Unit {
+        uint4 k[2][SL];
+        uint32_t v[8][SL];
+        float ks, vs;
+    } un[NS];
+    float4 qx[4 * SL];        // q as loaded
     halfx8 q[2 * SL];
     float qf;                 // scale log2(e) over q's power of two
     float m;                  // of head (lane % 16) % G
@@ -67,50 +84,54 @@ struct Walk8 {
         for (int j = 0; j < D; ++j) acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // Rows past `last` are read as row `last`.
-    __device__ __forceinline__ void load_k(const char *k, const float *scale, int last) {
-        ks = *scale;
+    // Rows past `last` (a list's last unit) are read as row `last`: loads without
+    // branches keep the compiler's wait counts exact.
+    __device__ __forceinline__ void load_k(int set, const char *k, int last) {
+        Unit &n = un[set];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const uint32_t o = (uint32_t)min(16 * t + r16, last) * DH + 16u * q4;
 #pragma unroll
-            for (int i = 0; i < SL; ++i) kr[t][i] = *reinterpret_cast<const uint4 *>(k + o + 64 * i);
+            for (int i = 0; i < SL; ++i) n.k[t][i] = *reinterpret_cast<const uint4 *>(k + o + 64 * i);
         }
     }
-    __device__ __forceinline__ void load_v(const char *v, const float *scale, int last) {
-        vs = *scale;
+    __device__ __forceinline__ void load_v(int set, const char *v, int last) {
+        Unit &n = un[set];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const uint32_t o = (uint32_t)min((j >> 2) * 16 + 4 * q4 + (j & 3), last) * DH + (uint32_t)D * r16;
             if constexpr (SL == 1) {
-                vr[j][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(v + o));
+                n.v[j][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(v + o));
             } else if constexpr (SL == 2) {
                 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
                 const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(v + o));
-                vr[j][0] = x[0];
-                vr[j][1] = x[1];
+                n.v[j][0] = x[0];
+                n.v[j][1] = x[1];
             } else {
                 const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(v + o));
 #pragma unroll
-                for (int i = 0; i < 4; ++i) vr[j][i] = x[i];
+                for (int i = 0; i < 4; ++i) n.v[j][i] = x[i];
             }
         }
     }
 
-    __device__ __forceinline__ void load_q(const DecodeParams &p, int b, int kvh) {
+    // The lane's quarter of its head's q.
+    __device__ __forceinline__ void request_q(const DecodeParams &p, int b, int kvh) {
         const float *qp = p.q + ((size_t)b * p.Hq + (size_t)kvh * G + (r16 % G)) * DH + 16 * q4;
+#pragma unroll
+        for (int i = 0; i < SL; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) qx[4 * i + e] = *reinterpret_cast<const float4 *>(qp + 64 * i + 4 * e);
+    }
+    __device__ __forceinline__ void split_q(const DecodeParams &p) {
         float x[16 * SL];
         uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < SL; ++i) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float4 f = *reinterpret_cast<const float4 *>(qp + 64 * i + 4 * e);
-                x[16 * i + 4 * e] = f.x;
-                x[16 * i + 4 * e + 1] = f.y;
-                x[16 * i + 4 * e + 2] = f.z;
-                x[16 * i + 4 * e + 3] = f.w;
-            }
+        for (int i = 0; i < 4 * SL; ++i) {
+            x[4 * i] = qx[i].x;
+            x[4 * i + 1] = qx[i].y;
+            x[4 * i + 2] = qx[i].z;
+            x[4 * i + 3] = qx[i].w;
         }
 #pragma unroll
         for (int e = 0; e < 16 * SL; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
@@ -122,14 +143,14 @@ struct Walk8 {
         const int up = min(127 + 14 + 127 - (int)(top >> 23), 253);
         const float mul = copysignf(__uint_as_float((uint32_t)up << 23), p.qscale);
         qf = fabsf(p.qscale) * __uint_as_float((uint32_t)(254 - up) << 23);
-        const bool lo = r16 >= 8;
+        const float part = r16 >= 8 ? 1.f : 0.f;
 #pragma unroll
         for (int i = 0; i < 2 * SL; ++i) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float y = x[8 * i + e] * mul;
                 const _Float16 h = (_Float16)y;
-                q[i][e] = lo ? (_Float16)(y - (float)h) : h;
+                q[i][e] = (_Float16)fmaf(-(float)h, part, y);  // hi: y itself; lo: what hi leaves
             }
         }
     }
@@ -142,63 +163,69 @@ struct Walk8 {
     }
 
     // Scores (in units of q's power of two and s_K) of rows 16 t + 4 q4 + i.
-    __device__ __forceinline__ void scores(floatx4 (&c)[2]) const {
+    __device__ __forceinline__ void scores(int set, floatx4 (&c)[2]) const {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             c[t] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < SL; ++i) {
-                c[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(half8(kr[t][i].x, kr[t][i].y), q[2 * i], c[t], 0, 0, 0);
-                c[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(half8(kr[t][i].z, kr[t][i].w), q[2 * i + 1], c[t], 0, 0, 0);
+                c[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(half8(un[set].k[t][i].x, un[set].k[t][i].y), q[2 * i], c[t], 0, 0, 0);
+                c[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(half8(un[set].k[t][i].z, un[set].k[t][i].w), q[2 * i + 1], c[t], 0, 0, 0);
             }
         }
     }
 
-    // The unit's share of l and acc; rows n and up are masked.
-    __device__ __forceinline__ void add(const floatx4 (&c)[2], float kscale, int n) {
-        const bool full = n >= kUnit8;  // uniform
+    // Has the sums finished here rather than behind the next loads, which would
+    // keep this unit's registers and put those loads in others, to be moved (and
+    // so waited for) at the end of a turn.
+    __device__ __forceinline__ void settle() {
+#pragma unroll
+        for (int j = 0; j < D; ++j) asm volatile("" : "+v"(acc[j]));
+        asm volatile("" : "+v"(l));
+    }
+
+    // The unit's share of l and acc; f: s_K over q's power of two.  Rows n and up are copies of row n - 1: they
+    // may count in the maximum, and weigh 0.
+    __device__ __forceinline__ void add(int set, const floatx4 (&c)[2], float f, int n) {
+        const float vs = un[set].vs;
         float x[8];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[4 * t + i] = c[t][i] + dpp_sum_operand<0x128>(c[t][i]);  // hi + lo
-        const float f = kscale * qf;
-        if (!full) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = (e >> 2) * 16 + 4 * q4 + (e & 3) < n ? x[e] : -FLT_MAX;
-        }
         const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
                                 fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))) * f;
-        if (__any(top > m + kMaxSlack)) {
+        if (__builtin_expect(__any(top > m + kMaxSlack), 0)) {
             const float mn = fmaxf(m, combine_xor32<OpMax>(combine_xor16<OpMax>(top)));
             const float alpha = fast_exp2(m - mn);  // 0 from kNoMax, where l and acc are 0
+            const bool sums = __any(m != kNoMax);  // not at a wave's first unit
             m = mn;
-            float al[4];
+            if (sums) {
+                float al[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) al[i] = __shfl(alpha, 4 * q4 + i);  // of row 4 q4 + i
+                for (int i = 0; i < 4; ++i) al[i] = __shfl(alpha, 4 * q4 + i);  // of row 4 q4 + i
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                l[i] *= al[i];
+                for (int i = 0; i < 4; ++i) {
+                    l[i] *= al[i];
 #pragma unroll
-                for (int j = 0; j < D; ++j) acc[j][i] *= al[i];
+                    for (int j = 0; j < D; ++j) acc[j][i] *= al[i];
+                }
             }
         }
         const float mp = m - (float)kWeightExp;
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = fast_exp2(fmaf(x[e], f, -mp));
+        if (__builtin_expect(n < kUnit8, 0)) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = (e >> 2) * 16 + 4 * q4 + (e & 3) < n ? w[e] : 0.f;
+        }
         const float part = r16 >= 8 ? 1.f : 0.f;
         halfx8 P;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            float w = fast_exp2(fmaf(x[e], f, -mp));
-            if (!full) w = (e >> 2) * 16 + 4 * q4 + (e & 3) < n ? w : 0.f;
-            const _Float16 h = (_Float16)w;
-            P[e] = (_Float16)fmaf(-(float)h, part, w);  // hi: w itself; lo: what hi leaves
-        }
-        if (!full && F::kHasNaN) {  // rows past the list may hold any bits, and 0 NaN is NaN
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if ((j >> 2) * 16 + 4 * q4 + (j & 3) >= n)
-#pragma unroll
-                    for (int i = 0; i < SL; ++i) vr[j][i] = 0u;
+            const _Float16 h = (_Float16)w[e];
+            P[e] = (_Float16)fmaf(-(float)h, part, w[e]);  // hi: w itself; lo: what hi leaves
         }
         constexpr _Float16 one = (_Float16)1.f;
         const halfx8 ones = {one, one, one, one, one, one, one, one};
@@ -207,7 +234,7 @@ struct Walk8 {
         for (int w = 0; w < SL; ++w) {
             uint32_t a[8][2];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) F::half4(vr[j][w], a[j][0], a[j][1]);
+            for (int j = 0; j < 8; ++j) F::half4(un[set].v[j][w], a[j][0], a[j][1]);
             floatx4 t[4];
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
@@ -227,129 +254,252 @@ struct Walk8 {
 };
 
 template <int DH>
-constexpr int kMinWaves8 = DH <= 128 ? 4 : 2;
+constexpr int kMinWaves8 = 2;
 
-// The leading arguments arrive in SGPRs at wave launch, as decode_kernel's do.
+// The kernel's parameters, loaded here and not before (the compiler would
+// load them at the kernel's start and wait for them there).
+struct Args8 {
+    const void *cme_k, *cme_v;
+    void *win_k, *win_v;
+    int k, W, N, Hkv, chunk, info;
+    Decode8Params p;
+};
+__device__ __forceinline__ Decode8Params late_params() {
+    typedef const __attribute__((address_space(4))) Args8 *Ptr;
+    Ptr at = (Ptr)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    Decode8Params p{};
+    p.q = at->p.q;
+    p.cme_ks = at->p.cme_ks;
+    p.cme_vs = at->p.cme_vs;
+    p.win_ks = at->p.win_ks;
+    p.win_vs = at->p.win_vs;
+    p.win_count = at->p.win_count;
+    p.new_k = at->p.new_k;
+    p.new_v = at->p.new_v;
+    p.new_bf16 = at->p.new_bf16;
+    p.out = at->p.out;
+    p.part_ml = at->p.part_ml;
+    p.part_acc = at->p.part_acc;
+    p.pair_counter = at->p.pair_counter;
+    p.seq_counter = at->p.seq_counter;
+    p.Hq = at->p.Hq;
+    p.qscale = at->p.qscale;
+    p.pool_blocks = at->p.pool_blocks;
+    p.ring_blocks = at->p.ring_blocks;
+    p.log2_block = at->p.log2_block;
+    return p;
+}
+
+// The leading arguments (Args8's, one by one) arrive in SGPRs at wave launch,
+// as decode_kernel's do.
 template <int NW, class F, int DH, int G>
 __global__ __launch_bounds__(NW * kWave, (kMinWaves8<DH>)) void decode8_kernel(const void *cme_k, const void *cme_v,
                                                                                void *win_k, void *win_v, int k, int W,
                                                                                int N, int Hkv, int chunk, int info,
                                                                                Decode8Params pm) {
-    Decode8Params p = pm;
-    p.k = k;
-    p.W = W;
-    p.N = N;
-    p.Hkv = Hkv;
-    p.S = info & 0xFF;
+    const int S = info & 0xFF;
     const bool own = (info >> 8) & 1;
-    const bool has_klen = (info >> 10) & 1;
-    p.T_new = (int)((unsigned)info >> 16);
     const int s = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int kb = k;
-    if (has_klen) {
-        const int v = p.k_len[b];
+    if ((info >> 10) & 1) {  // k_len is given
+        const int v = pm.k_len[b];
         kb = v < 0 ? 0 : (v > k ? k : v);
     }
     // Units: the pool's, then the ring's in physical slot order.
     const int pool_units = (kb + kUnit8 - 1) / kUnit8;
     const int units = pool_units + (int)(((unsigned)W + kUnit8 - 1) / kUnit8);
     int u = s * chunk, end = min(u + chunk, units);
-    if (s >= p.S - 1 - (own ? 1 : 0)) end = units;
-    if (own && s == p.S - 1) u = units;
+    if (s >= S - 1 - (own ? 1 : 0)) end = units;
+    if (own && s == S - 1) u = units;
 
     const size_t head = (size_t)b * Hkv + kvh;
     const char *pk = static_cast<const char *>(cme_k) + head * (size_t)N * DH;
     const char *pv = static_cast<const char *>(cme_v) + head * (size_t)N * DH;
     const char *rk = static_cast<const char *>(win_k) + head * (size_t)W * DH;
     const char *rv = static_cast<const char *>(win_v) + head * (size_t)W * DH;
+    // A unit's place: its first row's codes, its number in its own array, and
+    // its live rows.
+    struct Place {
+        const char *k, *v;
+        int r, n;
+        bool pool;
+    };
+    const auto place = [&](int u, int ring_rows) {
+        const bool pool = u < pool_units;
+        const int r = pool ? u : u - pool_units;
+        const size_t o = (size_t)r * (kUnit8 * DH);
+        return Place{(pool ? pk : rk) + o, (pool ? pv : rv) + o, r, min(kUnit8, (pool ? kb : ring_rows) - r * kUnit8), pool};
+    };
+    // The first unit is requested from the leading arguments alone, with all of
+    // the ring's slots as live: nothing waits for the others, nor for the count.
+    Walk8<NW, F, DH, G> st;
+    st.init();
+    u += wave;
+    const int u0 = u;
+    const bool some = u < end;
+    Place at{pk, pv, 0, 1, true};
+    if (some) {
+        at = place(u, W);
+        st.load_k(0, at.k, at.n - 1);
+        st.load_v(0, at.v, at.n - 1);
+    }
+    in_order();
+    Decode8Params p = late_params();
+    p.k = k;
+    p.W = W;
+    p.N = N;
+    p.Hkv = Hkv;
+    p.S = S;
+    p.T_new = (int)((unsigned)info >> 16);
     const float *pks = p.cme_ks + head * p.pool_blocks, *pvs = p.cme_vs + head * p.pool_blocks;
     float *rks = p.win_ks + head * p.ring_blocks, *rvs = p.win_vs + head * p.ring_blocks;
     const int unit_shift = p.log2_block - 5;  // units per block
+    const auto scale_k = [&](const Place &at) { return (at.pool ? pks : rks)[at.r >> unit_shift]; };
+    const auto scale_v = [&](const Place &at) { return (at.pool ? pvs : rvs)[at.r >> unit_shift]; };
 
     RingCount cnt{0, false};
-    Walk8<NW, F, DH, G> st;
-    st.init();
     int filled = 0;  // ring slots that hold a key of this step
     TouchedBlocks tb{0, 0, 1};
     bool ready = false;
-    const auto after_first_load = [&]() {
-        if (ready) return;
+    // q split, and what follows from the count, once both have been requested.
+    const auto start = [&]() {
         ready = true;
-        cnt.load(W > 0 ? p.win_count : nullptr, b);
-        st.load_q(p, b, kvh);
+        st.split_q(p);
         const int c = cnt.value();
         filled = (int)min((long long)c + p.T_new, (long long)W);
         if (p.T_new > 0 && W > 0) tb.set(c % W, p.T_new, W, p.log2_block);
         end = min(end, pool_units + (filled + kUnit8 - 1) / kUnit8);
     };
-    // Rows of unit u that take part (0: none), and its addresses.
-    const auto rows_of = [&](int u) {
-        if (u < pool_units) return kb - u * kUnit8;
-        const int r = u - pool_units;
-        return tb.has(r >> unit_shift) && tb.count > 0 ? 0 : filled - r * kUnit8;
-    };
-    const auto load_k = [&](int u) {
-        const bool pool = u < pool_units;
-        const int r = pool ? u : u - pool_units;
-        st.load_k((pool ? pk : rk) + (size_t)r * (kUnit8 * DH), (pool ? pks : rks) + (r >> unit_shift),
-                  min(kUnit8, (pool ? kb : W) - r * kUnit8) - 1);
-    };
-    const auto load_v = [&](int u) {
-        const bool pool = u < pool_units;
-        const int r = pool ? u : u - pool_units;
-        st.load_v((pool ? pv : rv) + (size_t)r * (kUnit8 * DH), (pool ? pvs : rvs) + (r >> unit_shift),
-                  min(kUnit8, (pool ? kb : W) - r * kUnit8) - 1);
+    const auto touched = [&](int u) { return u >= pool_units && tb.count > 0 && tb.has((u - pool_units) >> unit_shift); };
+    const auto after = [&](int u) {  // this wave's next unit, passing by the blocks that are being appended to
+        do u += NW;
+        while (touched(u) && u < end);
+        return u;
     };
 
-    u += wave;
-    if (u < end) {
-        load_k(u);
-        load_v(u);
-        after_first_load();
+    // The units in turn through NS register sets.  In the loop each set's next
+    // unit is requested as soon as its registers are free, always: branches
+    // around loads would have the waits count for the path without them.  Where
+    // there is none left, the last unit is requested again, of which no row
+    // counts.  The last NS units are worked off after the loop.
+    constexpr int NS = kSets8<DH>;
+    if (some) {
+        int n[NS];
+        st.un[0].ks = scale_k(at);
+        st.un[0].vs = scale_v(at);
+        in_order();  // before q, whose wait so covers the scales' too
+        st.request_q(p, b, kvh);
+        cnt.load(W > 0 ? p.win_count : nullptr, b);
+        n[0] = at.n;
+#pragma unroll
+        for (int i = 1; i < NS; ++i) {
+            n[i] = 0;
+            if (u + NW < end) {
+                u += NW;
+                at = place(u, W);
+                in_order();
+                st.load_k(i, at.k, at.n - 1);
+                st.un[i].ks = scale_k(at);
+                in_order();
+                st.load_v(i, at.v, at.n - 1);
+                st.un[i].vs = scale_v(at);
+                n[i] = at.n;
+            }
+        }
+        start();
+        // A unit among them that is being appended to or not filled: once more
+        // from the first, as it should have been.
+        bool again = false;
+        for (int i = 0, v = u0; i < NS; ++i, v += NW)
+            again |= v >= pool_units && n[i] > 0 && (touched(v) || v >= end || place(v, filled).n != n[i]);
+        if (__builtin_expect(again, 0)) {
+            u = u0;
+            if (touched(u)) u = after(u);
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                if (i > 0 && u < end) u = after(u);
+                if (u < end) at = place(u, filled);
+                st.load_k(i, at.k, at.n - 1);
+                st.un[i].ks = scale_k(at);
+                st.load_v(i, at.v, at.n - 1);
+                st.un[i].vs = scale_v(at);
+                n[i] = u < end ? at.n : 0;
+            }
+            __builtin_amdgcn_s_waitcnt(0);  // so that the loop's waits need not allow for this path
+        }
+        u = u < end ? after(u) : u;
 #pragma unroll 1
         while (u < end) {
-            const int n = rows_of(u), nu = u + NW;
-            const float kscale = st.ks;
-            floatx4 c[2];
-            st.scores(c);
-            __builtin_amdgcn_sched_barrier(0);
-            if (nu < end) load_k(nu);
-            __builtin_amdgcn_sched_barrier(0);
-            if (n > 0) st.add(c, kscale, n);
-            __builtin_amdgcn_sched_barrier(0);
-            if (nu < end) load_v(nu);
-            u = nu;
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                floatx4 c[2];
+                float f = st.un[i].ks * st.qf;
+                asm volatile("" : "+v"(f));  // taken here: the scale's register is the next load's
+                st.scores(i, c);
+                const bool more = u < end;
+                if (more) at = place(u, filled);
+                in_order();
+                st.load_k(i, at.k, at.n - 1);
+                st.un[i].ks = scale_k(at);
+                in_order();
+                st.add(i, c, f, n[i]);
+                st.settle();
+                in_order();
+                st.load_v(i, at.v, at.n - 1);
+                st.un[i].vs = scale_v(at);
+                n[i] = more ? at.n : 0;
+                u = more ? after(u) : u;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            if (n[i] > 0) {
+                floatx4 c[2];
+                st.scores(i, c);
+                st.add(i, c, st.un[i].ks * st.qf, n[i]);
+            }
         }
     }
     if (p.T_new > 0 && W > 0 && s == p.S - 1) {  // workgroup-uniform
-        after_first_load();
-        const int slot0 = cnt.value() % W;
-        for (int w = wave; w < 2 * tb.count; w += NW) {
-            const bool is_v = w & 1;
-            uint8_t *codes = static_cast<uint8_t *>(is_v ? win_v : win_k) + head * (size_t)W * DH;
-            float *scales = is_v ? rvs : rks;
-            const char *rows = static_cast<const char *>(is_v ? p.new_v : p.new_k);
-            const size_t first = head * (size_t)p.T_new * DH;
-            constexpr int shift = DH == 64 ? 2 : DH == 128 ? 3 : 4;
-            if (p.new_bf16)
-                append_block<uint16_t, F>(reinterpret_cast<const uint16_t *>(rows) + first, codes, scales,
-                                          tb.block(w >> 1), p.log2_block, shift, W, slot0, filled, p.T_new);
-            else
-                append_block<float, F>(reinterpret_cast<const float *>(rows) + first, codes, scales, tb.block(w >> 1),
-                                       p.log2_block, shift, W, slot0, filled, p.T_new);
+        if (!ready) {
+            st.request_q(p, b, kvh);
+            cnt.load(p.win_count, b);
+            start();
         }
-        __syncthreads();  // the blocks are in memory, for this workgroup's loads too
+        const int slot0 = cnt.value() % W;
+        const size_t src = head * (size_t)p.T_new * DH, dst = head * (size_t)W * DH;
+        constexpr int shift = DH == 64 ? 2 : DH == 128 ? 3 : 4;
+        uint8_t *const codes[2] = {static_cast<uint8_t *>(win_k) + dst, static_cast<uint8_t *>(win_v) + dst};
+        float *const scales[2] = {rks, rvs};
+        __shared__ uint32_t s_top[2][NW];
+#pragma unroll 1
+        for (int i = 0; i < tb.count; ++i) {
+            if (p.new_bf16)
+                append_block<uint16_t, F, NW * kWave>({static_cast<const uint16_t *>(p.new_k) + src,
+                                                       static_cast<const uint16_t *>(p.new_v) + src},
+                                                      codes, scales, tb.block(i), p.log2_block, shift, W, slot0, filled,
+                                                      p.T_new, s_top);
+            else
+                append_block<float, F, NW * kWave>({static_cast<const float *>(p.new_k) + src,
+                                                    static_cast<const float *>(p.new_v) + src},
+                                                   codes, scales, tb.block(i), p.log2_block, shift, W, slot0, filled,
+                                                   p.T_new, s_top);
+            __syncthreads();  // the block is in memory, for this workgroup's loads too
+        }
         const int per = 1 << unit_shift;
         for (int i = wave; i < tb.count * per; i += NW) {
             const int r = tb.block(i >> unit_shift) * per + (i & (per - 1));
-            const int n = filled - r * kUnit8;
-            if (n <= 0) continue;
-            load_k(pool_units + r);
-            load_v(pool_units + r);
+            if (r * kUnit8 >= filled) continue;
+            at = place(pool_units + r, filled);
+            st.load_k(0, at.k, at.n - 1);
+            st.load_v(0, at.v, at.n - 1);
+            st.un[0].ks = scale_k(at);
+            st.un[0].vs = scale_v(at);
             floatx4 c[2];
-            st.scores(c);
-            st.add(c, st.ks, n);
+            st.scores(0, c);
+            st.add(0, c, st.un[0].ks * st.qf, at.n);
         }
     }
     cnt.load(W > 0 ? p.win_count : nullptr, b);  // a wave without rows
@@ -378,16 +528,20 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves8<DH>)) void decode8_kernel(c
     if (st.lane < G) s_m[wave][st.lane] = st.m;
     if (st.lane == 0) s_cnt[wave] = cnt.raw;  // stored once the wave's count read has returned
     __syncthreads();
-    finish_pair<NW, DH, G, true>(p, b, kvh, s, s_m, s_l, s_acc, s_cnt, cnt_now);
+    finish_pair<NW, DH, G, true, true>(p, b, kvh, s, s_m, s_l, s_acc, s_cnt, cnt_now);
 }
 
 template <class F, int DH, int G>
 hipError_t launch3(const Decode8Params &p, hipStream_t stream) {
     const dim3 grid(p.S, p.Hkv, p.B);
-    if (p.S < 1 || p.S > 0xFF || p.T_new < 0 || p.T_new > kMaxAppendRows || p.waves != 4) return hipErrorInvalidValue;
+    if (p.S < 1 || p.S > 0xFF || p.T_new < 0 || p.T_new > kFusedRows8 || (p.waves != 4 && p.waves != 8)) return hipErrorInvalidValue;
     const int info = p.S | (p.new_split << 8) | ((p.k_len != nullptr) << 10) | (p.T_new << 16);
-    decode8_kernel<4, F, DH, G><<<grid, 4 * kWave, 0, stream>>>(p.cme_k, p.cme_v, p.win_k, p.win_v, p.k, p.W, p.N, p.Hkv,
-                                                                p.chunk, info, p);
+#define CMC_LAUNCH(NW_)                                                                                          \
+    decode8_kernel<NW_, F, DH, G><<<grid, NW_ * kWave, 0, stream>>>(p.cme_k, p.cme_v, p.win_k, p.win_v, p.k, p.W, \
+                                                                    p.N, p.Hkv, p.chunk, info, p)
+    if (p.waves == 4) CMC_LAUNCH(4);
+    else CMC_LAUNCH(8);
+#undef CMC_LAUNCH
     return hipGetLastError();
 }
 

@@ -118,7 +118,10 @@ struct Decode8Params : DecodeParams {
 };
 // Rows a wave takes at a time; chunk and the plan count in these.
 constexpr int kUnit8 = 32;
-DecodePlan plan_decode8(int B, int Hq, int Hkv, int Dh, int k, int W, int T_new);
+DecodePlan plan_decode8(int B, int Hq, int Hkv, int Dh, int k, int W, bool append);
+// Most appended rows that the decode kernel takes along (their blocks are written
+// by one workgroup); more are appended by launches of their own.
+constexpr int kFusedRows8 = 16;
 hipError_t launch_decode8(const Decode8Params &p, bool e4m3, int G, int Dh, hipStream_t stream);
 
 // Most appended rows that one workgroup per sequence takes (see
