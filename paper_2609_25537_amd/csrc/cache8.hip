@@ -1,13 +1,12 @@
 // Writing the 8-bit cache and reading it back (the format: cache8.hpp).
 //
-// The Tier-1 gather and a prefill's ring append take one workgroup per block
-// of rows, for K and V together: half of its threads hold the block's K in
-// registers, half its V, so every row is read once; the block's largest
-// magnitude is reduced over the half, and the codes go out as 16-byte stores.
-// A decode step's append (a few rows) takes one workgroup per sequence, a wave
-// per (kv head, block), and advances the count itself.  All of it is
+// The Tier-1 gather and the ring append take one workgroup per block of rows,
+// for K and V together: half of its threads hold the block's K in registers,
+// half its V, so every row is read once; the block's largest magnitude is
+// reduced over the half, and the codes go out as 16-byte stores.  All of it is
 // bound by memory, the small calls by latency.
 #include <algorithm>
+#include <type_traits>
 
 #include "cache8.hpp"
 #include "kernels.hpp"
@@ -116,102 +115,84 @@ __global__ __launch_bounds__(1024) void write_blocks_kernel(Write8Params p) {
     }
 }
 
-// A few rows appended: one workgroup per sequence.
-template <typename T, class F>
-__global__ __launch_bounds__(1024) void append_rows_kernel(Write8Params p) {
-    const int b = blockIdx.x;
-    const int count = max(p.count[b], 0);
-    const int slot0 = count % p.R;
-    const int filled = (int)min((long long)count + p.T_new, (long long)p.R);
-    TouchedBlocks tb;
-    tb.set(slot0, p.T_new, p.R, p.log2_block);
-    const int items = p.Hkv * tb.count;  // small: see launch_append
-    for (int w = threadIdx.x >> 6; w < items; w += (int)(blockDim.x >> 6)) {
-        const size_t head = (size_t)b * p.Hkv + w % p.Hkv;
-        const size_t src = ((head * p.T_new) << p.row_shift) * 16, dst = ((head * p.R) << p.row_shift) * 16;
-        append_block<T, F, kWave>({static_cast<const T *>(p.src_k) + src, static_cast<const T *>(p.src_v) + src},
-                              {static_cast<uint8_t *>(p.k) + dst, static_cast<uint8_t *>(p.v) + dst},
-                              {p.ks + head * p.blocks, p.vs + head * p.blocks}, tb.block(w / p.Hkv), p.log2_block,
-                              p.row_shift, p.R, slot0, filled, p.T_new, nullptr);
+// Sixteen bytes of values of 8 (bf16) or 4 codes.
+template <typename T, class F, typename Codes>
+__device__ __forceinline__ uint4 values16(const Codes &c, float scale) {
+    uint32_t w[4];
+    if constexpr (sizeof(T) == 2) {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            float f[4];
+            F::widen4(q ? c.y : c.x, f);
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                w[2 * q + e] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)(f[2 * e] * scale), (__bf16)(f[2 * e + 1] * scale)});
+        }
+    } else {
+        float f[4];
+        F::widen4(c, f);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(f[e] * scale);
     }
-    __syncthreads();
-    if (threadIdx.x == 0) p.count[b] = count + p.T_new;
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // Rows r < min(count, R) of the cache in the order they were written, oldest
 // first: row (first + r) mod R, first = count mod R where the ring has
-// wrapped.  A thread widens sixteen codes of K and sixteen of V.
-template <typename T>
-__device__ __forceinline__ void put16(T *p, const float (&x)[16]) {
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            st16_nt(reinterpret_cast<uint4 *>(p) + i,
-                    make_uint4(__float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]),
-                               __float_as_uint(x[4 * i + 3])));
-    } else {
-        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-        uint32_t w[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x[2 * i], (__bf16)x[2 * i + 1]});
-        st16_nt(reinterpret_cast<uint4 *>(p), make_uint4(w[0], w[1], w[2], w[3]));
-        st16_nt(reinterpret_cast<uint4 *>(p) + 1, make_uint4(w[4], w[5], w[6], w[7]));
-    }
-}
-
+// wrapped.  A thread makes 16 bytes of K and of V from 8 (bf16) or 4 codes, so
+// that every load and store of a wave takes a whole run.  Bound by memory: 64
+// sequences x 8 heads x 1000 rows of 128 to bf16 (393 MB) 64.6 us, 6.1 TB/s;
+// with 16 codes a thread, whose stores leave gaps for the next one, 96.4 us (to
+// fp32 446 against 85).
 template <typename T, class F>
 __global__ __launch_bounds__(256) void read_kernel(Read8Params p) {
+    constexpr int E = Vec16<T>::N;  // codes a thread takes
+    typedef std::conditional_t<E == 8, uint2, uint32_t> Codes;
     const int h = blockIdx.y, b = blockIdx.z;
     const size_t head = (size_t)b * p.Hkv + h;
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    const int shift = p.row_shift + (E == 8 ? 1 : 2);  // log2 of the threads to a row
     const int count = p.count ? p.count[b] : p.R;
-    const long long r = i >> p.row_shift;
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    const long long r = i >> shift;
     if (r >= min(count, p.R)) return;
     long long row = r + (count > p.R ? count % p.R : 0);
     row -= row >= p.R ? p.R : 0;
-    const size_t from = ((head * p.R + row) << p.row_shift) + (i & ((1 << p.row_shift) - 1));
-    const size_t to = (((head * p.R + r) << p.row_shift) + (i & ((1 << p.row_shift) - 1))) * 16;
+    const size_t from = ((head * p.R + row) << shift) + (i & ((1 << shift) - 1));
+    const size_t to = ((head * p.R) << shift) + i;
     const size_t at = head * p.blocks + (row >> p.log2_block);
-    const uint4 ck = static_cast<const uint4 *>(p.k)[from], cv = static_cast<const uint4 *>(p.v)[from];
+    const Codes k = static_cast<const Codes *>(p.k)[from], v = static_cast<const Codes *>(p.v)[from];
     const float ks = p.ks[at], vs = p.vs[at];
-    float x[16];
-    widen16<F>(ck, x);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) x[e] *= ks;
-    put16<T>(static_cast<T *>(p.out_k) + to, x);
-    widen16<F>(cv, x);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) x[e] *= vs;
-    put16<T>(static_cast<T *>(p.out_v) + to, x);
+    st16_nt(static_cast<uint4 *>(p.out_k) + to, values16<T, F>(k, ks));
+    st16_nt(static_cast<uint4 *>(p.out_v) + to, values16<T, F>(v, vs));
 }
 
 template <typename T, class F, bool RING>
 hipError_t launch_blocks(const Write8Params &p, int items, hipStream_t stream) {
     const int words = 1 << (p.log2_block + p.row_shift);  // of a whole block: 128 to 2048
-    const int half = std::min(words, 512);
+    // Two words a thread, four where the workgroup would pass 1024 threads.  One
+    // word a thread: an append of 1024 rows to 64 x 8 rings of 128 in blocks of
+    // 32 takes 80.6 us against 72.9, of one row 7.8 against 6.1, a gather of 512
+    // rows for them 39.8 against 39.1; four: 73.5, 6.8 and 41.6.
+    const int half = std::min(words / 2, 512);
     const dim3 grid(items, p.Hkv, p.B);
-    switch (words / half) {
-        case 1: write_blocks_kernel<T, F, RING, 1><<<grid, 2 * half, 0, stream>>>(p); break;
-        case 2: write_blocks_kernel<T, F, RING, 2><<<grid, 2 * half, 0, stream>>>(p); break;
-        case 4: write_blocks_kernel<T, F, RING, 4><<<grid, 2 * half, 0, stream>>>(p); break;
-        default: return hipErrorInvalidValue;
-    }
+    if (words / half == 2) write_blocks_kernel<T, F, RING, 2><<<grid, 2 * half, 0, stream>>>(p);
+    else write_blocks_kernel<T, F, RING, 4><<<grid, 2 * half, 0, stream>>>(p);
     return hipGetLastError();
 }
 
 // Ring blocks that an append of T rows can touch at most: two that it fills
-// in part and a short last block on the way.
+// in part, those between and a short last block on the way, each by a row.
 int touched_most(int T, int blocks, int log2_block) {
-    return std::min(blocks, ((T - 1) >> log2_block) + 3);
+    return std::min({T, blocks, ((T - 1) >> log2_block) + 3});
 }
 
+// Every workgroup reads the counts, so a launch of its own raises them.  (One
+// workgroup per sequence that does both at its end: 8.4 us against 6.1 for a row
+// of 64 sequences, 4.9 against 5.0 for one sequence.)
 template <typename T, class F>
 hipError_t launch_append(const Write8Params &p, hipStream_t stream) {
     const int most = touched_most(p.T_new, p.blocks, p.log2_block);
-    if (p.T_new <= kAppend8OneWg) {
-        append_rows_kernel<T, F><<<p.B, 1024, 0, stream>>>(p);
-        return hipGetLastError();
-    }
     if (hipError_t e = launch_blocks<T, F, true>(p, most, stream); e != hipSuccess) return e;
     return launch_window_count(p.count, p.B, p.T_new, stream);
 }
@@ -231,8 +212,8 @@ hipError_t launch_append8(const Write8Params &p, bool bf16, bool e4m3, hipStream
 }
 
 hipError_t launch_read8(const Read8Params &p, bool bf16, bool e4m3, hipStream_t stream) {
-    const long long words = (long long)p.R << p.row_shift;
-    const dim3 grid((unsigned)((words + 255) / 256), p.Hkv, p.B);
+    const long long threads = (long long)p.R << (p.row_shift + (bf16 ? 1 : 2));
+    const dim3 grid((unsigned)((threads + 255) / 256), p.Hkv, p.B);
     if (bf16 && e4m3) read_kernel<uint16_t, CodeE4M3><<<grid, 256, 0, stream>>>(p);
     else if (bf16) read_kernel<uint16_t, CodeI8><<<grid, 256, 0, stream>>>(p);
     else if (e4m3) read_kernel<float, CodeE4M3><<<grid, 256, 0, stream>>>(p);

@@ -216,8 +216,8 @@ __device__ __forceinline__ void widen16(const uint4 &c, float (&x)[16]) {
 }
 
 // The largest magnitude of a block's old codes as a part of its new maximum.  A
-// top of 0 (no live old row,
-// or only zeros) counts for nothing, whatever the old scale holds.
+// top of 0 (no live old row, or only zeros) counts for nothing, whatever the old
+// scale holds.
 __device__ __forceinline__ uint32_t old_mag(float codes_top, float old_scale) {
     return codes_top > 0.f ? finite_mag(codes_top * old_scale) : 0u;
 }
@@ -264,18 +264,17 @@ struct TouchedBlocks {
     }
 };
 
-// NT threads (a wave, or a workgroup of NT / 64) bring a ring block of K and V of
+// A workgroup of NT threads brings a ring block of K and V of
 // one (sequence, kv head) up to date with the rows appended at slot0: the
 // scales from the new rows and the live old ones, then the codes.  Where no
 // scale moves, only the new rows are written.  row_shift: log2 of a row's
-// 16-code words; filled: slots that are live after the append.  A workgroup
-// needs s_top[2][NT / 64] in LDS, and a barrier before anyone reads the block or
-// another block is begun.
+// 16-code words; filled: slots that are live after the append.  A barrier is
+// needed before anyone reads the block or another block is begun.
 template <typename T, class F, int NT>
 __device__ __forceinline__ void append_block(const T *const (&rows)[2], uint8_t *const (&codes)[2], float *const (&scales)[2],
                                              int j, int log2_block, int row_shift, int W, int slot0, int filled, int T_new,
                                              uint32_t (*s_top)[NT / 64]) {
-    const int me = NT == kWave ? threadIdx.x & 63 : threadIdx.x;
+    const int me = threadIdx.x;
     const int s0 = j << log2_block;
     const int words = min(1 << log2_block, filled - s0) << row_shift;
     uint4 *base[2];
@@ -295,7 +294,7 @@ __device__ __forceinline__ void append_block(const T *const (&rows)[2], uint8_t 
         return rows[x] + (((size_t)t << row_shift) + (i & ((1 << row_shift) - 1))) * 16;
     };
     bool plain = true;  // this thread's new words are finite
-    constexpr int kTrip = NT == kWave ? 4 : 2;  // words of each array that a thread requests before it looks at the first
+    constexpr int kTrip = 2;  // words of each array that a thread requests before it looks at the first
 #pragma unroll 1
     for (int i0 = me; i0 < words; i0 += NT * kTrip) {
         uint4 c[2][kTrip];
@@ -329,17 +328,15 @@ __device__ __forceinline__ void append_block(const T *const (&rows)[2], uint8_t 
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x) top[x] = wave_umax(max(top[x], old_mag(old_top[x], old_scale[x])));
-    if constexpr (NT > kWave) {
-        if ((me & 63) == 0) {
-            s_top[0][me >> 6] = top[0];
-            s_top[1][me >> 6] = top[1];
-        }
-        __syncthreads();
+    if ((me & 63) == 0) {
+        s_top[0][me >> 6] = top[0];
+        s_top[1][me >> 6] = top[1];
+    }
+    __syncthreads();
 #pragma unroll
-        for (int w = 0; w < NT / 64; ++w) {
-            top[0] = max(top[0], s_top[0][w]);
-            top[1] = max(top[1], s_top[1][w]);
-        }
+    for (int w = 0; w < NT / 64; ++w) {
+        top[0] = max(top[0], s_top[0][w]);
+        top[1] = max(top[1], s_top[1][w]);
     }
     float scale[2], inv[2];
 #pragma unroll

@@ -124,10 +124,6 @@ DecodePlan plan_decode8(int B, int Hq, int Hkv, int Dh, int k, int W, bool appen
 constexpr int kFusedRows8 = 16;
 hipError_t launch_decode8(const Decode8Params &p, bool e4m3, int G, int Dh, hipStream_t stream);
 
-// Most appended rows that one workgroup per sequence takes (see
-// launch_append in cache8.hip).
-constexpr int kAppend8OneWg = 4;
-
 struct SelectParams {
     const void *sel_keys;     // [B][N][D] fp32 or bf16 (keys_bf16)
     const float *q_vec;       // [B][D]
