@@ -115,6 +115,58 @@ __global__ __launch_bounds__(1024) void write_blocks_kernel(Write8Params p) {
     }
 }
 
+// One row appended, of up to 8 kv heads, to blocks of up to 256 words: one
+// workgroup per sequence, a wave for K and for V of each head.  A lane looks at
+// every 64th word of the block's codes, all of them requested together with the
+// new row; they are written again only where the scale moves.
+template <typename T, class F>
+__global__ __launch_bounds__(1024) void append_row_kernel(Write8Params p) {
+    const int b = blockIdx.x, lane = threadIdx.x & 63;
+    const int count = max(p.count[b], 0);
+    const int slot = count % p.R, shift = p.row_shift;
+    const int filled = min(count, p.R - 1) + 1;  // live after the append
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool is_v = w & 1;
+    const size_t head = (size_t)b * p.Hkv + (w >> 1);
+    const int j = slot >> p.log2_block, s0 = j << p.log2_block;
+    const int words = min(filled - s0, 1 << p.log2_block) << shift;
+    const T *src = static_cast<const T *>(is_v ? p.src_v : p.src_k) + (head << shift) * 16;
+    uint4 *dst = static_cast<uint4 *>(is_v ? p.v : p.k) + ((head * p.R + s0) << shift);
+    float *scale_at = (is_v ? p.vs : p.ks) + head * p.blocks + j;
+    const float old_scale = *scale_at;
+    const int first = (slot - s0) << shift;  // word of the new row
+    const auto is_old = [&](int i) { return i < words && (i >> shift) != slot - s0; };
+    Raw16<T> raw;
+    raw.clear();
+    const bool mine = lane < 1 << shift;
+    if (mine) raw.load(src + (size_t)lane * 16);
+    uint4 code[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) code[u] = dst[min(lane + u * 64, words - 1)];
+    float t_old = 0.f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+        if (is_old(lane + u * 64)) t_old = fmaxf(t_old, F::top16(code[u]));
+    uint32_t top = raw.top();
+    const bool plain = top < kInfBits;
+    if (!plain) top = raw.finite_top();
+    const int e = scale_exp<F>(wave_umax(max(top, old_mag(t_old, old_scale))));
+    const float scale = exp_scale(e), inv = exp_inverse(e);
+    if (scale != old_scale) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (is_old(lane + u * 64)) dst[lane + u * 64] = repack16<F>(code[u], old_scale, inv);
+        if (lane == 0) *scale_at = scale;
+    }
+    if (mine) {
+        float x[16];
+        raw.widen(x);
+        dst[first + lane] = pack16<F>(x, inv, plain);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) p.count[b] = count + 1;
+}
+
 // Sixteen bytes of values of 8 (bf16) or 4 codes.
 template <typename T, class F, typename Codes>
 __device__ __forceinline__ uint4 values16(const Codes &c, float scale) {
@@ -187,12 +239,20 @@ int touched_most(int T, int blocks, int log2_block) {
     return std::min({T, blocks, ((T - 1) >> log2_block) + 3});
 }
 
-// Every workgroup reads the counts, so a launch of its own raises them.  (One
-// workgroup per sequence that does both at its end: 8.4 us against 6.1 for a row
-// of 64 sequences, 4.9 against 5.0 for one sequence.)
+// Every workgroup of write_blocks_kernel reads the counts, so a launch of its own
+// raises them.  One row of a small block goes by append_row_kernel, which does
+// both.  Called from the host, 64 sequences of 8 heads of 128 take 6.7 us against
+// 9.7; in a graph one sequence takes 3.9 against 4.9, 8 take 5.0 against 5.3, 256
+// 8.8 against 9.0, and only about 64 lose (7.1 against 5.8).  Past a word in
+// each of four registers and a wave for every head, rounds add up: 8 sequences of 16
+// heads in blocks of 64 took 11.5 us in two rounds against 5.8.
 template <typename T, class F>
 hipError_t launch_append(const Write8Params &p, hipStream_t stream) {
     const int most = touched_most(p.T_new, p.blocks, p.log2_block);
+    if (p.T_new == 1 && p.Hkv <= 8 && p.log2_block + p.row_shift <= 8) {
+        append_row_kernel<T, F><<<p.B, 128 * p.Hkv, 0, stream>>>(p);
+        return hipGetLastError();
+    }
     if (hipError_t e = launch_blocks<T, F, true>(p, most, stream); e != hipSuccess) return e;
     return launch_window_count(p.count, p.B, p.T_new, stream);
 }
