@@ -806,6 +806,9 @@ def _decode_q8(step, q, cme_k, cme_v, cme_ks, cme_vs, k, win_k, win_v, win_ks, w
         raise ValueError("out [B][Hq][Dh] fp32")
     if workspace is None:
         workspace = decode_workspace_q8(B, Hq, Hkv, Dh, k, W, q.device)
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    scale = float(scale)
     dev = _device_index()
     if (q.get_device() != dev or out.get_device() != dev or workspace.get_device() != dev or cme_k.get_device() != dev
             or cme_v.get_device() != dev or cme_ks.get_device() != dev or cme_vs.get_device() != dev

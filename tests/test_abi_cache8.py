@@ -169,6 +169,17 @@ def test_wrappers_refuse_what_does_not_fit():
         cmc._code_dtype(x[0])
 
 
+def test_wrappers_refuse_a_workspace_with_gaps():
+    """Every second byte of a buffer that ends where the workspace would go on."""
+    w, q, count = _cache(), torch.zeros((1, 4, 64)), torch.zeros((1,), dtype=torch.int32)
+    new = torch.zeros((1, 2, 1, 64), dtype=torch.bfloat16)
+    ws = torch.zeros(2 * cmc.cmc_decode_q8_workspace_bytes(1, 4, 2, 64, 40, 40), dtype=torch.uint8)[::2]
+    with pytest.raises(ValueError, match="workspace must be contiguous"):
+        cmc.cmc_two_tier_decode_q8(q, *w, 40, *w, count, 0.1, 32, workspace=ws)
+    with pytest.raises(ValueError, match="workspace must be contiguous"):
+        cmc.cmc_decode_step_q8(q, *w, 40, *w, count, new, new, 0.1, 32, workspace=ws)
+
+
 def test_wrappers_refuse_host_tensors():
     w = _cache()
     with pytest.raises(Exception, match="device|CUDA|HIP|NVIDIA|GPU"):
