@@ -569,8 +569,10 @@ size_t cmc_decode_q8_workspace_bytes(int B, int Hq, int Hkv, int Dh, int k, int 
  *   q, win_count, scale, out, workspace: as cmc_two_tier_decode, the workspace
  *              of cmc_decode_q8_workspace_bytes
  *
- * A head with an empty key list gets zeros; one that attends to a NaN gets NaN.
- * Limits: Hq / Hkv in {1, 2, 4, 8}, 0 <= k <= N, k + W >= 1.
+ * A head with an empty key list gets zeros; one that attends to a NaN, or whose
+ * q is not finite, gets NaN, and no other head does.
+ * Limits: Hq / Hkv in {1, 2, 4, 8}, 0 <= k <= N, k + W >= 1; 4 (k + W) times the
+ * largest value within fp32's range.
  * Arithmetic: q and the softmax weights enter the products with 22 bits (two
  * fp16 parts), the codes as they are, fp32 sums in a fixed order (run-to-run
  * bit-identical); weights below 2^-16 of the largest keep fewer bits, to 2^-38 of

@@ -23,7 +23,8 @@
 // against ones gives l from the p that V was multiplied with.  p is scaled by
 // 2^13: hi + lo hold weights down to 2^-16 of the largest to 22 bits, and
 // below that to 2^-38 of the largest.  Each unit's product starts from zero and
-// is added with its block's s_V in fp32, so blocks of any scales mix.
+// is added with its block's s_V in fp32, so blocks of any scales mix; s_V and the
+// ones take the 2^13 away again, so sums stay within 4 times those of the values.
 //
 // The maximum is moved only when a score passes it by more than 2 (p <= 4),
 // which after the first units is rare; that test needs no exchange between
@@ -195,7 +196,8 @@ struct Walk8 {
     // The unit's share of l and acc; f: s_K over q's power of two.  Rows n and up are copies of row n - 1: they
     // may count in the maximum, and weigh 0.
     __device__ __forceinline__ void add(int set, const floatx4 (&c)[2], float f, int n) {
-        const float vs = un[set].vs;
+        constexpr float unscale = 1.f / (1 << kWeightExp);
+        const float vs = un[set].vs * unscale;
         float x[8];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -235,7 +237,7 @@ struct Walk8 {
             const _Float16 h = (_Float16)w[e];
             P[e] = (_Float16)fmaf(-(float)h, part, w[e]);  // hi: w itself; lo: what hi leaves
         }
-        constexpr _Float16 one = (_Float16)1.f;
+        constexpr _Float16 one = (_Float16)unscale;  // a normal fp16 number
         const halfx8 ones = {one, one, one, one, one, one, one, one};
         l = __builtin_amdgcn_mfma_f32_16x16x32_f16(P, ones, l, 0, 0, 0);
 #pragma unroll

@@ -235,3 +235,33 @@ def test_step_of_many_rows_captured_and_replayed():
         a = torch.randn(256, 256, device=DEV)
         (a @ a).sum().item()
     assert int(ring[4][0]) == int(start[4][0]) + 20 * 5
+
+
+@pytest.mark.parametrize("e", [106, -126])
+def test_values_of_extreme_blocks(e):
+    """Values near 2^115, whose sums over the keys (and twice the binades that the
+    running maximum may lag) fit fp32, and values at the smallest scale."""
+    for Dh in (64, 128, 256):
+        c = Case(2, 2, 2, Dh, 60, 50, "e4m3", 32, seed=e, counts=[50, 13])
+        c.pool[3].fill_(2.0 ** e)
+        c.win[3].fill_(2.0 ** e)
+        c.attend()
+        q = c.q()
+        out = cmc.cmc_two_tier_decode_q8(q, *c.pool, c.k, *c.win, c.count, np.float32(c.scale), c.block, workspace=c.ws)
+        assert torch.isfinite(out).all() and (out.abs().amax() > 2.0 ** e).item()
+
+
+def test_a_query_head_that_is_not_finite_stays_alone():
+    for what in (math.nan, math.inf, -math.inf):
+        for G, Dh in ((4, 128), (8, 64), (2, 256)):
+            c = Case(2, 2, G, Dh, 150, 70, "i8", 32, seed=G, counts=[70, 90])
+            q = c.q()
+            run = lambda: cmc.cmc_two_tier_decode_q8(q, *c.pool, c.k, *c.win, c.count, c.scale, c.block, workspace=c.ws)
+            good = run()
+            q[1, G, 5] = what
+            bad = run()
+            assert torch.isnan(bad[1, G]).all()
+            keep = torch.ones(bad.shape[:2], dtype=torch.bool, device=DEV)
+            keep[1, G] = False
+            assert torch.equal(bad[keep], good[keep])
+            assert not c.ws[:4 * (2 + 4)].any()
