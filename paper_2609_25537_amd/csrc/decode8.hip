@@ -203,8 +203,10 @@ struct Walk8 {
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[4 * t + i] = c[t][i] + dpp_sum_operand<0x128>(c[t][i]);  // hi + lo
-        const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
-                                fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))) * f;
+        float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
+                          fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))) * f;
+        if (__builtin_expect(__any(f < 0.f), 0))  // a cache made elsewhere may have scales below 0
+            top = fminf(fminf(fminf(x[0], x[1]), fminf(x[2], x[3])), fminf(fminf(x[4], x[5]), fminf(x[6], x[7]))) * f;
         if (__builtin_expect(__any(top > m + kMaxSlack), 0)) {
             const float mn = fmaxf(m, combine_xor32<OpMax>(combine_xor16<OpMax>(top)));
             const float alpha = fast_exp2(m - mn);  // 0 from kNoMax, where l and acc are 0

@@ -265,3 +265,18 @@ def test_a_query_head_that_is_not_finite_stays_alone():
             keep[1, G] = False
             assert torch.equal(bad[keep], good[keep])
             assert not c.ws[:4 * (2 + 4)].any()
+
+
+@pytest.mark.parametrize("code", ["e4m3", "i8"])
+def test_scales_below_zero(code):
+    """A cache made elsewhere whose scales have either sign, and logits of many
+    binades: the largest score of a block may be its smallest product."""
+    for Dh, G in ((64, 2), (128, 4), (256, 1)):
+        c = Case(2, 4, G, Dh, 333, 150, code, 32, seed=Dh, counts=[150, 70])
+        for s in (*c.pool[2:], *c.win[2:]):
+            s.mul_(torch.where(torch.rand(s.shape, generator=c.gen, device=DEV) < 0.5, -1.0, 1.0))
+        c.scale = 4.0
+        c.attend()
+        for kv, want_s in ((0, 2), (1, 3)):
+            got = cmc.cmc_cache_read_q8(*c.win, 32, dtype=torch.float32)[kv]
+            assert torch.equal(got.to(torch.float64), values(c.win[kv], c.win[want_s], 32))
