@@ -40,9 +40,10 @@
 // 256 (403 MB) 62 us, 6.4 TB/s; 64 of 8 heads of 128, 1536 keys and an append
 // (204 MB) 35.5 us, 5.7 TB/s.  Below that by the chain of one workgroup: 9 us
 // with 1.6 MB to read (8 pairs), of which the append 1.5.  Vector operations per
-// unit of Dh = 128: 221 for e4m3, 317 for int8, which costs int8 10% (192 pairs
-// of 1549 keys 17.8 / 19.6 us); the matrix units are busy for less than 10%
-// of the time.
+// unit of Dh = 128: 185 for e4m3, 281 for int8, which is up to 7% slower (one
+// sequence of 32808 keys 18.1 / 19.3 us); with the rows' addresses clamped and V
+// widened before its rows are paired they were 221 and 317, and times 1 to 2%
+// longer.  The matrix units are busy for less than 10% of the time.
 #include <stddef.h>
 
 #include "cache8.hpp"
@@ -93,31 +94,41 @@ struct Walk8 {
         for (int j = 0; j < D; ++j) acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // Rows past `last` (a list's last unit) are read as row `last`: loads without
-    // branches keep the compiler's wait counts exact.
-    __device__ __forceinline__ void load_k(int set, const char *k, int last) {
-        Unit &n = un[set];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const uint32_t o = (uint32_t)min(16 * t + r16, last) * DH + 16u * q4;
-#pragma unroll
-            for (int i = 0; i < SL; ++i) n.k[t][i] = *reinterpret_cast<const uint4 *>(k + o + 64 * i);
-        }
+    // The unit's first `rows` rows, the others as zeros, by the buffer loads'
+    // bounds: loads without branches keep the compiler's wait counts exact, and a
+    // row costs no address arithmetic (its offset is the lane's and a constant).
+    static constexpr int kNonTemporal = 2;
+    __device__ __forceinline__ static __amdgpu_buffer_rsrc_t unit_rows(const char *at, int rows) {
+        constexpr int untyped = 0x00027000;  // 32-bit elements, addressed by bytes
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at), 0, rows * DH, untyped);
     }
-    __device__ __forceinline__ void load_v(int set, const char *v, int last) {
+    __device__ __forceinline__ void load_k(int set, const char *k, int rows) {
         Unit &n = un[set];
+        const __amdgpu_buffer_rsrc_t from = unit_rows(k, rows);
+        const int o = r16 * DH + 16 * q4;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < SL; ++i) {
+                const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(from, o + 16 * t * DH + 64 * i, 0, 0);
+                n.k[t][i] = make_uint4(x[0], x[1], x[2], x[3]);
+            }
+    }
+    __device__ __forceinline__ void load_v(int set, const char *v, int rows) {
+        Unit &n = un[set];
+        const __amdgpu_buffer_rsrc_t from = unit_rows(v, rows);
+        const int o = 4 * q4 * DH + D * r16;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const uint32_t o = (uint32_t)min((j >> 2) * 16 + 4 * q4 + (j & 3), last) * DH + (uint32_t)D * r16;
+            const int at = o + ((j >> 2) * 16 + (j & 3)) * DH;
             if constexpr (SL == 1) {
-                n.v[j][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(v + o));
+                n.v[j][0] = __builtin_amdgcn_raw_buffer_load_b32(from, at, 0, kNonTemporal);
             } else if constexpr (SL == 2) {
-                typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-                const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(v + o));
+                const auto x = __builtin_amdgcn_raw_buffer_load_b64(from, at, 0, kNonTemporal);
                 n.v[j][0] = x[0];
                 n.v[j][1] = x[1];
             } else {
-                const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(v + o));
+                const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(from, at, 0, kNonTemporal);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) n.v[j][i] = x[i];
             }
@@ -193,8 +204,8 @@ struct Walk8 {
         asm volatile("" : "+v"(l));
     }
 
-    // The unit's share of l and acc; f: s_K over q's power of two.  Rows n and up are copies of row n - 1: they
-    // may count in the maximum, and weigh 0.
+    // The unit's share of l and acc; f: s_K over q's power of two.  Rows n and up
+    // neither count in the maximum nor weigh anything.
     __device__ __forceinline__ void add(int set, const floatx4 (&c)[2], float f, int n) {
         constexpr float unscale = 1.f / (1 << kWeightExp);
         const float vs = un[set].vs * unscale;
@@ -207,6 +218,12 @@ struct Walk8 {
                           fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))) * f;
         if (__builtin_expect(__any(f < 0.f), 0))  // a cache made elsewhere may have scales below 0
             top = fminf(fminf(fminf(x[0], x[1]), fminf(x[2], x[3])), fminf(fminf(x[4], x[5]), fminf(x[6], x[7]))) * f;
+        const auto live = [&](int e) { return (e >> 2) * 16 + 4 * q4 + (e & 3) < n; };
+        if (__builtin_expect(n < kUnit8, 0)) {
+            top = kNoMax;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = live(e) ? fmaxf(top, x[e] * f) : top;
+        }
         if (__builtin_expect(__any(top > m + kMaxSlack), 0)) {
             const float mn = fmaxf(m, combine_xor32<OpMax>(combine_xor16<OpMax>(top)));
             const float alpha = fast_exp2(m - mn);  // 0 from kNoMax, where l and acc are 0
@@ -230,7 +247,7 @@ struct Walk8 {
         for (int e = 0; e < 8; ++e) w[e] = fast_exp2(fmaf(x[e], f, -mp));
         if (__builtin_expect(n < kUnit8, 0)) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = (e >> 2) * 16 + 4 * q4 + (e & 3) < n ? w[e] : 0.f;
+            for (int e = 0; e < 8; ++e) w[e] = live(e) ? w[e] : 0.f;
         }
         const float part = r16 >= 8 ? 1.f : 0.f;
         halfx8 P;
@@ -244,19 +261,19 @@ struct Walk8 {
         l = __builtin_amdgcn_mfma_f32_16x16x32_f16(P, ones, l, 0, 0, 0);
 #pragma unroll
         for (int w = 0; w < SL; ++w) {
-            uint32_t a[8][2];
+            // Codes of two rows side by side, dim by dim, then widened.
+            uint32_t y[4][4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) F::half4(un[set].v[j][w], a[j][0], a[j][1]);
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t a = un[set].v[2 * j][w], b = un[set].v[2 * j + 1][w];
+                F::half4(__builtin_amdgcn_perm(b, a, 0x05010400), y[0][j], y[1][j]);
+                F::half4(__builtin_amdgcn_perm(b, a, 0x07030602), y[2][j], y[3][j]);
+            }
             floatx4 t[4];
 #pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                uint32_t y[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    y[j] = __builtin_amdgcn_perm(a[2 * j + 1][d >> 1], a[2 * j][d >> 1], d & 1 ? 0x07060302 : 0x05040100);
+            for (int d = 0; d < 4; ++d)
                 t[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-                    P, __builtin_bit_cast(halfx8, make_uint4(y[0], y[1], y[2], y[3])), floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-            }
+                    P, __builtin_bit_cast(halfx8, make_uint4(y[d][0], y[d][1], y[d][2], y[d][3])), floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
             for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -354,8 +371,8 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves8<DH>)) void decode8_kernel(c
     Place at{pk, pv, 0, 1, true};
     if (some) {
         at = place(u, W);
-        st.load_k(0, at.k, at.n - 1);
-        st.load_v(0, at.v, at.n - 1);
+        st.load_k(0, at.k, at.n);
+        st.load_v(0, at.v, at.n);
     }
     in_order();
     Decode8Params p = late_params();
@@ -412,10 +429,10 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves8<DH>)) void decode8_kernel(c
                 u += NW;
                 at = place(u, W);
                 in_order();
-                st.load_k(i, at.k, at.n - 1);
+                st.load_k(i, at.k, at.n);
                 st.un[i].ks = scale_k(at);
                 in_order();
-                st.load_v(i, at.v, at.n - 1);
+                st.load_v(i, at.v, at.n);
                 st.un[i].vs = scale_v(at);
                 n[i] = at.n;
             }
@@ -433,9 +450,9 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves8<DH>)) void decode8_kernel(c
             for (int i = 0; i < NS; ++i) {
                 if (i > 0 && u < end) u = after(u);
                 if (u < end) at = place(u, filled);
-                st.load_k(i, at.k, at.n - 1);
+                st.load_k(i, at.k, at.n);
                 st.un[i].ks = scale_k(at);
-                st.load_v(i, at.v, at.n - 1);
+                st.load_v(i, at.v, at.n);
                 st.un[i].vs = scale_v(at);
                 n[i] = u < end ? at.n : 0;
             }
@@ -453,13 +470,13 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves8<DH>)) void decode8_kernel(c
                 const bool more = u < end;
                 if (more) at = place(u, filled);
                 in_order();
-                st.load_k(i, at.k, at.n - 1);
+                st.load_k(i, at.k, at.n);
                 st.un[i].ks = scale_k(at);
                 in_order();
                 st.add(i, c, f, n[i]);
                 st.settle();
                 in_order();
-                st.load_v(i, at.v, at.n - 1);
+                st.load_v(i, at.v, at.n);
                 st.un[i].vs = scale_v(at);
                 n[i] = more ? at.n : 0;
                 u = more ? after(u) : u;
@@ -505,8 +522,8 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves8<DH>)) void decode8_kernel(c
             const int r = tb.block(i >> unit_shift) * per + (i & (per - 1));
             if (r * kUnit8 >= filled) continue;
             at = place(pool_units + r, filled);
-            st.load_k(0, at.k, at.n - 1);
-            st.load_v(0, at.v, at.n - 1);
+            st.load_k(0, at.k, at.n);
+            st.load_v(0, at.v, at.n);
             st.un[0].ks = scale_k(at);
             st.un[0].vs = scale_v(at);
             floatx4 c[2];
