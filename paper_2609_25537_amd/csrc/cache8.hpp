@@ -264,12 +264,13 @@ struct TouchedBlocks {
     }
 };
 
-// A workgroup of NT threads brings a ring block of K and V of
-// one (sequence, kv head) up to date with the rows appended at slot0: the
-// scales from the new rows and the live old ones, then the codes.  Where no
-// scale moves, only the new rows are written.  row_shift: log2 of a row's
-// 16-code words; filled: slots that are live after the append.  A barrier is
-// needed before anyone reads the block or another block is begun.
+// A workgroup of NT threads brings a ring block of K and V of one (sequence, kv
+// head) up to date with the rows appended at slot0, of which all make at most
+// NT words of 16 codes: the scales from the new rows and the live old ones, then
+// the codes.  A thread keeps one word of the new rows, requested together with
+// the old codes.  Where no scale moves, only the new rows are written.
+// row_shift: log2 of a row's words; filled: slots that are live after the append.
+// A barrier is needed before anyone reads the block or another block is begun.
 template <typename T, class F, int NT>
 __device__ __forceinline__ void append_block(const T *const (&rows)[2], uint8_t *const (&codes)[2], float *const (&scales)[2],
                                              int j, int log2_block, int row_shift, int W, int slot0, int filled, int T_new,
@@ -277,23 +278,22 @@ __device__ __forceinline__ void append_block(const T *const (&rows)[2], uint8_t 
     const int me = threadIdx.x;
     const int s0 = j << log2_block;
     const int words = min(1 << log2_block, filled - s0) << row_shift;
+    const int t = me >> row_shift, slot = slot0 + t < W ? slot0 + t : slot0 + t - W;
+    const bool mine = t < T_new && slot >> log2_block == j;
     uint4 *base[2];
     float old_scale[2], old_top[2] = {0.f, 0.f};
-    uint32_t top[2] = {0, 0};
+    Raw16<T> raw[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
         base[x] = reinterpret_cast<uint4 *>(codes[x]) + ((size_t)s0 << row_shift);
         old_scale[x] = scales[x][j];
+        raw[x].clear();
+        if (mine) raw[x].load(rows[x] + (size_t)me * 16);
     }
-    // appended row that word i belongs to; T_new or more: an old row
-    const auto row_of = [&](int i) {
-        const int t = s0 + (i >> row_shift) - slot0;
-        return t < 0 ? t + W : t;
+    const auto is_old = [&](int i) {
+        const int d = s0 + (i >> row_shift) - slot0;
+        return (d < 0 ? d + W : d) >= T_new;
     };
-    const auto new_word = [&](int x, int t, int i) {
-        return rows[x] + (((size_t)t << row_shift) + (i & ((1 << row_shift) - 1))) * 16;
-    };
-    bool plain = true;  // this thread's new words are finite
     constexpr int kTrip = 2;  // words of each array that a thread requests before it looks at the first
 #pragma unroll 1
     for (int i0 = me; i0 < words; i0 += NT * kTrip) {
@@ -304,66 +304,47 @@ __device__ __forceinline__ void append_block(const T *const (&rows)[2], uint8_t 
             for (int u = 0; u < kTrip; ++u) c[x][u] = base[x][min(i0 + u * NT, words - 1)];
 #pragma unroll
         for (int u = 0; u < kTrip; ++u) {
-            const int i = i0 + u * NT;
-            if (i >= words) continue;
-            const int t = row_of(i);
-            if (t < T_new) {
-                Raw16<T> r[2];
-#pragma unroll
-                for (int x = 0; x < 2; ++x) r[x].load(new_word(x, t, i));
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    uint32_t m = r[x].top();
-                    if (m >= kInfBits) {
-                        m = r[x].finite_top();
-                        plain = false;
-                    }
-                    top[x] = max(top[x], m);
-                }
-            } else {
+            if (i0 + u * NT < words && is_old(i0 + u * NT)) {
 #pragma unroll
                 for (int x = 0; x < 2; ++x) old_top[x] = fmaxf(old_top[x], F::top16(c[x][u]));
             }
         }
     }
+    bool plain[2];  // this thread's new words are finite
 #pragma unroll
-    for (int x = 0; x < 2; ++x) top[x] = wave_umax(max(top[x], old_mag(old_top[x], old_scale[x])));
-    if ((me & 63) == 0) {
-        s_top[0][me >> 6] = top[0];
-        s_top[1][me >> 6] = top[1];
+    for (int x = 0; x < 2; ++x) {
+        uint32_t top = raw[x].top();
+        plain[x] = top < kInfBits;
+        if (!plain[x]) top = raw[x].finite_top();
+        top = wave_umax(max(top, old_mag(old_top[x], old_scale[x])));
+        if ((me & 63) == 0) s_top[x][me >> 6] = top;
     }
     __syncthreads();
-#pragma unroll
-    for (int w = 0; w < NT / 64; ++w) {
-        top[0] = max(top[0], s_top[0][w]);
-        top[1] = max(top[1], s_top[1][w]);
-    }
     float scale[2], inv[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-        const int e = scale_exp<F>(top[x]);
+        uint32_t top = 0;
+#pragma unroll
+        for (int w = 0; w < NT / 64; ++w) top = max(top, s_top[x][w]);
+        const int e = scale_exp<F>(top);
         scale[x] = exp_scale(e);
         inv[x] = exp_inverse(e);
+        if (mine) {
+            float v[16];
+            raw[x].widen(v);
+            base[x][((slot - s0) << row_shift) + (me & ((1 << row_shift) - 1))] =
+                plain[x] ? pack16<F>(v, inv[x], true) : pack16<F>(v, inv[x], false);
+        }
     }
     // Old rows are passed by where no scale moved (where one did, codes of the
     // other array come out as they were).
-    const bool same = scale[0] == old_scale[0] && scale[1] == old_scale[1];
+    if (scale[0] != old_scale[0] || scale[1] != old_scale[1]) {
 #pragma unroll 1
-    for (int i = me; i < words; i += NT) {
-        const int t = row_of(i);
-        if (t < T_new) {
+        for (int i = me; i < words; i += NT)
+            if (is_old(i)) {
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                Raw16<T> r;
-                float v[16];
-                r.load(new_word(x, t, i));
-                r.widen(v);
-                base[x][i] = plain ? pack16<F>(v, inv[x], true) : pack16<F>(v, inv[x], false);
+                for (int x = 0; x < 2; ++x) base[x][i] = repack16<F>(base[x][i], old_scale[x], inv[x]);
             }
-        } else if (!same) {
-#pragma unroll
-            for (int x = 0; x < 2; ++x) base[x][i] = repack16<F>(base[x][i], old_scale[x], inv[x]);
-        }
     }
     if (me == 0) {
         scales[0][j] = scale[0];
