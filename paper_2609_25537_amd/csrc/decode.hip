@@ -788,6 +788,7 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves<NW, T, DH, G>)) void decode_
     }
 
     const bool bump = p.T_new > 0 && p.W > 0;
+    unsigned prev = ~0u;  // the sequence counter before this workgroup's arrival (one lane)
 
     WaveState<G, VEC> st;
     st.init();
@@ -822,7 +823,10 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves<NW, T, DH, G>)) void decode_
     if (bump && lane == 0) s_cnt[wave] = cnt.raw;  // stored once the wave's count read has returned
     __syncthreads();
 
-    finish_pair<NW, DH, G, false>(p, b, kvh, s, s_m, s_l, s_acc, s_cnt, cnt_now);
+    constexpr int kThreads = NW * kWave;
+    constexpr bool kKeepNaN = false;
+    constexpr int kMB = merge_batch<NW, DH, G>;
+#include "decode_finish.hpp"
 }
 
 template <typename T, int DH, int G>

@@ -46,6 +46,8 @@
 // longer.  The matrix units are busy for less than 10% of the time.
 #include <stddef.h>
 
+#include <type_traits>
+
 #include "cache8.hpp"
 #include "decode_common.hpp"
 
@@ -557,7 +559,19 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves8<DH>)) void decode8_kernel(c
     if (st.lane < G) s_m[wave][st.lane] = st.m;
     if (st.lane == 0) s_cnt[wave] = cnt.raw;  // stored once the wave's count read has returned
     __syncthreads();
-    finish_pair<NW, DH, G, true, true>(p, b, kvh, s, s_m, s_l, s_acc, s_cnt, cnt_now);
+    // The merge requests as many splits' partials at a time as there are, 8 to 32
+    // (one batch of 32 always: 8 pairs in 4 splits 7.4 -> 8.6 us).
+    constexpr int kThreads = NW * kWave, kMost = merge_batch<NW, DH, G>;
+    constexpr bool kKeepNaN = true, kOnePair = merge_pairs<NW, DH, G> == 1;
+    const bool bump = p.T_new > 0 && W > 0;
+    const auto finish = [&](auto batch) {
+        constexpr int kMB = decltype(batch)::value;
+        unsigned prev = ~0u;
+#include "decode_finish.hpp"
+    };
+    if (p.S <= 8 || kMost == 8) finish(std::integral_constant<int, 8>{});
+    else if (p.S <= 16 || !kOnePair) finish(std::integral_constant<int, kMost>{});
+    else finish(std::integral_constant<int, kOnePair ? 32 : 8>{});
 }
 
 template <class F, int DH, int G>
