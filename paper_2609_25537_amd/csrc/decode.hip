@@ -824,8 +824,7 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves<NW, T, DH, G>)) void decode_
     __syncthreads();
 
     constexpr int kThreads = NW * kWave;
-    constexpr bool kKeepNaN = false;
-    constexpr int kMB = merge_batch<NW, DH, G>;
+    constexpr bool kKeepNaN = false, kBySplits = false;
 #include "decode_finish.hpp"
 }
 

@@ -46,8 +46,6 @@
 // longer.  The matrix units are busy for less than 10% of the time.
 #include <stddef.h>
 
-#include <type_traits>
-
 #include "cache8.hpp"
 #include "decode_common.hpp"
 
@@ -345,11 +343,11 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves8<DH>)) void decode8_kernel(c
     if (s >= S - 1 - (own ? 1 : 0)) end = units;
     if (own && s == S - 1) u = units;
 
-    const size_t head = (size_t)b * Hkv + kvh;
-    const char *pk = static_cast<const char *>(cme_k) + head * (size_t)N * DH;
-    const char *pv = static_cast<const char *>(cme_v) + head * (size_t)N * DH;
-    const char *rk = static_cast<const char *>(win_k) + head * (size_t)W * DH;
-    const char *rv = static_cast<const char *>(win_v) + head * (size_t)W * DH;
+    const size_t pair = (size_t)b * Hkv + kvh;
+    const char *pk = static_cast<const char *>(cme_k) + pair * (size_t)N * DH;
+    const char *pv = static_cast<const char *>(cme_v) + pair * (size_t)N * DH;
+    const char *rk = static_cast<const char *>(win_k) + pair * (size_t)W * DH;
+    const char *rv = static_cast<const char *>(win_v) + pair * (size_t)W * DH;
     // A unit's place: its first row's codes, its number in its own array, and
     // its live rows.
     struct Place {
@@ -384,8 +382,8 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves8<DH>)) void decode8_kernel(c
     p.Hkv = Hkv;
     p.S = S;
     p.T_new = (int)((unsigned)info >> 16);
-    const float *pks = p.cme_ks + head * p.pool_blocks, *pvs = p.cme_vs + head * p.pool_blocks;
-    float *rks = p.win_ks + head * p.ring_blocks, *rvs = p.win_vs + head * p.ring_blocks;
+    const float *pks = p.cme_ks + pair * p.pool_blocks, *pvs = p.cme_vs + pair * p.pool_blocks;
+    float *rks = p.win_ks + pair * p.ring_blocks, *rvs = p.win_vs + pair * p.ring_blocks;
     const int unit_shift = p.log2_block - 5;  // units per block
     const auto scale_k = [&](const Place &at) { return (at.pool ? pks : rks)[at.r >> unit_shift]; };
     const auto scale_v = [&](const Place &at) { return (at.pool ? pvs : rvs)[at.r >> unit_shift]; };
@@ -500,7 +498,7 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves8<DH>)) void decode8_kernel(c
             start();
         }
         const int slot0 = cnt.value() % W;
-        const size_t src = head * (size_t)p.T_new * DH, dst = head * (size_t)W * DH;
+        const size_t src = pair * (size_t)p.T_new * DH, dst = pair * (size_t)W * DH;
         constexpr int shift = DH == 64 ? 2 : DH == 128 ? 3 : 4;
         uint8_t *const codes[2] = {static_cast<uint8_t *>(win_k) + dst, static_cast<uint8_t *>(win_v) + dst};
         float *const scales[2] = {rks, rvs};
@@ -559,19 +557,11 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves8<DH>)) void decode8_kernel(c
     if (st.lane < G) s_m[wave][st.lane] = st.m;
     if (st.lane == 0) s_cnt[wave] = cnt.raw;  // stored once the wave's count read has returned
     __syncthreads();
-    // The merge requests as many splits' partials at a time as there are, 8 to 32
-    // (one batch of 32 always: 8 pairs in 4 splits 7.4 -> 8.6 us).
-    constexpr int kThreads = NW * kWave, kMost = merge_batch<NW, DH, G>;
-    constexpr bool kKeepNaN = true, kOnePair = merge_pairs<NW, DH, G> == 1;
+    constexpr int kThreads = NW * kWave;
+    constexpr bool kKeepNaN = true, kBySplits = true;
     const bool bump = p.T_new > 0 && W > 0;
-    const auto finish = [&](auto batch) {
-        constexpr int kMB = decltype(batch)::value;
-        unsigned prev = ~0u;
+    unsigned prev = ~0u;  // the sequence counter before this workgroup's arrival (one lane)
 #include "decode_finish.hpp"
-    };
-    if (p.S <= 8 || kMost == 8) finish(std::integral_constant<int, 8>{});
-    else if (p.S <= 16 || !kOnePair) finish(std::integral_constant<int, kMost>{});
-    else finish(std::integral_constant<int, kOnePair ? 32 : 8>{});
 }
 
 template <class F, int DH, int G>

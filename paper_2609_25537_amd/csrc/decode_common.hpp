@@ -6,6 +6,8 @@
 #include <float.h>
 #include <limits.h>
 
+#include <type_traits>
+
 #include "device_common.hpp"
 #include "kernels.hpp"
 
