@@ -4,7 +4,7 @@
 // for K and V together: half of its threads hold the block's K in registers,
 // half its V, so every row is read once; the block's largest magnitude is
 // reduced over the half, and the codes go out as 16-byte stores.  All of it is
-// bound by memory (a gather of fp32 rows to int8, 229 MB, 44.6 us; an append of
+// bound by memory (a gather of fp32 rows to int8, 229 MB, 43 us; an append of
 // 1024 bf16 rows to 64 x 8 rings 72.9 us, 5.5 TB/s), the small calls by latency
 // (3.7 us for a gather of 256 rows of one sequence).
 #include <algorithm>

@@ -41,7 +41,7 @@
 // (204 MB) 35.5 us, 5.7 TB/s.  Below that by the chain of one workgroup: 9 us
 // with 1.6 MB to read (8 pairs), of which the append 1.5.  Vector operations per
 // unit of Dh = 128: 185 for e4m3, 281 for int8, which is up to 7% slower (one
-// sequence of 32808 keys 18.1 / 19.3 us); with the rows' addresses clamped and V
+// sequence of 32808 keys in a graph 18.1 / 19.3 us); with the rows' addresses clamped and V
 // widened before its rows are paired they were 221 and 317, and times 1 to 2%
 // longer.  The matrix units are busy for less than 10% of the time.
 #include <stddef.h>
