@@ -55,6 +55,25 @@ namespace {
 
 constexpr int kWeightExp = 13;   // p is held times 2^13
 constexpr float kMaxSlack = 2.f; // how far a score may pass the running maximum
+// Running maxima from here on, where fp32 is spaced by a half and more, take the
+// weights' argument apart (Walk8::add).
+constexpr float kFarScore = (float)(1 << 22);
+
+// x f and x f - m with the product rounded on its own: a maximum is such a product,
+// so its own difference is 0 (contracted, x f would enter with all its bits).
+__device__ __forceinline__ float rounded_product(float x, float f) {
+#pragma clang fp contract(off)
+    return x * f;
+}
+__device__ __forceinline__ float product_less(float x, float f, float m) {
+#pragma clang fp contract(off)
+    const float xf = x * f;
+    return xf - m;
+}
+__device__ __forceinline__ float difference(float a, float b) {
+#pragma clang fp contract(off)
+    return a - b;
+}
 
 // Keeps loads after this point from being issued before it, and arithmetic on
 // the registers they go to from being moved behind it.
@@ -214,17 +233,18 @@ struct Walk8 {
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[4 * t + i] = c[t][i] + dpp_sum_operand<0x128>(c[t][i]);  // hi + lo
-        float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
-                          fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))) * f;
+        float top = rounded_product(fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
+                                          fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))), f);
         if (__builtin_expect(__any(f < 0.f), 0))  // a cache made elsewhere may have scales below 0
-            top = fminf(fminf(fminf(x[0], x[1]), fminf(x[2], x[3])), fminf(fminf(x[4], x[5]), fminf(x[6], x[7]))) * f;
+            top = rounded_product(fminf(fminf(fminf(x[0], x[1]), fminf(x[2], x[3])),
+                                        fminf(fminf(x[4], x[5]), fminf(x[6], x[7]))), f);
         const auto live = [&](int e) { return (e >> 2) * 16 + 4 * q4 + (e & 3) < n; };
         if (__builtin_expect(n < kUnit8, 0)) {
             top = kNoMax;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = live(e) ? fmaxf(top, x[e] * f) : top;
+            for (int e = 0; e < 8; ++e) top = live(e) ? fmaxf(top, rounded_product(x[e], f)) : top;
         }
-        if (__builtin_expect(__any(top > m + kMaxSlack), 0)) {
+        if (__builtin_expect(__any(difference(top, m) > kMaxSlack), 0)) {
             const float mn = fmaxf(m, combine_xor32<OpMax>(combine_xor16<OpMax>(top)));
             const float alpha = fast_exp2(m - mn);  // 0 from kNoMax, where l and acc are 0
             const bool sums = __any(m != kNoMax);  // not at a wave's first unit
@@ -245,6 +265,15 @@ struct Walk8 {
         float w[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] = fast_exp2(fmaf(x[e], f, -mp));
+        // Below kFarScore the argument is off by half the spacing of m and of x f at
+        // most, so weights stay under 2^15.6, within fp16.  Above, m - 13 may round to
+        // m - 16, and the exact product lie far from the rounded one that m is: the
+        // largest key's own weight would leave fp16's range at either end.
+        if (__builtin_expect(__any(fabsf(m) >= kFarScore), 0)) {
+            const bool far = fabsf(m) >= kFarScore;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = far ? fast_exp2(product_less(x[e], f, m) + (float)kWeightExp) : w[e];
+        }
         if (__builtin_expect(n < kUnit8, 0)) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[e] = live(e) ? w[e] : 0.f;

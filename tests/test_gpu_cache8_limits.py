@@ -1,0 +1,135 @@
+"""The 8-bit cache at the ends of fp32's range: scores far past what a model has,
+against results that do not depend on how a score is rounded."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_25537_amd import cmc
+from tests.gpu_util import DEV, say
+
+pytestmark = pytest.mark.gpu
+
+CODE = {"e4m3": torch.float8_e4m3fn, "i8": torch.int8}
+
+
+def as_codes(x, code):
+    """Tensors of whole numbers (e4m3: multiples of 8 up to 120) as codes."""
+    return x.to(torch.float32).to(CODE[code])
+
+
+class Far:
+    """k Tier-1 rows and a full ring of W whose keys differ in their first dim
+    alone: key t holds level[t] there, and the query `size` times a factor of its
+    head's own in [1, 2)."""
+
+    def __init__(self, level, k, Hkv, G, Dh, code, seed):
+        B, n = 2, level.shape[-1]
+        W = n - k
+        gen = torch.Generator(device=DEV).manual_seed(seed)
+        self.K = torch.zeros((B, Hkv, n, Dh), device=DEV)
+        self.K[..., 0] = level
+        self.V = 8.0 * torch.randint(-15, 16, (B, Hkv, n, Dh), generator=gen, device=DEV)
+        self.B, self.Hkv, self.G, self.Dh, self.k, self.W = B, Hkv, G, Dh, k, W
+        one = lambda r: torch.ones((B, Hkv, -(-r // 32)), device=DEV)
+        cut = lambda x, a, b: as_codes(x[:, :, a:b].contiguous(), code)
+        self.pool = [cut(self.K, 0, k), cut(self.V, 0, k), one(k), one(k)]
+        self.win = [cut(self.K, k, n), cut(self.V, k, n), one(W), one(W)]
+        self.count = torch.full((B,), W, dtype=torch.int32, device=DEV)
+        self.factor = 1.0 + torch.rand((B, Hkv * G), generator=gen, device=DEV)
+        self.ws = cmc.decode_workspace_q8(B, Hkv * G, Hkv, Dh, k, W, DEV)
+
+    def query(self, size):
+        q = torch.zeros((self.B, self.Hkv * self.G, self.Dh), device=DEV)
+        q[..., 0] = self.factor * size
+        return q
+
+    def attend(self, q):
+        return cmc.cmc_two_tier_decode_q8(q, *self.pool, self.k, *self.win, self.count, 0.125, 32, workspace=self.ws)
+
+
+# log2 of the largest score (in units of log 2, a factor of 2 or so aside)
+SIZES = [18, 20, 21, 22, 23, 24, 25, 26, 27, 28, 29, 30, 31, 32, 34, 40, 60, 100]
+SHAPES = [(64, 1), (64, 8), (128, 4), (256, 2)]
+
+
+@pytest.mark.parametrize("code", ["e4m3", "i8"])
+@pytest.mark.parametrize("Dh,G", SHAPES)
+@pytest.mark.parametrize("sign", [1, -1])
+def test_far_scores_one_key(code, Dh, G, sign):
+    """One key's score passes the others' by an eighth of itself at least, 2^15 and
+    more: the output is its value.  Its weight is exact up to exp2's 2^-23, the
+    sum's and the quotient's roundings come to less than 2^-21."""
+    for at in (0, 37, 70, 129):  # in the pool, the ring, a unit of its own
+        gen = torch.Generator(device=DEV).manual_seed(at)
+        level = 8.0 * torch.randint(1, 8, (2, 3, 130), generator=gen, device=DEV)
+        level[..., at] = 64.0
+        if sign < 0:  # scores of -120 up to -64, and one of -56
+            level = level - 128.0
+            level[..., at] = -56.0
+        c = Far(level, 60, 3, G, Dh, code, seed=at)
+        want = c.V[:, :, at].repeat_interleave(G, dim=1)
+        for size in SIZES:
+            say("far scores", code, Dh, G, sign, "key", at, "2 **", size)
+            out = c.attend(c.query(2.0 ** size / 64 / 0.125))
+            assert ((out - want).abs() <= want.abs() * 2.0 ** -21).all(), (at, size)
+
+
+@pytest.mark.parametrize("code", ["e4m3", "i8"])
+@pytest.mark.parametrize("Dh,G", SHAPES)
+@pytest.mark.parametrize("sign", [1, -1])
+def test_far_scores_equal_keys(code, Dh, G, sign):
+    """Keys that are all the same weigh the same: the mean of the values, off by
+    the roundings of 130 terms' sums."""
+    c = Far(torch.full((2, 3, 130), 40.0 * sign, device=DEV), 60, 3, G, Dh, code, seed=1)
+    want = c.V.mean(2).repeat_interleave(G, dim=1)
+    bound = c.V.abs().mean(2).repeat_interleave(G, dim=1) * (130 * 2.0 ** -24 + 2.0 ** -20)
+    for size in SIZES:
+        say("far scores, equal keys", code, Dh, G, sign, "2 **", size)
+        out = c.attend(c.query(2.0 ** size / 40 / 0.125))
+        assert ((out - want).abs() <= bound).all(), size
+
+
+@pytest.mark.parametrize("code", ["e4m3", "i8"])
+@pytest.mark.parametrize("Dh,G", SHAPES)
+@pytest.mark.parametrize("sign", [1, -1])
+def test_far_scores_a_rounding_apart(code, Dh, G, sign):
+    """Scores that creep up (or down) by about a rounding from key to key, so that
+    the maximum is passed by about its slack: whatever they weigh, equal values
+    come out, off by the roundings of 130 terms' sums."""
+    c = Far(torch.full((2, 3, 130), 64.0 * sign, device=DEV), 60, 3, G, Dh, code, seed=2)
+    step = 8.0 * (torch.arange(130, device=DEV) // 9)  # 0 .. 112
+    K = c.K.clone()
+    K[..., 1] = step
+    c.pool[0], c.win[0] = as_codes(K[:, :, :60].contiguous(), code), as_codes(K[:, :, 60:].contiguous(), code)
+    for x in (c.pool[1], c.win[1]):
+        x.copy_(as_codes(torch.full(x.shape, 88.0, device=DEV), code))
+    for size in SIZES:
+        for creep in (2.0, -2.0, 8.0):
+            q = c.query(2.0 ** size / 64 / 0.125)
+            q[..., 1] = creep * max(2.0 ** (size - 23), 1.0)
+            say("far scores, close keys", code, Dh, G, sign, "2 **", size, creep)
+            out = c.attend(q)
+            assert ((out - 88.0).abs() <= 88.0 * (130 * 2.0 ** -24 + 2.0 ** -20)).all(), (size, creep)
+
+
+@pytest.mark.parametrize("code", ["e4m3", "i8"])
+def test_far_scores_in_a_step(code):
+    """The appended row against the others, by the fused step and by one of more
+    rows than it takes along."""
+    for T in (1, 20):
+        level = torch.full((2, 3, 130), 32.0, device=DEV)
+        c = Far(level, 60, 3, 4, 128, code, seed=3)
+        nk = torch.zeros((2, 3, T, 128), device=DEV)
+        nv = 8.0 * torch.randint(-15, 16, (2, 3, T, 128), device=DEV)
+        nv[..., 0] = 120.0  # the blocks' V scale stays 1 or a power of two below
+        nk[:, :, -1, 0] = 64.0
+        for size in (22, 26, 27, 30, 33):
+            say("far scores, step", code, T, "2 **", size)
+            out = cmc.cmc_decode_step_q8(c.query(2.0 ** size / 64 / 0.125), *c.pool, c.k, *c.win, c.count, nk, nv, 0.125, 32,
+                                         workspace=c.ws)
+            want = nv[:, :, -1].repeat_interleave(4, dim=1)
+            # nv's codes: e4m3's own numbers, or whole numbers under a scale of 1 or below
+            assert ((out - want).abs() <= want.abs() * 2.0 ** -21).all(), (T, size)
+            c.count.fill_(c.W)
