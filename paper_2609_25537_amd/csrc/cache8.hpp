@@ -63,11 +63,23 @@ struct CodeE4M3 {
         const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
         f[0] = lo[0]; f[1] = lo[1]; f[2] = hi[0]; f[3] = hi[1];
     }
-    // Four codes as fp16, which holds every code exactly.
-    __device__ __forceinline__ static void half4(uint32_t w, uint32_t &lo, uint32_t &hi) {
-        lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.f, false));
-        hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.f, true));
+    // Four codes as fp16, which holds every code exactly, times a power of two.
+    __device__ __forceinline__ static void half4(uint32_t w, uint32_t &lo, uint32_t &hi, float by = 1.f) {
+        lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, by, false));
+        hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, by, true));
     }
+    // The factor of 2^-13 that weights times 2^13 leave to a block's codes or to its
+    // scale.  The scale takes it where it stays a normal number.  Codes hold it exactly
+    // too, but as subnormals, of whose products the matrix units keep a bit less.
+    struct Down13 {
+        float by;
+        __device__ __forceinline__ explicit Down13(float &scale) {
+            const bool small = fabsf(scale) < 0x1p-113f;
+            by = small ? 0x1p-13f : 1.f;
+            scale *= small ? 1.f : 0x1p-13f;
+        }
+        __device__ __forceinline__ void half4(uint32_t w, uint32_t &lo, uint32_t &hi) const { CodeE4M3::half4(w, lo, hi, by); }
+    };
 };
 
 struct CodeI8 {
@@ -103,13 +115,22 @@ struct CodeI8 {
         f[3] = (float)((int32_t)w >> 24);
     }
     // fp16 with the bits 0x6400 | u is 1024 + u for u < 1024, and u = code +
-    // 128 is the code with its sign bit flipped: subtracting 1152 is exact.
+    // 128 is the code with its sign bit flipped: subtracting 1152 is exact.  With
+    // an exponent DOWN lower all of it is times 2^-DOWN.
+    template <int DOWN = 0>
     __device__ __forceinline__ static void half4(uint32_t w, uint32_t &lo, uint32_t &hi) {
+        constexpr uint32_t top = (0x64u - (DOWN << 2)) * 0x01010101u;
+        constexpr float mid = 1152.f / (1 << DOWN);
         const uint32_t u = w ^ 0x80808080u;
-        const halfx2 k = {(_Float16)1152.f, (_Float16)1152.f};
-        lo = __builtin_bit_cast(uint32_t, __builtin_bit_cast(halfx2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400)) - k);
-        hi = __builtin_bit_cast(uint32_t, __builtin_bit_cast(halfx2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402)) - k);
+        const halfx2 k = {(_Float16)mid, (_Float16)mid};
+        lo = __builtin_bit_cast(uint32_t, __builtin_bit_cast(halfx2, __builtin_amdgcn_perm(top, u, 0x04010400)) - k);
+        hi = __builtin_bit_cast(uint32_t, __builtin_bit_cast(halfx2, __builtin_amdgcn_perm(top, u, 0x04030402)) - k);
     }
+    // As CodeE4M3's: whole numbers times 2^-13 are normal, so the codes take it always.
+    struct Down13 {
+        __device__ __forceinline__ explicit Down13(float &) {}
+        __device__ __forceinline__ void half4(uint32_t w, uint32_t &lo, uint32_t &hi) const { CodeI8::half4<13>(w, lo, hi); }
+    };
 };
 
 // e of the scale 2^e for the largest magnitude whose fp32 bits are `a` (finite).

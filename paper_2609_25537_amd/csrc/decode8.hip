@@ -23,8 +23,9 @@
 // against ones gives l from the p that V was multiplied with.  p is scaled by
 // 2^13: hi + lo hold weights down to 2^-16 of the largest to 22 bits, and
 // below that to 2^-38 of the largest.  Each unit's product starts from zero and
-// is added with its block's s_V in fp32, so blocks of any scales mix; s_V and the
-// ones take the 2^13 away again, so sums stay within 4 times those of the values.
+// is added with its block's s_V in fp32, so blocks of any scales mix; the ones, and
+// V's codes or s_V (Down13), take the 2^13 away again, so sums stay within 4 times
+// those of the values.
 //
 // The maximum is moved only when a score passes it by more than 2 (p <= 4),
 // which after the first units is rare; that test needs no exchange between
@@ -53,7 +54,7 @@ namespace cmc {
 
 namespace {
 
-constexpr int kWeightExp = 13;   // p is held times 2^13
+constexpr int kWeightExp = 13;   // p is held times 2^13 (Down13 takes it away)
 constexpr float kMaxSlack = 2.f; // how far a score may pass the running maximum
 // Running maxima from here on, where fp32 is spaced by a half and more, take the
 // weights' argument apart (Walk8::add).
@@ -226,8 +227,8 @@ struct Walk8 {
     // The unit's share of l and acc; f: s_K over q's power of two.  Rows n and up
     // neither count in the maximum nor weigh anything.
     __device__ __forceinline__ void add(int set, const floatx4 (&c)[2], float f, int n) {
-        constexpr float unscale = 1.f / (1 << kWeightExp);
-        const float vs = un[set].vs * unscale;
+        float vs = un[set].vs;
+        const typename F::Down13 down(vs);
         float x[8];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -285,7 +286,7 @@ struct Walk8 {
             const _Float16 h = (_Float16)w[e];
             P[e] = (_Float16)fmaf(-(float)h, part, w[e]);  // hi: w itself; lo: what hi leaves
         }
-        constexpr _Float16 one = (_Float16)unscale;  // a normal fp16 number
+        constexpr _Float16 one = (_Float16)(1.f / (1 << kWeightExp));  // a normal fp16 number
         const halfx8 ones = {one, one, one, one, one, one, one, one};
         l = __builtin_amdgcn_mfma_f32_16x16x32_f16(P, ones, l, 0, 0, 0);
 #pragma unroll
@@ -295,8 +296,8 @@ struct Walk8 {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const uint32_t a = un[set].v[2 * j][w], b = un[set].v[2 * j + 1][w];
-                F::half4(__builtin_amdgcn_perm(b, a, 0x05010400), y[0][j], y[1][j]);
-                F::half4(__builtin_amdgcn_perm(b, a, 0x07030602), y[2][j], y[3][j]);
+                down.half4(__builtin_amdgcn_perm(b, a, 0x05010400), y[0][j], y[1][j]);
+                down.half4(__builtin_amdgcn_perm(b, a, 0x07030602), y[2][j], y[3][j]);
             }
             floatx4 t[4];
 #pragma unroll

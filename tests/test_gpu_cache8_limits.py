@@ -133,3 +133,33 @@ def test_far_scores_in_a_step(code):
             # nv's codes: e4m3's own numbers, or whole numbers under a scale of 1 or below
             assert ((out - want).abs() <= want.abs() * 2.0 ** -21).all(), (T, size)
             c.count.fill_(c.W)
+
+
+# ------------------------------------------------------------------ scales
+
+@pytest.mark.parametrize("code", ["e4m3", "i8"])
+@pytest.mark.parametrize("Dh,G", SHAPES)
+@pytest.mark.parametrize("span", ["all", "small"])
+def test_small_scales_of_a_foreign_cache(code, Dh, G, span):
+    """V scales down to fp32's smallest normal numbers that are no powers of two.
+    Keys of zeros make every weight the same, and values of one sign keep the mean's
+    magnitude: sums of 130 terms, exp2 and the quotient are off by less than
+    (130 + 16) 2^-24 of it."""
+    gen = torch.Generator(device=DEV).manual_seed(Dh + G)
+    c = Far(torch.zeros((2, 3, 130), device=DEV), 60, 3, G, Dh, code, seed=4)
+    # every code above 0, or the least of them (e4m3: its subnormals, under scales that
+    # leave the means normal numbers)
+    top = 8 if span == "small" else 127
+    floor = 2.0 ** -117 if code == "e4m3" and span == "small" else 2.0 ** -126
+    b = torch.randint(1, top, (2, 3, 130, Dh), generator=gen, device=DEV, dtype=torch.int32).to(torch.int8)
+    V = b.view(CODE[code])
+    c.pool[1], c.win[1] = V[:, :, :60].contiguous(), V[:, :, 60:].contiguous()
+    for e in (0, 1, 6, 12, 13, 14, 30):
+        for s in (c.pool[3], c.win[3]):
+            s.copy_((1.0 + torch.rand(s.shape, generator=gen, device=DEV)) * floor * 2.0 ** e)
+        rows = lambda s, n: s.to(torch.float64)[:, :, torch.arange(n, device=DEV) // 32, None]
+        v = V.to(torch.float32).to(torch.float64) * torch.cat([rows(c.pool[3], 60), rows(c.win[3], 70)], dim=2)
+        want = v.mean(2).repeat_interleave(G, dim=1)
+        say("small scales", code, Dh, G, span, e)
+        out = c.attend(c.query(1.0)).to(torch.float64)
+        assert ((out - want).abs() <= want * (130 + 16) * 2.0 ** -24).all(), e
