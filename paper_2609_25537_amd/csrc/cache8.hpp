@@ -74,9 +74,11 @@ struct CodeE4M3 {
     struct Down13 {
         float by;
         __device__ __forceinline__ explicit Down13(float &scale) {
-            const bool small = fabsf(scale) < 0x1p-113f;
-            by = small ? 0x1p-13f : 1.f;
-            scale *= small ? 1.f : 0x1p-13f;
+            uint32_t e = __builtin_amdgcn_ubfe(__float_as_uint(scale), 23, 8);
+            asm("" : "+v"(e));  // compared as it is, with a constant that needs no register
+            const bool small = e < 127 - 113;
+            by = ldexpf(1.f, small ? -13 : 0);
+            scale = ldexpf(scale, small ? 0 : -13);
         }
         __device__ __forceinline__ void half4(uint32_t w, uint32_t &lo, uint32_t &hi) const { CodeE4M3::half4(w, lo, hi, by); }
     };

@@ -55,10 +55,10 @@ namespace cmc {
 namespace {
 
 constexpr int kWeightExp = 13;   // p is held times 2^13 (Down13 takes it away)
-constexpr float kMaxSlack = 2.f; // how far a score may pass the running maximum
-// Running maxima from here on, where fp32 is spaced by a half and more, take the
+constexpr float kMaxSlack = 2.f; // how far a score may pass a running maximum below 2^22
+// Running maxima of 2^22 and more, where fp32 is spaced by a half and more, take the
 // weights' argument apart (Walk8::add).
-constexpr float kFarScore = (float)(1 << 22);
+constexpr int kFarExp = 22;
 
 // x f and x f - m with the product rounded on its own: a maximum is such a product,
 // so its own difference is 0 (contracted, x f would enter with all its bits).
@@ -71,9 +71,13 @@ __device__ __forceinline__ float product_less(float x, float f, float m) {
     const float xf = x * f;
     return xf - m;
 }
-__device__ __forceinline__ float difference(float a, float b) {
-#pragma clang fp contract(off)
-    return a - b;
+
+// A constant loaded where it is used, on a rare path: the walk's loop fills the scalar
+// registers, and with one more constant kept in them its pointers were spilled
+// (batch-1 step 9.05 -> 9.2 us, 64 sequences 36.7 -> 37.1).
+__device__ __forceinline__ float made_here(float c) {
+    asm("" : "+v"(c));
+    return c;
 }
 
 // Keeps loads after this point from being issued before it, and arithmetic on
@@ -101,6 +105,7 @@ struct Walk8 {
     halfx8 q[2 * SL];
     float qf;                 // scale log2(e) over q's power of two
     float m;                  // of head (lane % 16) % G
+    float limit;              // the largest score that m may stay for
     floatx4 l, acc[D];        // rows 4 (lane / 16) + i: heads, hi and lo
     int lane, r16, q4;
 
@@ -109,6 +114,7 @@ struct Walk8 {
         r16 = lane & 15;
         q4 = lane >> 4;
         m = kNoMax;
+        limit = kNoMax;
         l = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < D; ++j) acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -241,15 +247,18 @@ struct Walk8 {
                                         fminf(fminf(x[4], x[5]), fminf(x[6], x[7]))), f);
         const auto live = [&](int e) { return (e >> 2) * 16 + 4 * q4 + (e & 3) < n; };
         if (__builtin_expect(n < kUnit8, 0)) {
-            top = kNoMax;
+            top = made_here(kNoMax);
 #pragma unroll
             for (int e = 0; e < 8; ++e) top = live(e) ? fmaxf(top, rounded_product(x[e], f)) : top;
         }
-        if (__builtin_expect(__any(difference(top, m) > kMaxSlack), 0)) {
+        float mp = m - (float)kWeightExp, by = f;
+        if (__builtin_expect(__any(top > limit), 0)) {
             const float mn = fmaxf(m, combine_xor32<OpMax>(combine_xor16<OpMax>(top)));
             const float alpha = fast_exp2(m - mn);  // 0 from kNoMax, where l and acc are 0
-            const bool sums = __any(m != kNoMax);  // not at a wave's first unit
+            const bool sums = __any(m != made_here(kNoMax));  // not at a wave's first unit
             m = mn;
+            const bool far = __builtin_amdgcn_frexp_expf(m) > kFarExp;
+            limit = far ? -INFINITY : m + kMaxSlack;  // far maxima come here with every unit
             if (sums) {
                 float al[4];
 #pragma unroll
@@ -261,20 +270,21 @@ struct Walk8 {
                     for (int j = 0; j < D; ++j) acc[j][i] *= al[i];
                 }
             }
+            mp = far ? 0.f : m - (float)kWeightExp;
+            // Below 2^22 the argument x f - mp is off by half the spacing of m and
+            // of x f at most, so weights stay under 2^15.6, within fp16.  Above, m - 13
+            // may round to m - 16, and the exact product lie far from the rounded one
+            // that m is: the largest key's own weight would leave fp16's range at either
+            // end.
+            if (__builtin_expect(__any(far), 0)) {
+                by = far ? 1.f : f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = far ? product_less(x[e], f, m) + (float)kWeightExp : x[e];
+            }
         }
-        const float mp = m - (float)kWeightExp;
         float w[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = fast_exp2(fmaf(x[e], f, -mp));
-        // Below kFarScore the argument is off by half the spacing of m and of x f at
-        // most, so weights stay under 2^15.6, within fp16.  Above, m - 13 may round to
-        // m - 16, and the exact product lie far from the rounded one that m is: the
-        // largest key's own weight would leave fp16's range at either end.
-        if (__builtin_expect(__any(fabsf(m) >= kFarScore), 0)) {
-            const bool far = fabsf(m) >= kFarScore;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = far ? fast_exp2(product_less(x[e], f, m) + (float)kWeightExp) : w[e];
-        }
+        for (int e = 0; e < 8; ++e) w[e] = fast_exp2(fmaf(x[e], by, -mp));
         if (__builtin_expect(n < kUnit8, 0)) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[e] = live(e) ? w[e] : 0.f;
@@ -462,8 +472,8 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves8<DH>)) void decode8_kernel(c
                 st.load_k(i, at.k, at.n);
                 st.un[i].ks = scale_k(at);
                 in_order();
-                st.load_v(i, at.v, at.n);
                 st.un[i].vs = scale_v(at);
+                st.load_v(i, at.v, at.n);
                 n[i] = at.n;
             }
         }
@@ -506,8 +516,8 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves8<DH>)) void decode8_kernel(c
                 st.add(i, c, f, n[i]);
                 st.settle();
                 in_order();
-                st.load_v(i, at.v, at.n);
                 st.un[i].vs = scale_v(at);
+                st.load_v(i, at.v, at.n);
                 n[i] = more ? at.n : 0;
                 u = more ? after(u) : u;
             }
