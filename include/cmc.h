@@ -493,7 +493,9 @@ cmc_status cmc_decode_step_noalloc(const float *q,
  * codes are multiplied by old scale / new scale and rounded, which is exact
  * when the scale falls; when it grows e4m3 loses only what falls below its
  * normal range, and int8 at most half of the new scale.  The decode and the
- * read-back take any finite scales, e.g. of a cache made elsewhere.
+ * read-back take any finite scales, e.g. of a cache made elsewhere.  Elements of
+ * 31/32 (e4m3; int8: 127/128) times 2^128 and more round to 2^128, which reads back
+ * as infinity and is past the decode's limits; appends keep them as they are.
  *
  * Common limits: Hkv >= 1, B and Hkv <= 65535, Dh in {64, 128, 256}, at most
  * 2^26 rows an array, else CMC_ERR_UNSUPPORTED.

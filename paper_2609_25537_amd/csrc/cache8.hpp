@@ -18,6 +18,8 @@
 // each time the maximum moved.
 #pragma once
 
+#include <float.h>
+
 #include "device_common.hpp"
 
 namespace cmc {
@@ -240,9 +242,12 @@ __device__ __forceinline__ void widen16(const uint4 &c, float (&x)[16]) {
 
 // The largest magnitude of a block's old codes as a part of its new maximum.  A
 // top of 0 (no live old row, or only zeros) counts for nothing, whatever the old
-// scale holds.
+// scale holds.  Codes may stand for more than fp32's largest number (elements within
+// half a step of 2^128, and infinities next to those): they count as that number,
+// whose scale is the one that they have.
 __device__ __forceinline__ uint32_t old_mag(float codes_top, float old_scale) {
-    return codes_top > 0.f ? finite_mag(codes_top * old_scale) : 0u;
+    const uint32_t u = __float_as_uint(codes_top * old_scale) & 0x7fffffffu;
+    return codes_top > 0.f && u <= kInfBits ? min(u, kInfBits - 1) : 0u;
 }
 
 // Codes of sixteen elements.  plain: all of them are finite, so that none
@@ -259,14 +264,17 @@ __device__ __forceinline__ uint4 pack16(const float (&x)[16], float inv, bool pl
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// Codes under a new scale of sixteen codes under an old one.
+// Codes under a new scale of sixteen codes under an old one, by the scales' ratio:
+// the values themselves may lie past fp32's largest number.  Only where all codes are
+// 0 may the ratio.
 template <class F>
 __device__ __forceinline__ uint4 repack16(const uint4 &c, float old_scale, float inv) {
+    const float ratio = __builtin_amdgcn_fmed3f(old_scale * inv, -FLT_MAX, FLT_MAX);
     float x[16];
     widen16<F>(c, x);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) x[e] *= old_scale;
-    return pack16<F>(x, inv, false);
+    for (int e = 0; e < 16; ++e) x[e] *= ratio;
+    return pack16<F>(x, 1.f, false);
 }
 
 // The ring blocks that an append of T_new rows at slot0 writes: consecutive

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from paper_2609_25537_amd import cmc
+from tests import q8_ref
 from tests.gpu_util import DEV, say
 
 pytestmark = pytest.mark.gpu
@@ -163,3 +164,52 @@ def test_small_scales_of_a_foreign_cache(code, Dh, G, span):
         say("small scales", code, Dh, G, span, e)
         out = c.attend(c.query(1.0)).to(torch.float64)
         assert ((out - want).abs() <= want * (130 + 16) * 2.0 ** -24).all(), e
+
+
+# ------------------------------------------------------------------ values
+
+def host(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+@pytest.mark.parametrize("code", ["e4m3", "i8"])
+@pytest.mark.parametrize("Dh,block", [(64, 32), (256, 128)])
+@pytest.mark.parametrize("path,T", [("append", 1), ("append", 3), ("step", 1), ("step", 5), ("append", 40)])
+def test_rings_of_the_largest_values(code, Dh, block, path, T):
+    """Elements up to fp32's largest, whose codes stand for 2^128, and infinities,
+    whose codes stand for more, keep their block's scale until they are evicted,
+    and their codes where only the other array's scale moves."""
+    H, W = 2, 40
+    rng = np.random.default_rng(T)
+    n = -(-W // block)
+    most = float(np.finfo(np.float32).max)
+    fresh = lambda: torch.zeros((1, H, W, Dh), dtype=torch.int8, device=DEV).view(CODE[code])
+    ring = [fresh(), fresh(), torch.zeros((1, H, n), device=DEV), torch.zeros((1, H, n), device=DEV)]
+    count = torch.zeros((1,), dtype=torch.int32, device=DEV)
+    model = [(np.zeros((H, W, Dh)), np.zeros((H, n))) for _ in range(2)]
+    pool = [torch.zeros((1, H, 8, Dh), dtype=torch.int8, device=DEV).view(CODE[code]), torch.ones((1, H, 1), device=DEV)]
+    q = torch.zeros((1, H, Dh), device=DEV)
+    seen, step = 0, 0
+    while seen < 3 * W:
+        nk = rng.standard_normal((1, H, T, Dh)) * 1.5 ** step  # K's scale moves every other time
+        nv = rng.standard_normal((1, H, T, Dh)) * 1e37
+        if step == 0:
+            nv[0, 0, 0, :8] = [most, -most, np.inf, -np.inf, 3.3e38, -3.37e38, 2.5e38, 0.96875 * 2.0 ** 128]
+            nv[0, 1, 0, :3] = [np.inf, 3e38, -1e-3]
+        nk, nv = nk.astype(np.float32), nv.astype(np.float32)
+        dk, dv = (torch.from_numpy(x).to(DEV) for x in (nk, nv))
+        say("largest values", code, Dh, block, path, T, "row", seen)
+        if path == "append":
+            cmc.cmc_window_append_q8(*ring, count, dk, dv, block)
+        else:
+            cmc.cmc_decode_step_q8(q, pool[0], pool[0], pool[1], pool[1], 8, *ring, count, dk, dv, 0.1, block)
+        for x, new in enumerate((nk, nv)):
+            c, s = model[x]
+            for h in range(H):
+                q8_ref.append(c[h], s[h], seen, new[0, h].astype(np.float64), code, block)
+            assert (host(ring[2 + x])[0] == s).all(), (seen, x)
+            assert (host(ring[x])[0] == c).all(), (seen, x)
+        seen += T
+        step += 1
+        assert int(count) == seen
+    assert model[1][1].max() < 2.0 ** (120 if code == "e4m3" else 122)  # the large ones are gone
