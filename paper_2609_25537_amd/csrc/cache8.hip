@@ -200,14 +200,14 @@ __device__ __forceinline__ uint4 values16(const Codes &c, float scale) {
 // with 16 codes a thread, whose stores leave gaps for the next one, 96.4 us (to
 // fp32 446 against 85).
 template <typename T, class F>
-__global__ __launch_bounds__(256) void read_kernel(Read8Params p) {
+__global__ __launch_bounds__(256) void read_kernel(Read8Params p, int group0) {
     constexpr int E = Vec16<T>::N;  // codes a thread takes
     typedef std::conditional_t<E == 8, uint2, uint32_t> Codes;
     const int h = blockIdx.y, b = blockIdx.z;
     const size_t head = (size_t)b * p.Hkv + h;
     const int shift = p.row_shift + (E == 8 ? 1 : 2);  // log2 of the threads to a row
     const int count = p.count ? p.count[b] : p.R;
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    const long long i = (long long)(group0 + (int)blockIdx.x) * 256 + threadIdx.x;
     const long long r = i >> shift;
     if (r >= min(count, p.R)) return;
     long long row = r + (count > p.R ? count % p.R : 0);
@@ -259,6 +259,20 @@ hipError_t launch_append(const Write8Params &p, hipStream_t stream) {
     return launch_window_count(p.count, p.B, p.T_new, stream);
 }
 
+template <typename T, class F>
+hipError_t launch_read(const Read8Params &p, hipStream_t stream) {
+    const long long threads = (long long)p.R << (p.row_shift + (sizeof(T) == 2 ? 1 : 2));
+    const int groups = (int)((threads + 255) / 256);  // 2^24 at most
+    // A grid holds less than 2^32 threads a dimension, which 2^26 rows of 256 in fp32
+    // reach: those take two launches.
+    constexpr int kMost = (1 << 24) - 1;
+    for (int at = 0; at < groups; at += kMost) {
+        read_kernel<T, F><<<dim3(std::min(groups - at, kMost), p.Hkv, p.B), 256, 0, stream>>>(p, at);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 }  // namespace
 
 hipError_t launch_gather8(const Write8Params &p, bool bf16, bool e4m3, hipStream_t stream) {
@@ -274,13 +288,8 @@ hipError_t launch_append8(const Write8Params &p, bool bf16, bool e4m3, hipStream
 }
 
 hipError_t launch_read8(const Read8Params &p, bool bf16, bool e4m3, hipStream_t stream) {
-    const long long threads = (long long)p.R << (p.row_shift + (bf16 ? 1 : 2));
-    const dim3 grid((unsigned)((threads + 255) / 256), p.Hkv, p.B);
-    if (bf16 && e4m3) read_kernel<uint16_t, CodeE4M3><<<grid, 256, 0, stream>>>(p);
-    else if (bf16) read_kernel<uint16_t, CodeI8><<<grid, 256, 0, stream>>>(p);
-    else if (e4m3) read_kernel<float, CodeE4M3><<<grid, 256, 0, stream>>>(p);
-    else read_kernel<float, CodeI8><<<grid, 256, 0, stream>>>(p);
-    return hipGetLastError();
+    if (bf16) return e4m3 ? launch_read<uint16_t, CodeE4M3>(p, stream) : launch_read<uint16_t, CodeI8>(p, stream);
+    return e4m3 ? launch_read<float, CodeE4M3>(p, stream) : launch_read<float, CodeI8>(p, stream);
 }
 
 }  // namespace cmc

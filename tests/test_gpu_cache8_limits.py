@@ -213,3 +213,32 @@ def test_rings_of_the_largest_values(code, Dh, block, path, T):
         step += 1
         assert int(count) == seen
     assert model[1][1].max() < 2.0 ** (120 if code == "e4m3" else 122)  # the large ones are gone
+
+
+@pytest.mark.parametrize("R", [1 << 26, (1 << 26) - 3])
+def test_read_back_of_the_longest_cache(R):
+    """As many rows as a cache may have, of 256 to fp32: more threads than a launch
+    holds in one dimension."""
+    torch.cuda.empty_cache()
+    Dh = 256
+    k8 = torch.zeros((1, 1, R, Dh), dtype=torch.int8, device=DEV)
+    scale = torch.ones((1, 1, -(-R // 128)), device=DEV)
+    k8[0, 0, 0], k8[0, 0, R - 1], k8[0, 0, R // 2] = 5, 7, 9
+    scale[0, 0, -1] = 0.5
+    count = torch.full((1,), R, dtype=torch.int32, device=DEV)
+    out = torch.empty((1, 1, R, Dh), device=DEV)
+    say("longest cache", R)
+    # K and V alike, into the same place: 64 GiB of output instead of 128
+    cmc.cmc_cache_read_q8(k8, k8, scale, scale, 128, count=count, out_k=out, out_v=out)
+    for at, want in ((0, 5.0), (1, 0.0), (R // 2, 9.0), (R - 2, 0.0), (R - 1, 3.5)):
+        assert (out[0, 0, at] == want).all(), at
+    assert float(out[0, 0, R - 4096:].sum(dtype=torch.float64)) == 3.5 * Dh
+    out[0, 0, :8] = -1.0
+    count.fill_(3)  # three live rows: nothing else is written
+    cmc.cmc_cache_read_q8(k8, k8, scale, scale, 128, count=count, out_k=out, out_v=out)
+    assert (out[0, 0, 0] == 5).all() and (out[0, 0, 1:3] == 0).all() and (out[0, 0, 3:8] == -1).all()
+    count.fill_(R + 1)  # wrapped by one: the oldest is row 1
+    cmc.cmc_cache_read_q8(k8, k8, scale, scale, 128, count=count, out_k=out, out_v=out)
+    assert (out[0, 0, R - 1] == 5).all() and (out[0, 0, R - 2] == 3.5).all() and (out[0, 0, 0] == 0).all()
+    del k8, out
+    torch.cuda.empty_cache()
