@@ -72,14 +72,6 @@ __device__ __forceinline__ float product_less(float x, float f, float m) {
     return xf - m;
 }
 
-// A constant loaded where it is used, on a rare path: the walk's loop fills the scalar
-// registers, and with one more constant kept in them its pointers were spilled
-// (batch-1 step 9.05 -> 9.2 us, 64 sequences 36.7 -> 37.1).
-__device__ __forceinline__ float made_here(float c) {
-    asm("" : "+v"(c));
-    return c;
-}
-
 // Keeps loads after this point from being issued before it, and arithmetic on
 // the registers they go to from being moved behind it.
 __device__ __forceinline__ void in_order() {
