@@ -9,6 +9,10 @@ Names match the C entry points: ``cmc_select_cmes``, ``cmc_window_append``,
 ``cmc_two_tier_decode``, ``cmc_decode_step``, their ``*_ragged`` variants,
 the two workspace queries and ``cmc_window_start``.
 bf16 K/V tensors (torch.bfloat16) are passed through as their raw bits.
+
+``stream`` (a torch stream or a raw handle) takes the place of the current
+stream.  Outputs and workspaces that a call makes itself are then made on that
+stream too; tensors handed in have to be ready for it, as for any work there.
 """
 from __future__ import annotations
 
@@ -188,6 +192,20 @@ def _stream(stream) -> Optional[int]:
     return stream.cuda_stream
 
 
+def _make(stream, make, *args, **kw):
+    """make(*args, **kw), a tensor that a call on `stream` needs (an output or a
+    workspace), made in that stream's order: its memory is not still in use by
+    another stream's earlier work, a fill of it runs before the call's kernels, and
+    dropped at the call's end it serves only work behind them."""
+    if stream is None:
+        return make(*args, **kw)
+    torch = _torch or _load_torch()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    with torch.cuda.stream(stream):
+        return make(*args, **kw)
+
+
 def _kv_dtype(t) -> int:
     torch = _torch or _load_torch()
     d = t.dtype
@@ -219,15 +237,15 @@ def cmc_select_cmes(sel_keys, q_vec, k: int, idx_out=None, scores_out=None, work
     _need(q_vec.shape == (B, D) and q_vec.is_contiguous(), "q_vec must be contiguous [B][D]")
     _need(q_vec.dtype == torch.float32, "q_vec must be fp32")
     if idx_out is None:
-        idx_out = torch.empty((B, k), dtype=torch.int32, device=sel_keys.device)
+        idx_out = _make(stream, torch.empty, (B, k), dtype=torch.int32, device=sel_keys.device)
     _need(idx_out.shape == (B, k) and idx_out.dtype == torch.int32 and idx_out.is_contiguous(),
           "idx_out must be contiguous int32 [B][k]")
     if scores_out is not None:
         _need(scores_out.shape == (B, N) and scores_out.dtype == torch.float32, "scores_out [B][N] fp32")
     ws_bytes = 0
     if scores_out is None and workspace is None:
-        workspace = torch.empty(max(1, cmc_select_workspace_bytes(B, N)), dtype=torch.uint8,
-                                device=sel_keys.device)
+        workspace = _make(stream, torch.empty, max(1, cmc_select_workspace_bytes(B, N)), dtype=torch.uint8,
+                          device=sel_keys.device)
     if workspace is not None:
         ws_bytes = workspace.numel() * workspace.element_size()
     rc = lib().cmc_select_cmes(_ptr(sel_keys), _kv_dtype(sel_keys), _ptr(q_vec), B, N, D, int(k), _ptr(idx_out),
@@ -254,11 +272,11 @@ def cmc_select_cmes_ragged(sel_keys, q_vec, n_rows, k: int, q_rows=None, idx_str
     stride = int(k if idx_stride is None else idx_stride)
     dev = sel_keys.device
     if idx_out is None:
-        idx_out = torch.empty((B, stride), dtype=torch.int32, device=dev)
+        idx_out = _make(stream, torch.empty, (B, stride), dtype=torch.int32, device=dev)
     _need(idx_out.shape == (B, stride) and idx_out.dtype == torch.int32 and idx_out.is_contiguous(),
           "idx_out must be contiguous int32 [B][idx_stride]")
     if k_out is None:
-        k_out = torch.empty((B,), dtype=torch.int32, device=dev)
+        k_out = _make(stream, torch.empty, (B,), dtype=torch.int32, device=dev)
     _need(k_out.shape == (B,) and k_out.dtype == torch.int32, "k_out [B] int32")
     if scores_out is not None:
         _need(scores_out.shape == (B, N) and scores_out.dtype == torch.float32, "scores_out [B][N] fp32")
@@ -267,7 +285,7 @@ def cmc_select_cmes_ragged(sel_keys, q_vec, n_rows, k: int, q_rows=None, idx_str
               "norms_out [B][N] fp32")
     ws_bytes = 0
     if scores_out is None and workspace is None:
-        workspace = torch.empty(max(1, cmc_select_workspace_bytes(B, N)), dtype=torch.uint8, device=dev)
+        workspace = _make(stream, torch.empty, max(1, cmc_select_workspace_bytes(B, N)), dtype=torch.uint8, device=dev)
     if workspace is not None:
         ws_bytes = workspace.numel() * workspace.element_size()
     rc = lib().cmc_select_cmes_ragged(_ptr(sel_keys), _kv_dtype(sel_keys), _ptr(q_vec), _ptr(n_rows), _ptr(q_rows),
@@ -295,9 +313,9 @@ def cmc_locate_window(norms, ctx_len, W: int, mems_per_chunk: int, n_rows=None, 
               and chunk_offset.is_contiguous(), "chunk_offset [B][n_chunks] int32")
         n_chunks = int(chunk_offset.shape[1])
     if alpha_out is None:
-        alpha_out = torch.empty((B,), dtype=torch.int32, device=norms.device)
+        alpha_out = _make(stream, torch.empty, (B,), dtype=torch.int32, device=norms.device)
     if start_out is None:
-        start_out = torch.empty((B,), dtype=torch.int32, device=norms.device)
+        start_out = _make(stream, torch.empty, (B,), dtype=torch.int32, device=norms.device)
     _need(alpha_out.shape == (B,) and start_out.shape == (B,) and alpha_out.dtype == start_out.dtype == torch.int32,
           "alpha_out/start_out [B] int32")
     rc = lib().cmc_locate_window(_ptr(norms), _ptr(n_rows), _ptr(ctx_len), B, N, int(mems_per_chunk),
@@ -330,13 +348,14 @@ def cmc_memory_bridge(h, w1, b1, w2, b2, ln_gamma, ln_beta, nu: float, ln_eps: f
     for name, v, n in (("b1", b1, F), ("b2", b2, Hd), ("ln_gamma", ln_gamma, Hd), ("ln_beta", ln_beta, Hd)):
         _need(v.shape == (n,) and v.dtype == f32 and v.is_contiguous(), f"{name} [{n}] fp32")
     if out is None:
-        out = torch.empty((M, Hd), dtype=f32, device=h.device)
+        out = _make(stream, torch.empty, (M, Hd), dtype=f32, device=h.device)
     _need(out.shape == (M, Hd) and out.dtype == f32 and out.is_contiguous(), "out [M][Hd] fp32")
     if h_norms_out is not None:
         _need(h_norms_out.numel() == M and h_norms_out.dtype == f32 and h_norms_out.is_contiguous(),
               "h_norms_out [M] fp32")
     if workspace is None:
-        workspace = torch.empty(max(1, cmc_bridge_workspace_bytes(M, F)), dtype=torch.uint8, device=h.device)
+        workspace = _make(stream, torch.empty, max(1, cmc_bridge_workspace_bytes(M, F)), dtype=torch.uint8,
+                          device=h.device)
     ws_bytes = workspace.numel() * workspace.element_size()
     rc = lib().cmc_memory_bridge(_ptr(h), _ptr(w1), _ptr(b1), _ptr(w2), _ptr(b2), _ptr(ln_gamma), _ptr(ln_beta),
                                  float(nu), float(ln_eps), M, Hc, F, Hd, _ptr(out), _ptr(h_norms_out),
@@ -368,9 +387,9 @@ def cmc_denoise(emb, g: int = 3, tau: float = 0.05, keep_min_every: int = 16, n_
         _need(n_tokens.shape == (B,) and n_tokens.dtype == torch.int32 and n_tokens.is_contiguous(),
               "n_tokens [B] int32")
     if kept_idx is None:
-        kept_idx = torch.empty((B, n), dtype=torch.int32, device=dev)
+        kept_idx = _make(stream, torch.empty, (B, n), dtype=torch.int32, device=dev)
     if kept_count is None:
-        kept_count = torch.empty((B,), dtype=torch.int32, device=dev)
+        kept_count = _make(stream, torch.empty, (B,), dtype=torch.int32, device=dev)
     _need(kept_idx.shape == (B, n) and kept_idx.dtype == torch.int32, "kept_idx [B][n] int32")
     _need(kept_count.shape == (B,) and kept_count.dtype == torch.int32, "kept_count [B] int32")
     if max_cos_out is not None:
@@ -380,13 +399,13 @@ def cmc_denoise(emb, g: int = 3, tau: float = 0.05, keep_min_every: int = 16, n_
     nch = -(-n // chunk_tokens) if chunk_tokens > 0 else 0
     if chunk_tokens > 0:
         if chunk_offset is None:
-            chunk_offset = torch.empty((B, max(nch, 1)), dtype=torch.int32, device=dev)
+            chunk_offset = _make(stream, torch.empty, (B, max(nch, 1)), dtype=torch.int32, device=dev)
         if n_chunks_out is None:
-            n_chunks_out = torch.empty((B,), dtype=torch.int32, device=dev)
+            n_chunks_out = _make(stream, torch.empty, (B,), dtype=torch.int32, device=dev)
         _need(chunk_offset.dtype == torch.int32 and chunk_offset.shape[0] == B and chunk_offset.shape[1] >= nch,
               "chunk_offset [B][ceil(n/chunk_tokens)] int32")
     if workspace is None:
-        workspace = torch.empty(max(1, cmc_denoise_workspace_bytes(B, n)), dtype=torch.uint8, device=dev)
+        workspace = _make(stream, torch.empty, max(1, cmc_denoise_workspace_bytes(B, n)), dtype=torch.uint8, device=dev)
     ws_bytes = workspace.numel() * workspace.element_size()
     rc = lib().cmc_denoise(_ptr(emb), dtype, _ptr(n_tokens), B, n, H, int(g), float(tau), int(keep_min_every),
                            int(chunk_tokens), _ptr(max_cos_out), _ptr(keep_out), _ptr(kept_idx), _ptr(kept_count),
@@ -419,9 +438,9 @@ def cmc_gather_tier1(cme_k, cme_v, idx, k: int, k_len=None, out_k=None, out_v=No
     if k_len is not None:
         _need(k_len.shape == (B,) and k_len.dtype == torch.int32 and k_len.is_contiguous(), "k_len [B] int32")
     if out_k is None:
-        out_k = torch.empty((B, Hkv, k, Dh), dtype=cme_k.dtype, device=cme_k.device)
+        out_k = _make(stream, torch.empty, (B, Hkv, k, Dh), dtype=cme_k.dtype, device=cme_k.device)
     if out_v is None:
-        out_v = torch.empty((B, Hkv, k, Dh), dtype=cme_k.dtype, device=cme_k.device)
+        out_v = _make(stream, torch.empty, (B, Hkv, k, Dh), dtype=cme_k.dtype, device=cme_k.device)
     _need(out_k.shape == (B, Hkv, k, Dh) and out_v.shape == out_k.shape and out_k.dtype == out_v.dtype == cme_k.dtype,
           "out_k/v [B][Hkv][k][Dh]")
     rc = lib().cmc_gather_tier1(_ptr(cme_k), _ptr(cme_v), _kv_dtype(cme_k), _ptr(idx), _ptr(k_len), stride, B, Hkv,
@@ -467,7 +486,7 @@ def decode_workspace(B: int, Hq: int, Hkv: int, Dh: int, k: int, W: int, device)
 
 
 def _decode_args(q, cme_k, cme_v, idx, k, win_k, win_v, win_count, new_k, new_v, out, workspace, W, k_len,
-                 noalloc=False):
+                 stream, noalloc=False):
     """Checks shared by the decode wrappers; returns the C call's sizes and
     the (possibly allocated) out and workspace (none with noalloc)."""
     torch = _torch or _load_torch()
@@ -511,13 +530,13 @@ def _decode_args(q, cme_k, cme_v, idx, k, win_k, win_v, win_count, new_k, new_v,
     if k_len is not None and not (k_len.shape == (B,) and k_len.dtype is i32 and k_len.is_contiguous()):
         raise ValueError("k_len [B] int32")
     if out is None:
-        out = torch.empty((B, Hq, Dh), dtype=f32, device=q.device)
+        out = _make(stream, torch.empty, (B, Hq, Dh), dtype=f32, device=q.device)
     elif not (out.shape == qs and out.dtype is f32 and out.is_contiguous()):
         raise ValueError("out [B][Hq][Dh] fp32")
     ws_bytes = 0
     if not noalloc:
         if workspace is None:
-            workspace = decode_workspace(B, Hq, Hkv, Dh, k, W, q.device)
+            workspace = _make(stream, decode_workspace, B, Hq, Hkv, Dh, k, W, q.device)
         ws_bytes = workspace.numel() * workspace.element_size()
     if W > 0:
         wk, wv, wc = _ptr(win_k), _ptr(win_v), _ptr(win_count)
@@ -532,7 +551,8 @@ def cmc_two_tier_decode(q, cme_k, cme_v, idx, k: int, win_k, win_v, win_count, s
     """One decode step over [pool rows idx || ring slots].  q [B][Hq][Dh] fp32,
     cme_* [B][Hkv][N][Dh], idx [B][k] int32 or None, win_* [B][Hkv][W][Dh] or
     None (W = 0), win_count [B] int32.  Returns out [B][Hq][Dh] fp32."""
-    a = _decode_args(q, cme_k, cme_v, idx, k, win_k, win_v, win_count, None, None, out, workspace, W, None)
+    a = _decode_args(q, cme_k, cme_v, idx, k, win_k, win_v, win_count, None, None, out, workspace, W, None,
+                     stream)
     rc = lib().cmc_two_tier_decode(_ptr(q), _ptr(cme_k), _ptr(cme_v), _ptr(idx), int(k), *a["win"], a["W"],
                                    a["dtype"], a["B"], a["Hq"], a["Hkv"], a["Dh"], a["N"], float(scale),
                                    _ptr(a["out"]), _ptr(a["workspace"]), a["ws_bytes"], _stream(stream))
@@ -545,7 +565,8 @@ def cmc_decode_step(q, cme_k, cme_v, idx, k: int, win_k, win_v, win_count, new_k
     """Ring append of new_k/new_v [B][Hkv][T][Dh] followed by the two-tier
     decode, in one launch.  Same arguments as cmc_two_tier_decode plus the
     new rows.  Returns out [B][Hq][Dh] fp32."""
-    a = _decode_args(q, cme_k, cme_v, idx, k, win_k, win_v, win_count, new_k, new_v, out, workspace, W, None)
+    a = _decode_args(q, cme_k, cme_v, idx, k, win_k, win_v, win_count, new_k, new_v, out, workspace, W, None,
+                     stream)
     rc = lib().cmc_decode_step(_ptr(q), _ptr(cme_k), _ptr(cme_v), _ptr(idx), int(k), *a["win"], a["W"],
                                *a["new"], a["T"], a["dtype"], a["B"], a["Hq"], a["Hkv"], a["Dh"], a["N"],
                                float(scale), _ptr(a["out"]), _ptr(a["workspace"]), a["ws_bytes"], _stream(stream))
@@ -557,7 +578,8 @@ def cmc_two_tier_decode_ragged(q, cme_k, cme_v, idx, k_len, k: int, win_k, win_v
                                out=None, workspace=None, W: Optional[int] = None, stream=None):
     """cmc_two_tier_decode with per-sequence pool-row counts k_len [B] int32
     (device); k is the row stride of idx."""
-    a = _decode_args(q, cme_k, cme_v, idx, k, win_k, win_v, win_count, None, None, out, workspace, W, k_len)
+    a = _decode_args(q, cme_k, cme_v, idx, k, win_k, win_v, win_count, None, None, out, workspace, W, k_len,
+                     stream)
     rc = lib().cmc_two_tier_decode_ragged(_ptr(q), _ptr(cme_k), _ptr(cme_v), _ptr(idx), _ptr(k_len), int(k),
                                           *a["win"], a["W"], a["dtype"], a["B"], a["Hq"], a["Hkv"], a["Dh"],
                                           a["N"], float(scale), _ptr(a["out"]), _ptr(a["workspace"]),
@@ -569,7 +591,8 @@ def cmc_two_tier_decode_ragged(q, cme_k, cme_v, idx, k_len, k: int, win_k, win_v
 def cmc_decode_step_ragged(q, cme_k, cme_v, idx, k_len, k: int, win_k, win_v, win_count, new_k, new_v,
                            scale: float, out=None, workspace=None, W: Optional[int] = None, stream=None):
     """cmc_decode_step with per-sequence pool-row counts k_len [B] int32."""
-    a = _decode_args(q, cme_k, cme_v, idx, k, win_k, win_v, win_count, new_k, new_v, out, workspace, W, k_len)
+    a = _decode_args(q, cme_k, cme_v, idx, k, win_k, win_v, win_count, new_k, new_v, out, workspace, W, k_len,
+                     stream)
     rc = lib().cmc_decode_step_ragged(_ptr(q), _ptr(cme_k), _ptr(cme_v), _ptr(idx), _ptr(k_len), int(k),
                                       *a["win"], a["W"], *a["new"], a["T"], a["dtype"], a["B"], a["Hq"], a["Hkv"],
                                       a["Dh"], a["N"], float(scale), _ptr(a["out"]), _ptr(a["workspace"]),
@@ -584,7 +607,7 @@ def cmc_decode_step_noalloc(q, cme_k, cme_v, idx, k: int, win_k, win_v, win_coun
     the counters and split partials (no device allocation in the call; `out`
     must then be passed by callers that cannot allocate)."""
     a = _decode_args(q, cme_k, cme_v, idx, k, win_k, win_v, win_count, new_k, new_v, out, None, W, None,
-                     noalloc=True)
+                     stream, noalloc=True)
     rc = lib().cmc_decode_step_noalloc(_ptr(q), _ptr(cme_k), _ptr(cme_v), _ptr(idx), int(k), *a["win"], a["W"],
                                        *a["new"], a["T"], a["dtype"], a["B"], a["Hq"], a["Hkv"], a["Dh"], a["N"],
                                        float(scale), _ptr(a["out"]), _stream(stream))
@@ -670,13 +693,13 @@ def cmc_gather_tier1_q8(cme_k, cme_v, idx, k: int, block: int, k_len=None, dtype
     if k_len is not None and not (k_len.shape == (B,) and k_len.dtype is torch.int32 and k_len.is_contiguous()):
         raise ValueError("k_len [B] int32")
     if out_k is None:
-        out_k = torch.empty((B, Hkv, k, Dh), dtype=dtype or torch.float8_e4m3fn, device=cme_k.device)
+        out_k = _make(stream, torch.empty, (B, Hkv, k, Dh), dtype=dtype or torch.float8_e4m3fn, device=cme_k.device)
     if out_v is None:
-        out_v = torch.empty_like(out_k)
+        out_v = _make(stream, torch.empty_like, out_k)
     if out_ks is None:
-        out_ks = torch.empty((B, Hkv, -(-k // block)), dtype=torch.float32, device=cme_k.device)
+        out_ks = _make(stream, torch.empty, (B, Hkv, -(-k // block)), dtype=torch.float32, device=cme_k.device)
     if out_vs is None:
-        out_vs = torch.empty_like(out_ks)
+        out_vs = _make(stream, torch.empty_like, out_ks)
     if _cache_args("out", out_k, out_v, out_ks, out_vs, block) != (B, Hkv, k, Dh):
         raise ValueError("out_k/v [B][Hkv][k][Dh]")
     dev = _device_index()
@@ -741,9 +764,9 @@ def cmc_cache_read_q8(k8, v8, ks, vs, block: int, count=None, dtype=None, out_k=
     if count is not None and not (count.shape == (B,) and count.dtype is torch.int32 and count.is_contiguous()):
         raise ValueError("count [B] int32")
     if out_k is None:
-        out_k = torch.empty(s, dtype=dtype or torch.bfloat16, device=k8.device)
+        out_k = _make(stream, torch.empty, s, dtype=dtype or torch.bfloat16, device=k8.device)
     if out_v is None:
-        out_v = torch.empty_like(out_k)
+        out_v = _make(stream, torch.empty_like, out_k)
     if not (out_k.shape == s and out_v.shape == s and out_v.dtype is out_k.dtype and out_k.is_contiguous()
             and out_v.is_contiguous()):
         raise ValueError("out_k/v [B][Hkv][R][Dh]")
@@ -801,11 +824,11 @@ def _decode_q8(step, q, cme_k, cme_v, cme_ks, cme_vs, k, win_k, win_v, win_ks, w
     if k_len is not None and not (k_len.shape == (B,) and k_len.dtype is i32 and k_len.is_contiguous()):
         raise ValueError("k_len [B] int32")
     if out is None:
-        out = torch.empty(qs, dtype=f32, device=q.device)
+        out = _make(stream, torch.empty, qs, dtype=f32, device=q.device)
     elif not (out.shape == qs and out.dtype is f32 and out.is_contiguous()):
         raise ValueError("out [B][Hq][Dh] fp32")
     if workspace is None:
-        workspace = decode_workspace_q8(B, Hq, Hkv, Dh, k, W, q.device)
+        workspace = _make(stream, decode_workspace_q8, B, Hq, Hkv, Dh, k, W, q.device)
     elif not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
     scale = float(scale)
