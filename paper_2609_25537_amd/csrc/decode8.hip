@@ -45,7 +45,7 @@
 // sequence of 32808 keys in a graph 18.1 / 19.3 us); with the rows' addresses clamped and V
 // widened before its rows are paired they were 221 and 317, and times 1 to 2%
 // longer.  The matrix units are busy for less than 10% of the time.
-#include <stddef.h>
+#include <type_traits>
 
 #include "cache8.hpp"
 #include "decode_common.hpp"
@@ -317,19 +317,26 @@ struct Walk8 {
 template <int DH>
 constexpr int kMinWaves8 = 2;
 
-// The kernel's parameters, loaded here and not before (the compiler would
-// load them at the kernel's start and wait for them there).
+// decode8_kernel's parameter list as it lies in the kernarg segment: each where its
+// alignment puts it, as in a struct.
 struct Args8 {
     const void *cme_k, *cme_v;
     void *win_k, *win_v;
     int k, W, N, Hkv, chunk, info;
     Decode8Params p;
 };
+typedef void (*Kernel8)(const void *, const void *, void *, void *, int, int, int, int, int, int, Decode8Params);
+static_assert(sizeof(Args8) == 4 * sizeof(void *) + 6 * sizeof(int) + sizeof(Decode8Params) &&
+                  std::is_trivially_copyable_v<Decode8Params>,
+              "Args8 holds Kernel8's parameters, in its order and without gaps");
+
+// The last parameter, loaded here and not before (the compiler would load it at
+// the kernel's start and wait for it there); fields that nothing uses are not.
 __device__ __forceinline__ Decode8Params late_params() {
     typedef const __attribute__((address_space(4))) Args8 *Ptr;
     Ptr at = (Ptr)__builtin_amdgcn_kernarg_segment_ptr();
     asm volatile("" : "+s"(at));
-    Decode8Params p{};
+    Decode8Params p;
     p.q = at->p.q;
     p.cme_ks = at->p.cme_ks;
     p.cme_vs = at->p.cme_vs;
@@ -349,6 +356,22 @@ __device__ __forceinline__ Decode8Params late_params() {
     p.pool_blocks = at->p.pool_blocks;
     p.ring_blocks = at->p.ring_blocks;
     p.log2_block = at->p.log2_block;
+    p.cme_k = at->p.cme_k;
+    p.cme_v = at->p.cme_v;
+    p.idx = at->p.idx;
+    p.k_len = at->p.k_len;
+    p.win_k = at->p.win_k;
+    p.win_v = at->p.win_v;
+    p.k = at->p.k;
+    p.W = at->p.W;
+    p.B = at->p.B;
+    p.Hkv = at->p.Hkv;
+    p.N = at->p.N;
+    p.T_new = at->p.T_new;
+    p.S = at->p.S;
+    p.chunk = at->p.chunk;
+    p.new_split = at->p.new_split;
+    p.waves = at->p.waves;
     return p;
 }
 
@@ -599,6 +622,7 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves8<DH>)) void decode8_kernel(c
 template <class F, int DH, int G>
 hipError_t launch3(const Decode8Params &p, hipStream_t stream) {
     const dim3 grid(p.S, p.Hkv, p.B);
+    static_assert(std::is_same_v<decltype(&decode8_kernel<4, F, DH, G>), Kernel8>, "Args8 is taken from the kernel's list");
     if (p.S < 1 || p.S > 0xFF || p.T_new < 0 || p.T_new > kFusedRows8 || (p.waves != 4 && p.waves != 8)) return hipErrorInvalidValue;
     const int info = p.S | (p.new_split << 8) | ((p.k_len != nullptr) << 10) | (p.T_new << 16);
 #define CMC_LAUNCH(NW_)                                                                                          \
