@@ -39,7 +39,9 @@ if ROOT not in sys.path:
 
 HBM_PEAK_GBS = 8000.0
 LLC_BYTES = 256 << 20  # MI355X last-level (Infinity) cache
-DECODE_SOURCES = ["paper_2609_25537_amd/csrc/decode.hip", "paper_2609_25537_amd/csrc/device_common.hpp"]
+# The decode kernel's code: decode.hip and what it includes, but for kernels.hpp (parameter lists of every kernel).
+DECODE_SOURCES = ["paper_2609_25537_amd/csrc/" + f for f in
+                  ("decode.hip", "decode_common.hpp", "decode_finish.hpp", "decode_merge.hpp", "device_common.hpp")]
 TRAFFIC_FILE = os.path.join(ROOT, "profiles", "decode_traffic.json")
 
 

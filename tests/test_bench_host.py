@@ -6,6 +6,7 @@ import argparse
 import csv
 import json
 import os
+import re
 import subprocess
 import sys
 
@@ -127,6 +128,22 @@ def test_kernel_hash_ignores_comments():
     same = "int a; // another note\n\n/* a different\nblock */ int b;\n"
     assert bench._strip_comments(src) == bench._strip_comments(same)
     assert bench._strip_comments(src) != bench._strip_comments("int a; // note\n/* block\ncomment */ int c;\n")
+
+
+def test_kernel_hash_covers_what_the_kernel_includes():
+    """Every file of the decode kernel's text is in its hash, however the text
+    is cut into files (kernels.hpp holds the parameter lists of all kernels)."""
+    csrc = os.path.join(ROOT, "paper_2609_25537_amd", "csrc")
+    todo, seen = ["decode.hip"], set()
+    while todo:
+        name = todo.pop()
+        if name in seen or name == "kernels.hpp":
+            continue
+        seen.add(name)
+        with open(os.path.join(csrc, name)) as f:
+            todo += re.findall(r'^\s*#include "(\w+\.hpp)"', f.read(), flags=re.M)
+    assert len(seen) > 2
+    assert sorted(bench.DECODE_SOURCES) == sorted(f"paper_2609_25537_amd/csrc/{n}" for n in seen)
 
 
 def test_more_than_one_gpu_is_refused():
