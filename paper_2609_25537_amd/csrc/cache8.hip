@@ -243,11 +243,11 @@ int touched_most(int T, int blocks, int log2_block) {
 
 // Every workgroup of write_blocks_kernel reads the counts, so a launch of its own
 // raises them.  One row of a small block goes by append_row_kernel, which does
-// both.  Called from the host, 64 sequences of 8 heads of 128 take 6.7 us against
-// 9.7; in a graph one sequence takes 3.9 against 4.9, 8 take 5.0 against 5.3, 256
-// 8.8 against 9.0, and only about 64 lose (7.1 against 5.8).  Past a word in
-// each of four registers and a wave for every head, rounds add up: 8 sequences of 16
-// heads in blocks of 64 took 11.5 us in two rounds against 5.8.
+// both: for 1 / 8 / 64 / 256 sequences of 8 heads of 128 in a graph 4.1 / 4.7 / 5.3 /
+// 6.6 us against 5.1 / 5.2 / 5.8 / 9.1 (the one that lost of those measured: the append
+// case of perf/operators.py, 64 sequences, 6.1 against 5.9), called from the host 7.6
+// against 10.6 at every size.  Past a word in each of four registers and a wave for every head, rounds add up:
+// 8 sequences of 16 heads in blocks of 64 took 11.5 us in two rounds against 5.8.
 template <typename T, class F>
 hipError_t launch_append(const Write8Params &p, hipStream_t stream) {
     const int most = touched_most(p.T_new, p.blocks, p.log2_block);

@@ -28,8 +28,8 @@ typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
 typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 
-// A constant loaded where it is used, on a rare path: the walk's loop fills the scalar
-// registers, and with one more constant kept in them its pointers were spilled
+// A constant loaded where it is used, on a rare path: the decode's loop fills the
+// scalar registers, and with one more constant kept in them its pointers were spilled
 // (batch-1 step 9.05 -> 9.2 us, 64 sequences 36.7 -> 37.1).
 __device__ __forceinline__ float made_here(float c) {
     asm("" : "+v"(c));

@@ -174,8 +174,9 @@ DecodePlan plan_decode(int B, int Hq, int Hkv, int Dh, int k, int W, int T_new) 
 
 // Split plan of the decode over the 8-bit cache, in units of kUnit8 rows; times in
 // us of a launch that appends a row, G = 4, Dh = 128 unless said otherwise.
-// Two 4-wave workgroups or one of 8 waves are resident per CU, so 512 (256) fill
-// the chip.
+// Two 4-wave workgroups (three at Dh = 64) or one of 8 waves are resident per CU, so
+// 512 (256) are taken to fill the chip.  Where no Dh is named, both sides of a bound
+// were measured at 128 and the other head sizes follow it.
 //   - Up to 64 (sequence, kv head) pairs: 256 workgroups at most, one of each
 //     pair's for the block that is appended to, and no more splits than about
 //     the root of the units, since the last split to arrive reads all of their

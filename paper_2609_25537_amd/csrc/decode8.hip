@@ -29,8 +29,10 @@
 //
 // The maximum is moved only when a score passes it by more than 2 (p <= 4),
 // which after the first units is rare; that test needs no exchange between
-// lanes.  The next unit's K is requested when this unit's scores are done,
-// its V when this unit's P V is.
+// lanes.  Maxima of 2^22 and more, where fp32 no longer resolves that, move with every
+// unit and have their weights' arguments subtracted first.  The next unit's K is
+// requested when this unit's scores are done, its V (and its scale before it, which
+// the widening of V takes) when this unit's P V is.
 //
 // Fused append: the last split (one of its own where the plan says so) brings
 // the ring blocks that the appended rows touch up to date (append_block), then
@@ -41,10 +43,10 @@
 // 256 (403 MB) 62 us, 6.4 TB/s; 64 of 8 heads of 128, 1536 keys and an append
 // (204 MB) 35.5 us, 5.7 TB/s.  Below that by the chain of one workgroup: 9 us
 // with 1.6 MB to read (8 pairs), of which the append 1.5.  Vector operations per
-// unit of Dh = 128: 185 for e4m3, 281 for int8, which is up to 7% slower (one
-// sequence of 32808 keys in a graph 18.1 / 19.3 us); with the rows' addresses clamped and V
-// widened before its rows are paired they were 221 and 317, and times 1 to 2%
-// longer.  The matrix units are busy for less than 10% of the time.
+// unit of Dh = 128: 188 for e4m3, 279 for int8, which is up to 7% slower (24 sequences
+// of 8 heads and 1549 keys in a graph 21.1 / 22.6 us, one sequence of 32808 keys 18.3 /
+// 18.8); with the rows' addresses clamped and V widened before its rows are paired
+// they were 221 and 317, and times 1 to 2% longer.  The matrix units are busy for less than 10% of the time.
 #include <type_traits>
 
 #include "cache8.hpp"
