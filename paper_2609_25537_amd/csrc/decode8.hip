@@ -97,7 +97,8 @@ struct Walk8 {
     } un[NS];
     float4 qx[4 * SL];        // q as loaded
     halfx8 q[2 * SL];
-    float qf;                 // scale log2(e) over q's power of two
+    float qm;                 // scale log2(e) over q's power of two: qm 2^qe
+    int qe;
     float m;                  // of head (lane % 16) % G
     float limit;              // the largest score that m may stay for
     floatx4 l, acc[D];        // rows 4 (lane / 16) + i: heads, hi and lo
@@ -182,7 +183,11 @@ struct Walk8 {
         // times 2^(up - 127): up <= 253 keeps the inverse normal
         const int up = min(127 + 14 + 127 - (int)(top >> 23), 253);
         const float mul = copysignf(__uint_as_float((uint32_t)up << 23), p.qscale);
-        qf = fabsf(p.qscale) * __uint_as_float((uint32_t)(254 - up) << 23);
+        // Apart: the product of a small scale and a small q's power may be subnormal,
+        // and the K scale it meets large.
+        const float qs = made_here(p.qscale);
+        qm = __builtin_amdgcn_frexp_mantf(fabsf(qs));
+        qe = __builtin_amdgcn_frexp_expf(qs) + 127 - up;
         const float part = r16 >= 8 ? 1.f : 0.f;
 #pragma unroll
         for (int i = 0; i < 2 * SL; ++i) {
@@ -194,6 +199,9 @@ struct Walk8 {
             }
         }
     }
+
+    // s_K over q's power of two.
+    __device__ __forceinline__ float factor(int set) const { return ldexpf(un[set].ks * qm, qe); }
 
     __device__ __forceinline__ static halfx8 half8(uint32_t a, uint32_t b) {
         uint32_t w[4];
@@ -521,7 +529,7 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves8<DH>)) void decode8_kernel(c
 #pragma unroll
             for (int i = 0; i < NS; ++i) {
                 floatx4 c[2];
-                float f = st.un[i].ks * st.qf;
+                float f = st.factor(i);
                 asm volatile("" : "+v"(f));  // taken here: the scale's register is the next load's
                 st.scores(i, c);
                 const bool more = u < end;
@@ -544,7 +552,7 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves8<DH>)) void decode8_kernel(c
             if (n[i] > 0) {
                 floatx4 c[2];
                 st.scores(i, c);
-                st.add(i, c, st.un[i].ks * st.qf, n[i]);
+                st.add(i, c, st.factor(i), n[i]);
             }
         }
     }
@@ -585,7 +593,7 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves8<DH>)) void decode8_kernel(c
             st.un[0].vs = scale_v(at);
             floatx4 c[2];
             st.scores(0, c);
-            st.add(0, c, st.un[0].ks * st.qf, at.n);
+            st.add(0, c, st.factor(0), at.n);
         }
     }
     cnt.load(W > 0 ? p.win_count : nullptr, b);  // a wave without rows

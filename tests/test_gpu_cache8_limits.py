@@ -9,6 +9,7 @@ import torch
 from paper_2609_25537_amd import cmc
 from tests import q8_ref
 from tests.gpu_util import DEV, say
+from tests.test_gpu_cache8_plans import Case
 
 pytestmark = pytest.mark.gpu
 
@@ -242,3 +243,32 @@ def test_read_back_of_the_longest_cache(R):
     assert (out[0, 0, R - 1] == 5).all() and (out[0, 0, R - 2] == 3.5).all() and (out[0, 0, 0] == 0).all()
     del k8, out
     torch.cuda.empty_cache()
+
+
+# ---------------------------------------------------------------- products
+
+@pytest.mark.parametrize("code", ["e4m3", "i8"])
+@pytest.mark.parametrize("Dh,G", SHAPES)
+def test_powers_of_two_between_q_k_and_scale(code, Dh, G):
+    """K's scales times 2^a, q times 2^b and scale times 2^-(a + b) leave the scores
+    as they are: the same bits out, however small or large each of them is.  (A q
+    below 2^-111 is held with other parts: within the bound.)"""
+    c = Case(2, 2, G, Dh, 333, 150, code, 32, seed=Dh, counts=[150, 70])
+    q = c.q()
+    run = lambda q: cmc.cmc_two_tier_decode_q8(q, *c.pool, c.k, *c.win, c.count, c.scale, c.block, workspace=c.ws)
+    want = run(q)
+    c.check(q, want, c.win, c.count)
+    ks = [t.clone() for t in (c.pool[2], c.win[2])]
+    base = c.scale
+    for a, b in ((126, -100), (120, -100), (100, -60), (126, -20), (-110, 100), (-110, -10), (100, 0), (60, 40), (-60, -60),
+                 (126, -118), (110, -124)):
+        say("powers", code, Dh, G, a, b)
+        for t, s in zip((c.pool[2], c.win[2]), ks):
+            t.copy_(s * 2.0 ** a)
+        c.scale = base * 2.0 ** -(a + b)
+        qb = q * 2.0 ** b
+        out = run(qb)
+        if b >= -104:
+            assert torch.equal(out, want), (a, b, float((out - want).abs().max()))
+        else:
+            c.check(qb, out, c.win, c.count)
