@@ -574,9 +574,10 @@ size_t cmc_decode_q8_workspace_bytes(int B, int Hq, int Hkv, int Dh, int k, int 
  * A head with an empty key list gets zeros; one that attends to a NaN, or whose
  * q is not finite, gets NaN, and no other head does.
  * Limits: Hq / Hkv in {1, 2, 4, 8}, 0 <= k <= N, k + W >= 1.  Within fp32's range:
- * 4 (k + W) times the largest value of V; and 2 Dh |scale| times the largest
- * elements of a head's q and of its K, so that its scores are (past that the head may
- * hold zeros or NaN).  A scale below 2^-126 keeps only the bits that fp32 has for it.
+ * 2 |scale|; 4 (k + W) times the largest value of V; and 2 Dh |scale| times the
+ * largest elements of a head's q and of its K, so that its scores are (past that the
+ * head may hold zeros or NaN).  A scale below 2^-126 keeps only the bits that fp32 has
+ * for it.
  * Arithmetic: q and the softmax weights enter the products with 22 bits (two
  * fp16 parts), the codes as they are, fp32 sums in a fixed order (run-to-run
  * bit-identical); weights below 2^-16 of the largest keep fewer bits, to 2^-38 of
