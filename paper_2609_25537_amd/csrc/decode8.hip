@@ -43,7 +43,7 @@
 // 256 (403 MB) 62 us, 6.4 TB/s; 64 of 8 heads of 128, 1536 keys and an append
 // (204 MB) 35.5 us, 5.7 TB/s.  Below that by the chain of one workgroup: 9 us
 // with 1.6 MB to read (8 pairs), of which the append 1.5.  Vector operations per
-// unit of Dh = 128: 188 for e4m3, 279 for int8, which is up to 7% slower (24 sequences
+// unit of Dh = 128: 189 for e4m3, 280 for int8, which is up to 7% slower (24 sequences
 // of 8 heads and 1549 keys in a graph 21.1 / 22.6 us, one sequence of 32808 keys 18.3 /
 // 18.8); with the rows' addresses clamped and V widened before its rows are paired
 // they were 221 and 317, and times 1 to 2% longer.  The matrix units are busy for less than 10% of the time.
