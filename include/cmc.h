@@ -19,6 +19,9 @@
  *   *_ragged             the same with per-sequence sizes (ragged batches)
  *   *_q8                 the gather, append and decode on a cache of 8-bit codes,
  *                        and cmc_cache_read_q8, which reads such a cache back
+ *   *_q4                 the same on a cache of 4-bit codes
+ *   cmc_norm_rope        a projection's heads normed, rotated by position and laid out
+ *                        for the append and the decode (every step)
  *   cmc_locate_window    CME-guided Tier-2 window placement (once per question)
  *   cmc_denoise          graph-based context denoising before compression
  *                        (Sec. 2.1, once per context)
@@ -608,6 +611,173 @@ cmc_status cmc_decode_step_q8(const float *q, const void *cme_k, const void *cme
                               cmc_dtype code, int block,
                               int B, int Hq, int Hkv, int Dh, int N, float scale, float *out,
                               void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------ */
+/* 4-bit cache.                                                             */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * The two-tier cache in 4 bits: 17/64 of the bytes of bf16 per decode step.  A K or
+ * V array of R rows is held as
+ *   codes   [B][Hkv][R][Dh / 2]   uint8: e2m1 codes, dim 2i in the low half of byte
+ *                                 i, dim 2i + 1 in the high half; a code's sign bit,
+ *                                 two exponent bits and one fraction bit stand for
+ *                                 +-{0, 0.5, 1, 1.5, 2, 3, 4, 6}
+ *   scales  [B][Hkv][R][Dh / 32]  uint8: one for 32 dims of a row, byte s for
+ *                                 2^(s - 127) (e8m0), 255 for NaN
+ * and an element's value is code * scale.  With a the largest finite magnitude of the
+ * 32 elements, the library writes
+ *   s = the least byte >= 1 with a <= 6 * 2^(s - 127)
+ *   code = x / 2^(s - 127) rounded to nearest even (error at most 1/4 of the scale
+ *          where the value is below 2 scales, 1/2 below 4, 1 up to 6)
+ * with infinities stored as +-6 scales (elements of 7/8 of 2^128 and more round to 2^128, which reads
+ * back as infinity and is past the decode's limits); a NaN makes its 32 dims NaN (s = 255, codes
+ * 0).  Rows do not depend on each other, so appends leave the others as they are, and
+ * rows appended in one call or in several come out the same.  The decode and the
+ * read-back take any codes and scales, e.g. of a cache made elsewhere.
+ *
+ * Common limits: Hkv >= 1, B and Hkv <= 65535, Dh in {64, 128, 256}, at most 2^26
+ * rows an array, else CMC_ERR_UNSUPPORTED.
+ */
+
+/*
+ * cmc_gather_tier1 into a 4-bit block.
+ *
+ *   cme_k/v, kv_dtype, idx, k_len, idx_stride: as cmc_gather_tier1 (fp32 or bf16)
+ *   out_k/v    [B][Hkv][k][Dh / 2] codes; out_ks/vs [B][Hkv][k][Dh / 32]
+ *
+ * Rows j >= k_b are left as they were.
+ */
+cmc_status cmc_gather_tier1_q4(const void *cme_k, const void *cme_v, cmc_dtype kv_dtype,
+                               const int32_t *idx, const int32_t *k_len, int idx_stride,
+                               int B, int Hkv, int N, int k, int Dh,
+                               uint8_t *out_k, uint8_t *out_v, uint8_t *out_ks, uint8_t *out_vs,
+                               void *stream);
+
+/*
+ * cmc_window_append on a 4-bit ring (win_k/v [B][Hkv][W][Dh / 2] codes, win_ks/vs
+ * [B][Hkv][W][Dh / 32]): new_k/v [B][Hkv][T_new][Dh] in new_dtype (fp32 or bf16), row
+ * t to slot (count_b + t) mod W, then count_b += T_new.
+ *
+ * Limits: 1 <= T_new <= W, count_b >= 0 and count_b + T_new < 2^31.  W == 0 is a
+ * no-op.
+ */
+cmc_status cmc_window_append_q4(uint8_t *win_k, uint8_t *win_v, uint8_t *win_ks, uint8_t *win_vs,
+                                int32_t *win_count, const void *new_k, const void *new_v,
+                                cmc_dtype new_dtype, int B, int Hkv, int W, int Dh, int T_new,
+                                void *stream);
+
+/*
+ * Reads the newest rows of a 4-bit cache back, in the order they were written: with
+ * n = min(count_b, R) rows held and m = min(n, rows), out[b][h][r] for r < m is the
+ * value of the row written m - r rows before the end, which lies at slot
+ * (count_b - m + r) mod R.  A Tier-1 block's count is at most R, and its rows come as
+ * they stand.
+ *
+ *   k4, v4     [B][Hkv][R][Dh / 2] codes; ks, vs [B][Hkv][R][Dh / 32]
+ *   count      [B] int32: win_count, or the k_len of a Tier-1 block; NULL: R
+ *   out_k/v    [B][Hkv][rows][Dh] fp32 or bf16, both exact (past 2^128 infinity);
+ *              rows r >= m are left as they were
+ *
+ * Limits: 0 <= rows <= R.
+ */
+cmc_status cmc_cache_read_q4(const uint8_t *k4, const uint8_t *v4, const uint8_t *ks, const uint8_t *vs,
+                             const int32_t *count, int B, int Hkv, int R, int rows, int Dh,
+                             cmc_dtype out_dtype, void *out_k, void *out_v, void *stream);
+
+/* Bytes of workspace cmc_two_tier_decode_q4 and cmc_decode_step_q4 need; 0 for
+ * invalid sizes.  To be zero-filled before its first use and kept as
+ * cmc_decode_workspace_bytes says. */
+size_t cmc_decode_q4_workspace_bytes(int B, int Hq, int Hkv, int Dh, int k, int W);
+
+/*
+ * cmc_two_tier_decode on the 4-bit cache: softmax(scale q K^T) V over Tier-1 rows
+ * 0 .. k_b - 1 and the valid ring slots.
+ *
+ *   cme_k/v    [B][Hkv][N][Dh / 2] codes; cme_ks/vs [B][Hkv][N][Dh / 32]
+ *              (cmc_gather_tier1_q4's output; there is no index list)
+ *   k_len      [B] int32 (device): k_b = k_len[b] clamped into [0, k], or NULL for
+ *              all k
+ *   win_*      the ring as cmc_window_append_q4 keeps it
+ *   q, win_count, scale, out, workspace: as cmc_two_tier_decode, the workspace of
+ *              cmc_decode_q4_workspace_bytes
+ *
+ * Rows and slots that are not attended may hold anything.  A head with an empty key
+ * list gets zeros; one that attends to a NaN, or whose q is not finite, gets NaN, and
+ * no other head does.
+ * Limits: Hq / Hkv in {1, 2, 4, 8}, 0 <= k <= N, k + W >= 1.  Within fp32's range:
+ * 2 |scale|; 4 (k + W) times the largest value of V; and 2 Dh |scale| times the
+ * largest elements of a head's q and of its K, so that its scores are (past that the
+ * head may hold zeros or NaN).
+ * Arithmetic: q and the softmax weights enter the products with fp32's 24 bits
+ * (three bf16 parts), the cache's values as they are, fp32 sums in a fixed order
+ * (run-to-run bit-identical).
+ */
+cmc_status cmc_two_tier_decode_q4(const float *q, const uint8_t *cme_k, const uint8_t *cme_v,
+                                  const uint8_t *cme_ks, const uint8_t *cme_vs,
+                                  const int32_t *k_len, int k,
+                                  const uint8_t *win_k, const uint8_t *win_v,
+                                  const uint8_t *win_ks, const uint8_t *win_vs,
+                                  const int32_t *win_count, int W,
+                                  int B, int Hq, int Hkv, int Dh, int N, float scale, float *out,
+                                  void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * One decode step: cmc_window_append_q4, then cmc_two_tier_decode_q4 over the
+ * updated cache; in a single launch for up to 16 rows.  The ring's codes, scales and
+ * counts are those of the two calls; out is the same attention over the same keys, up
+ * to the order of the sums.  With W == 0 there is no Tier-2 and the new rows are
+ * ignored.
+ */
+cmc_status cmc_decode_step_q4(const float *q, const uint8_t *cme_k, const uint8_t *cme_v,
+                              const uint8_t *cme_ks, const uint8_t *cme_vs,
+                              const int32_t *k_len, int k,
+                              uint8_t *win_k, uint8_t *win_v, uint8_t *win_ks, uint8_t *win_vs,
+                              int32_t *win_count, int W,
+                              const void *new_k, const void *new_v, int T_new, cmc_dtype new_dtype,
+                              int B, int Hq, int Hkv, int Dh, int N, float scale, float *out,
+                              void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------ */
+/* Norms of heads and their rotation by position.                           */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * What a decoder does to a projection's heads before they are attended or cached, in
+ * one pass: the root-mean-square norm of each query and key head (where the model has
+ * one) and the rotation by position, with the results laid out as the calls above take
+ * them.  For a head x of Dh dims at position pos
+ *   y  = x / sqrt(mean(x^2) + eps) * weight           (y = x without a weight)
+ *   (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t),  t = pos * inv_freq[i]
+ * for i < rot / 2, with (a, b) = (i, i + rot / 2), or (2i, 2i + 1) if interleaved; dims
+ * rot and up are not rotated.  Values are only laid out.
+ *
+ *   q, k, v    in_dtype (fp32 or bf16): B * T tokens of Hq, Hkv and Hkv heads of Dh,
+ *              consecutive tokens q_stride, k_stride, v_stride elements apart (e.g.
+ *              the three parts of one projection's rows)
+ *   pos        [B][T] int32
+ *   inv_freq   [rot / 2] fp32
+ *   q_weight, k_weight  [Dh] fp32, or NULL: that array is not normed
+ *   out_q      [B][T][Hq][Dh] q_dtype (fp32 or bf16); with T = 1 and fp32 the q of
+ *              the decode calls
+ *   out_k/v    [B][Hkv][T][Dh] kv_dtype (fp32 or bf16): the new rows of an append, or
+ *              a Tier-1 pool's
+ *
+ * q with Hq = 0, k, and v may be NULL and are then left out (v needs k).  Limits: B, T
+ * >= 0, B * T < 2^31, Hq, Hkv <= 65535, Dh in {64, 128, 256}, rot in [0, Dh] and a
+ * multiple of 16, strides at least a token's elements and multiples of 16 bytes, eps
+ * >= 0 and finite.  No output may overlap an input.
+ * Arithmetic: fp32, rounded once to the outputs; angles in fp64 (pos * inv_freq to
+ * 2^-52 of itself), their sines and cosines to fp32's accuracy.  A head with an
+ * infinity or a NaN is NaN where the formula gives one.
+ */
+cmc_status cmc_norm_rope(const void *q, long long q_stride, const void *k, long long k_stride,
+                         const void *v, long long v_stride, cmc_dtype in_dtype,
+                         const int32_t *pos, const float *inv_freq, int rot, int interleaved,
+                         const float *q_weight, const float *k_weight, float eps,
+                         int B, int T, int Hq, int Hkv, int Dh,
+                         void *out_q, cmc_dtype q_dtype, void *out_k, void *out_v, cmc_dtype kv_dtype,
+                         void *stream);
 
 /* ------------------------------------------------------------------------ */
 /* Diagnostics.                                                             */

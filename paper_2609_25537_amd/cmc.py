@@ -43,6 +43,8 @@ EXPORTED = [
     "cmc_denoise", "cmc_bridge_workspace_bytes", "cmc_memory_bridge", "cmc_status_string", "cmc_last_error",
     "cmc_version", "cmc_decode_step_noalloc", "cmc_gather_tier1_q8", "cmc_window_append_q8", "cmc_cache_read_q8",
     "cmc_decode_q8_workspace_bytes", "cmc_two_tier_decode_q8", "cmc_decode_step_q8",
+    "cmc_gather_tier1_q4", "cmc_window_append_q4", "cmc_cache_read_q4", "cmc_decode_q4_workspace_bytes",
+    "cmc_two_tier_decode_q4", "cmc_decode_step_q4", "cmc_norm_rope",
 ]
 
 
@@ -119,6 +121,24 @@ def lib() -> ctypes.CDLL:
         L.cmc_decode_step_q8.argtypes = [P, P, P, P, P, P, I, P, P, P, P, P, I, P, P, I, I, I, I, I, I, I, I, I,
                                          ctypes.c_float, P, P, SZ, P]
         L.cmc_decode_step_q8.restype = I
+        L.cmc_gather_tier1_q4.argtypes = [P, P, I, P, P, I, I, I, I, I, I, P, P, P, P, P]
+        L.cmc_gather_tier1_q4.restype = I
+        L.cmc_window_append_q4.argtypes = [P, P, P, P, P, P, P, I, I, I, I, I, I, P]
+        L.cmc_window_append_q4.restype = I
+        L.cmc_cache_read_q4.argtypes = [P, P, P, P, P, I, I, I, I, I, I, P, P, P]
+        L.cmc_cache_read_q4.restype = I
+        L.cmc_decode_q4_workspace_bytes.argtypes = [I, I, I, I, I, I]
+        L.cmc_decode_q4_workspace_bytes.restype = SZ
+        L.cmc_two_tier_decode_q4.argtypes = [P, P, P, P, P, P, I, P, P, P, P, P, I, I, I, I, I, I,
+                                             ctypes.c_float, P, P, SZ, P]
+        L.cmc_two_tier_decode_q4.restype = I
+        L.cmc_decode_step_q4.argtypes = [P, P, P, P, P, P, I, P, P, P, P, P, I, P, P, I, I, I, I, I, I, I,
+                                         ctypes.c_float, P, P, SZ, P]
+        L.cmc_decode_step_q4.restype = I
+        LL = ctypes.c_longlong
+        L.cmc_norm_rope.argtypes = [P, LL, P, LL, P, LL, I, P, P, I, I, P, P, ctypes.c_float, I, I, I, I, I,
+                                    P, I, P, P, I, P]
+        L.cmc_norm_rope.restype = I
         L.cmc_status_string.argtypes = [I]
         L.cmc_status_string.restype = ctypes.c_char_p
         L.cmc_last_error.argtypes = []
@@ -882,3 +902,324 @@ def cmc_decode_step_q8(q, cme_k, cme_v, cme_ks, cme_vs, k: int, win_k, win_v, wi
     cmc_two_tier_decode_q8, in one launch.  Returns out [B][Hq][Dh] fp32."""
     return _decode_q8(True, q, cme_k, cme_v, cme_ks, cme_vs, k, win_k, win_v, win_ks, win_vs, win_count, new_k, new_v, scale,
                       block, k_len, out, workspace, stream)
+
+
+# ----------------------------------------------------------- 4-bit cache
+
+_q4_calls = None
+
+
+def _load_q4():
+    """The C functions of the 4-bit cache, looked up once."""
+    global _q4_calls
+    L = lib()
+    _q4_calls = (L.cmc_gather_tier1_q4, L.cmc_window_append_q4, L.cmc_cache_read_q4, L.cmc_two_tier_decode_q4,
+                 L.cmc_decode_step_q4)
+    return _q4_calls
+
+
+def _cache4_args(name, codes_k, codes_v, scales_k, scales_v):
+    """Checks of one 4-bit cache array pair; returns its (B, Hkv, R, Dh)."""
+    u8 = _torch.uint8
+    s = codes_k.shape
+    if not (len(s) == 4 and codes_v.shape == s and codes_k.dtype is u8 and codes_v.dtype is u8):
+        raise ValueError(f"{name}_k/v must be matching codes, uint8 [B][Hkv][rows][Dh / 2]")
+    B, Hkv, R, half = s
+    n = (B, Hkv, R, half // 16)
+    if not (scales_k.shape == n and scales_v.shape == n and scales_k.dtype is u8 and scales_v.dtype is u8):
+        raise ValueError(f"{name}_ks/vs must be uint8 [B][Hkv][rows][Dh / 32]")
+    if not (codes_k.is_contiguous() and codes_v.is_contiguous() and scales_k.is_contiguous()
+            and scales_v.is_contiguous()):
+        raise ValueError(f"{name}: codes and scales must be contiguous")
+    return B, Hkv, R, 2 * half
+
+
+def cmc_gather_tier1_q4(cme_k, cme_v, idx, k: int, k_len=None, out_k=None, out_v=None, out_ks=None, out_vs=None,
+                        stream=None):
+    """cmc_gather_tier1 into 4-bit codes with a power-of-two scale for every 32 dims of
+    a row.  cme_* [B][Hkv][N][Dh] fp32 or bf16.  Returns (out_k, out_v [B][Hkv][k][Dh /
+    2], out_ks, out_vs [B][Hkv][k][Dh / 32]), uint8."""
+    torch = _torch or _load_torch()
+    k = int(k)
+    ps = cme_k.shape
+    if not (len(ps) == 4 and cme_v.shape == ps and cme_v.dtype is cme_k.dtype and cme_k.is_contiguous()
+            and cme_v.is_contiguous()):
+        raise ValueError("cme_k/v [B][Hkv][N][Dh]")
+    B, Hkv, N, Dh = ps
+    if k < 0:
+        raise ValueError("k must be at least 0")
+    stride = 0
+    if idx is not None:
+        i = idx.shape
+        if not (len(i) == 2 and i[0] == B and idx.dtype is torch.int32 and idx.is_contiguous()):
+            raise ValueError("idx [B][idx_stride] int32")
+        stride = i[1]
+    if k_len is not None and not (k_len.shape == (B,) and k_len.dtype is torch.int32 and k_len.is_contiguous()):
+        raise ValueError("k_len [B] int32")
+    if out_k is None:
+        out_k = _make(stream, torch.empty, (B, Hkv, k, Dh // 2), dtype=torch.uint8, device=cme_k.device)
+    if out_v is None:
+        out_v = _make(stream, torch.empty_like, out_k)
+    if out_ks is None:
+        out_ks = _make(stream, torch.empty, (B, Hkv, k, Dh // 32), dtype=torch.uint8, device=cme_k.device)
+    if out_vs is None:
+        out_vs = _make(stream, torch.empty_like, out_ks)
+    if _cache4_args("out", out_k, out_v, out_ks, out_vs) != (B, Hkv, k, Dh):
+        raise ValueError("out_k/v [B][Hkv][k][Dh / 2]")
+    dev = _device_index()
+    if (cme_k.get_device() != dev or cme_v.get_device() != dev or out_k.get_device() != dev or out_v.get_device() != dev
+            or out_ks.get_device() != dev or out_vs.get_device() != dev
+            or (idx is not None and idx.get_device() != dev) or (k_len is not None and k_len.get_device() != dev)):
+        _elsewhere(dev, cme_k, cme_v, idx, k_len, out_k, out_v, out_ks, out_vs)
+    rc = (_q4_calls or _load_q4())[0](
+        cme_k.data_ptr(), cme_v.data_ptr(), _kv_dtype(cme_k), None if idx is None else idx.data_ptr(),
+        None if k_len is None else k_len.data_ptr(), stride, B, Hkv, N, k, Dh, out_k.data_ptr(), out_v.data_ptr(),
+        out_ks.data_ptr(), out_vs.data_ptr(), _raw_stream(dev) if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return out_k, out_v, out_ks, out_vs
+
+
+def cmc_window_append_q4(win_k, win_v, win_ks, win_vs, win_count, new_k, new_v, stream=None) -> None:
+    """Append to a 4-bit ring in place.  win_k/v [B][Hkv][W][Dh / 2] and win_ks/vs
+    [B][Hkv][W][Dh / 32] uint8, win_count [B] int32, new_* [B][Hkv][T][Dh] fp32 or
+    bf16."""
+    torch = _torch or _load_torch()
+    B, Hkv, W, Dh = _cache4_args("win", win_k, win_v, win_ks, win_vs)
+    T = _new_rows(new_k, new_v, B, Hkv, Dh)
+    if not (win_count.shape == (B,) and win_count.dtype is torch.int32 and win_count.is_contiguous()):
+        raise ValueError("win_count [B] int32")
+    dev = _device_index()
+    if (win_k.get_device() != dev or win_v.get_device() != dev or win_ks.get_device() != dev
+            or win_vs.get_device() != dev or win_count.get_device() != dev or new_k.get_device() != dev
+            or new_v.get_device() != dev):
+        _elsewhere(dev, win_k, win_v, win_ks, win_vs, win_count, new_k, new_v)
+    rc = (_q4_calls or _load_q4())[1](
+        win_k.data_ptr(), win_v.data_ptr(), win_ks.data_ptr(), win_vs.data_ptr(), win_count.data_ptr(),
+        new_k.data_ptr(), new_v.data_ptr(), _kv_dtype(new_k), B, Hkv, W, Dh, T,
+        _raw_stream(dev) if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def cmc_cache_read_q4(k4, v4, ks, vs, count=None, rows: Optional[int] = None, dtype=None, out_k=None, out_v=None,
+                      stream=None):
+    """Values of the newest `rows` rows (all R unless given; those of out_k where it is)
+    of a 4-bit cache, in the order they were written: rows r < min(count, R, rows) of
+    out_k/v [B][Hkv][rows][Dh], fp32 or bf16 (`dtype`, bf16 unless said otherwise, where
+    out_k is not given).  count [B] int32, or None for R rows.  Returns (out_k, out_v)."""
+    torch = _torch or _load_torch()
+    B, Hkv, R, Dh = _cache4_args("cache", k4, v4, ks, vs)
+    if count is not None and not (count.shape == (B,) and count.dtype is torch.int32 and count.is_contiguous()):
+        raise ValueError("count [B] int32")
+    if out_k is None:
+        rows = R if rows is None else int(rows)
+        if rows < 0:
+            raise ValueError("rows must be at least 0")
+        out_k = _make(stream, torch.empty, (B, Hkv, rows, Dh), dtype=dtype or torch.bfloat16, device=k4.device)
+    if out_v is None:
+        out_v = _make(stream, torch.empty_like, out_k)
+    s = out_k.shape
+    if not (len(s) == 4 and s == (B, Hkv, s[2] if rows is None else int(rows), Dh) and out_v.shape == s
+            and out_v.dtype is out_k.dtype and out_k.is_contiguous() and out_v.is_contiguous()):
+        raise ValueError("out_k/v [B][Hkv][rows][Dh]")
+    dev = _device_index()
+    if (k4.get_device() != dev or v4.get_device() != dev or ks.get_device() != dev or vs.get_device() != dev
+            or out_k.get_device() != dev or out_v.get_device() != dev
+            or (count is not None and count.get_device() != dev)):
+        _elsewhere(dev, k4, v4, ks, vs, count, out_k, out_v)
+    rc = (_q4_calls or _load_q4())[2](
+        k4.data_ptr(), v4.data_ptr(), ks.data_ptr(), vs.data_ptr(), None if count is None else count.data_ptr(), B, Hkv,
+        R, s[2], Dh, _kv_dtype(out_k), out_k.data_ptr(), out_v.data_ptr(),
+        _raw_stream(dev) if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return out_k, out_v
+
+
+def cmc_decode_q4_workspace_bytes(B: int, Hq: int, Hkv: int, Dh: int, k: int, W: int) -> int:
+    return int(lib().cmc_decode_q4_workspace_bytes(int(B), int(Hq), int(Hkv), int(Dh), int(k), int(W)))
+
+
+def decode_workspace_q4(B: int, Hq: int, Hkv: int, Dh: int, k: int, W: int, device):
+    """A zero-filled workspace of the 4-bit decode calls (the library keeps it
+    zeroed)."""
+    import torch
+    return torch.zeros(max(1, cmc_decode_q4_workspace_bytes(B, Hq, Hkv, Dh, k, W)), dtype=torch.uint8, device=device)
+
+
+def _decode_q4(step, q, cme_k, cme_v, cme_ks, cme_vs, k, win_k, win_v, win_ks, win_vs, win_count, new_k, new_v, scale,
+               k_len, out, workspace, stream):
+    """Both decode calls: the checks, then the C call."""
+    torch = _torch or _load_torch()
+    f32, i32 = torch.float32, torch.int32
+    k = int(k)
+    qs = q.shape
+    if not (len(qs) == 3 and q.dtype is f32 and q.is_contiguous()):
+        raise ValueError("q must be contiguous fp32 [B][Hq][Dh]")
+    B, Hq, Dh = qs
+    s = _cache4_args("cme", cme_k, cme_v, cme_ks, cme_vs)
+    _, Hkv, N, _ = s
+    if not (s[0] == B and s[3] == Dh):
+        raise ValueError("cme_k/v [B][Hkv][N][Dh / 2]")
+    W = T = 0
+    if win_k is not None:
+        s = _cache4_args("win", win_k, win_v, win_ks, win_vs)
+        W = s[2]
+        if s != (B, Hkv, W, Dh):
+            raise ValueError("win_k/v [B][Hkv][W][Dh / 2]")
+        if not (win_count is not None and win_count.shape == (B,) and win_count.dtype is i32
+                and win_count.is_contiguous()):
+            raise ValueError("win_count [B] int32")
+        if step and W > 0:
+            T = _new_rows(new_k, new_v, B, Hkv, Dh)
+    if k_len is not None and not (k_len.shape == (B,) and k_len.dtype is i32 and k_len.is_contiguous()):
+        raise ValueError("k_len [B] int32")
+    if out is None:
+        out = _make(stream, torch.empty, qs, dtype=f32, device=q.device)
+    elif not (out.shape == qs and out.dtype is f32 and out.is_contiguous()):
+        raise ValueError("out [B][Hq][Dh] fp32")
+    if workspace is None:
+        workspace = _make(stream, decode_workspace_q4, B, Hq, Hkv, Dh, k, W, q.device)
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    scale = float(scale)
+    dev = _device_index()
+    if (q.get_device() != dev or out.get_device() != dev or workspace.get_device() != dev or cme_k.get_device() != dev
+            or cme_v.get_device() != dev or cme_ks.get_device() != dev or cme_vs.get_device() != dev
+            or (k_len is not None and k_len.get_device() != dev)):
+        _elsewhere(dev, q, out, workspace, cme_k, cme_v, cme_ks, cme_vs, k_len)
+    wk = wv = wks = wvs = wc = nk = nv = None
+    if W > 0:
+        if (win_k.get_device() != dev or win_v.get_device() != dev or win_ks.get_device() != dev
+                or win_vs.get_device() != dev or win_count.get_device() != dev):
+            _elsewhere(dev, win_k, win_v, win_ks, win_vs, win_count)
+        wk, wv, wks, wvs, wc = (win_k.data_ptr(), win_v.data_ptr(), win_ks.data_ptr(), win_vs.data_ptr(),
+                                win_count.data_ptr())
+    kl = None if k_len is None else k_len.data_ptr()
+    ws_bytes = workspace.numel() * workspace.element_size()
+    st = _raw_stream(dev) if stream is None else _stream(stream)
+    calls = _q4_calls or _load_q4()
+    if step:
+        new_dtype = CMC_F32
+        if T > 0:
+            if new_k.get_device() != dev or new_v.get_device() != dev:
+                _elsewhere(dev, new_k, new_v)
+            nk, nv, new_dtype = new_k.data_ptr(), new_v.data_ptr(), _kv_dtype(new_k)
+        rc = calls[4](q.data_ptr(), cme_k.data_ptr(), cme_v.data_ptr(), cme_ks.data_ptr(), cme_vs.data_ptr(), kl, k, wk, wv,
+                      wks, wvs, wc, W, nk, nv, T, new_dtype, B, Hq, Hkv, Dh, N, scale, out.data_ptr(),
+                      workspace.data_ptr(), ws_bytes, st)
+    else:
+        rc = calls[3](q.data_ptr(), cme_k.data_ptr(), cme_v.data_ptr(), cme_ks.data_ptr(), cme_vs.data_ptr(), kl, k, wk, wv,
+                      wks, wvs, wc, W, B, Hq, Hkv, Dh, N, scale, out.data_ptr(), workspace.data_ptr(), ws_bytes, st)
+    if rc:
+        _check(rc)
+    return out
+
+
+def cmc_two_tier_decode_q4(q, cme_k, cme_v, cme_ks, cme_vs, k: int, win_k, win_v, win_ks, win_vs, win_count,
+                           scale: float, k_len=None, out=None, workspace=None, stream=None):
+    """cmc_two_tier_decode over the 4-bit cache: rows 0 .. k - 1 (k_len[b] - 1) of
+    cme_k/v [B][Hkv][N][Dh / 2] codes with cme_ks/vs [B][Hkv][N][Dh / 32] scales (uint8),
+    then the ring (None: no Tier-2).  Returns out [B][Hq][Dh] fp32."""
+    return _decode_q4(False, q, cme_k, cme_v, cme_ks, cme_vs, k, win_k, win_v, win_ks, win_vs, win_count, None, None, scale,
+                      k_len, out, workspace, stream)
+
+
+def cmc_decode_step_q4(q, cme_k, cme_v, cme_ks, cme_vs, k: int, win_k, win_v, win_ks, win_vs, win_count, new_k, new_v,
+                       scale: float, k_len=None, out=None, workspace=None, stream=None):
+    """cmc_window_append_q4 of new_k/new_v [B][Hkv][T][Dh] (fp32 or bf16), then
+    cmc_two_tier_decode_q4, in one launch.  Returns out [B][Hq][Dh] fp32."""
+    return _decode_q4(True, q, cme_k, cme_v, cme_ks, cme_vs, k, win_k, win_v, win_ks, win_vs, win_count, new_k, new_v, scale,
+                      k_len, out, workspace, stream)
+
+
+# ------------------------------------------------------ norm and rotation
+
+_rope_call = None
+
+
+def _heads(name, x, B, T, Dh):
+    """Checks of one projection part [B][T][H][Dh]; returns (heads, token stride).  Heads
+    are dense, tokens evenly spaced (a slice of a wider projection is)."""
+    s, st = x.shape, x.stride()
+    if not (len(s) == 4 and s[0] == B and s[1] == T and s[3] == Dh):
+        raise ValueError(f"{name} [B][T][H][Dh]")
+    H = s[2]
+    token = st[1] if T > 1 else st[0] if B > 1 else H * Dh
+    if x.numel() and not (st[3] == 1 and (H == 1 or st[2] == Dh) and (B == 1 or T == 1 or st[0] == T * token)):
+        raise ValueError(f"{name}: heads must be dense and tokens evenly spaced")
+    return H, token
+
+
+def cmc_norm_rope(q, k, v, pos, inv_freq, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False,
+                  out_q=None, out_k=None, out_v=None, q_dtype=None, kv_dtype=None, stream=None):
+    """Heads of a projection normed (where a weight is given), rotated by position and
+    laid out for the append and the decode.  q [B][T][Hq][Dh], k and v [B][T][Hkv][Dh]
+    fp32 or bf16, possibly slices of one projection; q, or v, or k and v, may be None.
+    pos [B][T] int32, inv_freq [rot / 2] fp32, weights [Dh] fp32.  Returns (out_q
+    [B][T][Hq][Dh] in q_dtype (fp32 unless said otherwise), out_k, out_v
+    [B][Hkv][T][Dh] in kv_dtype (the inputs' type unless said otherwise)), with None for
+    what was not given."""
+    global _rope_call
+    torch = _torch or _load_torch()
+    f32 = torch.float32
+    first = q if q is not None else k
+    if first is None or (v is not None and k is None):
+        raise ValueError("q or k must be given, and k where v is")
+    if first.dim() != 4:
+        raise ValueError("q [B][T][Hq][Dh]" if q is not None else "k [B][T][Hkv][Dh]")
+    B, T, _, Dh = first.shape
+    dtype, dev = first.dtype, _device_index()
+    if not (pos.shape == (B, T) and pos.dtype is torch.int32 and pos.is_contiguous()):
+        raise ValueError("pos [B][T] int32")
+    if not (inv_freq.dim() == 1 and inv_freq.dtype is f32 and inv_freq.is_contiguous()):
+        raise ValueError("inv_freq [rot / 2] fp32")
+    for w in (q_weight, k_weight):
+        if w is not None and not (w.shape == (Dh,) and w.dtype is f32 and w.is_contiguous()):
+            raise ValueError("weights [Dh] fp32")
+    Hq = Hkv = qs = ks = vs = 0
+    if q is not None:
+        Hq, qs = _heads("q", q, B, T, Dh)
+        if out_q is None:
+            out_q = _make(stream, torch.empty, (B, T, Hq, Dh), dtype=q_dtype or f32, device=q.device)
+        elif not (out_q.shape == (B, T, Hq, Dh) and out_q.is_contiguous()):
+            raise ValueError("out_q must be contiguous [B][T][Hq][Dh]")
+    else:
+        out_q = None
+    if k is not None:
+        Hkv, ks = _heads("k", k, B, T, Dh)
+        shape = (B, Hkv, T, Dh)
+        if out_k is None:
+            out_k = _make(stream, torch.empty, shape, dtype=kv_dtype or dtype, device=k.device)
+        elif not (out_k.shape == shape and out_k.is_contiguous()):
+            raise ValueError("out_k must be contiguous [B][Hkv][T][Dh]")
+    else:
+        out_k = None
+    if v is not None:
+        Hv, vs = _heads("v", v, B, T, Dh)
+        if out_v is None:
+            out_v = _make(stream, torch.empty_like, out_k)
+        if not (Hv == Hkv and out_v.shape == shape and out_v.dtype is out_k.dtype and out_v.is_contiguous()):
+            raise ValueError("v must match k, and out_v out_k")
+    else:
+        out_v = None
+    for x in (q, k, v):
+        if x is not None and x.dtype is not dtype:
+            raise ValueError("q, k and v must be of one type")
+    for x in (q, k, v, pos, inv_freq, q_weight, k_weight, out_q, out_k, out_v):
+        if x is not None and x.get_device() != dev:
+            _elsewhere(dev, x)
+    if _rope_call is None:
+        _rope_call = lib().cmc_norm_rope
+    rc = _rope_call(
+        None if q is None else q.data_ptr(), qs, None if k is None else k.data_ptr(), ks,
+        None if v is None else v.data_ptr(), vs, _kv_dtype(first), pos.data_ptr(), inv_freq.data_ptr(),
+        2 * inv_freq.shape[0], 1 if interleaved else 0, None if q_weight is None else q_weight.data_ptr(),
+        None if k_weight is None else k_weight.data_ptr(), float(eps), B, T, Hq, Hkv, Dh,
+        None if out_q is None else out_q.data_ptr(), CMC_F32 if out_q is None else _kv_dtype(out_q),
+        None if out_k is None else out_k.data_ptr(), None if out_v is None else out_v.data_ptr(),
+        CMC_F32 if out_k is None else _kv_dtype(out_k), _raw_stream(dev) if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return out_q, out_k, out_v

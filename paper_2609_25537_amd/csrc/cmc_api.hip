@@ -261,6 +261,11 @@ DecodePlan plan_decode8(int B, int Hq, int Hkv, int Dh, int k, int W, bool appen
     return pl;
 }
 
+DecodePlan plan_decode4(int B, int Hq, int Hkv, int Dh, int k, int W, bool append) {
+    static_assert(kUnit4 == kUnit8, "the plans count in the same units");
+    return plan_decode8(B, Hq, Hkv, Dh, k, W, append);
+}
+
 }  // namespace cmc
 
 extern "C" {
@@ -994,6 +999,292 @@ cmc_status cmc_decode_step_q8(const float *q, const void *cme_k, const void *cme
     return decode8_impl("decode_step_q8", q, cme_k, cme_v, cme_ks, cme_vs, k_len, k, win_k, win_v, win_ks, win_vs,
                         win_count, W, new_k, new_v, T_new, new_dtype, code, block, B, Hq, Hkv, Dh, N, scale, out,
                         workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"
+
+// ----------------------------------------------------------- 4-bit cache
+
+namespace {
+
+// Checks shared by the calls on a 4-bit cache array of R rows a head.
+cmc_status check_cache4(const char *fn, int B, int Hkv, int Dh, const char *rows, int R) {
+    if (B < 0 || Hkv < 1 || R < 0)
+        return fail(CMC_ERR_INVALID_ARGUMENT, "%s: need B, %s >= 0 and Hkv >= 1 (got B=%d %s=%d Hkv=%d)", fn, rows, B, rows,
+                    R, Hkv);
+    if (!supported_dh(Dh)) return fail(CMC_ERR_UNSUPPORTED, "%s: Dh=%d not in {64,128,256}", fn, Dh);
+    if (B > 65535 || Hkv > 65535) return fail(CMC_ERR_UNSUPPORTED, "%s: B and Hkv must be <= 65535", fn);
+    if (R > cmc::kCache4MaxRows)
+        return fail(CMC_ERR_UNSUPPORTED, "%s: %s=%d exceeds %d", fn, rows, R, cmc::kCache4MaxRows);
+    return CMC_OK;
+}
+
+cmc_status decode4_impl(const char *fn, const float *q, const uint8_t *cme_k, const uint8_t *cme_v,
+                        const uint8_t *cme_ks, const uint8_t *cme_vs, const int32_t *k_len, int k, uint8_t *win_k,
+                        uint8_t *win_v, uint8_t *win_ks, uint8_t *win_vs, int32_t *win_count, int W, const void *new_k,
+                        const void *new_v, int T_new, cmc_dtype new_dtype, int B, int Hq, int Hkv, int Dh, int N,
+                        float scale, float *out, void *workspace, size_t workspace_bytes, void *stream) {
+    if (cmc_status st = check_cache4(fn, B, Hkv, Dh, "W", W)) return st;
+    if (cmc_status st = check_cache4(fn, B, Hkv, Dh, "N", N)) return st;
+    if (Hq < 1 || k < 0) return fail(CMC_ERR_INVALID_ARGUMENT, "%s: need Hq >= 1 and k >= 0", fn);
+    if (Hq % Hkv != 0) return fail(CMC_ERR_INVALID_ARGUMENT, "%s: Hq=%d not a multiple of Hkv=%d", fn, Hq, Hkv);
+    const int G = Hq / Hkv;
+    if (G != 1 && G != 2 && G != 4 && G != 8)
+        return fail(CMC_ERR_UNSUPPORTED, "%s: Hq/Hkv=%d not in {1,2,4,8}", fn, G);
+    if ((long long)k + W < 1) return fail(CMC_ERR_INVALID_ARGUMENT, "%s: empty cache (k + W = 0)", fn);
+    if (k > N) return fail(CMC_ERR_INVALID_ARGUMENT, "%s: k=%d exceeds N=%d", fn, k, N);
+    if (!(scale == scale) || isinf(scale)) return fail(CMC_ERR_INVALID_ARGUMENT, "%s: scale must be finite", fn);
+    if (T_new < 0 || (W > 0 && T_new > W))
+        return fail(CMC_ERR_INVALID_ARGUMENT, "%s: need 0 <= T_new <= W (got T_new=%d W=%d)", fn, T_new, W);
+    if (W == 0) T_new = 0;  // no Tier-2: appending is a no-op
+    if (T_new > 0) {
+        if (cmc_status st = check_float(fn, new_dtype)) return st;
+    }
+    if (B == 0) return ok();
+    if (!q || !out) return fail(CMC_ERR_INVALID_ARGUMENT, "%s: q and out must be non-null", fn);
+    if (k > 0 && (!cme_k || !cme_v || !cme_ks || !cme_vs))
+        return fail(CMC_ERR_INVALID_ARGUMENT, "%s: null Tier-1 codes or scales", fn);
+    if (W > 0 && (!win_k || !win_v || !win_ks || !win_vs || !win_count))
+        return fail(CMC_ERR_INVALID_ARGUMENT, "%s: null Tier-2 window", fn);
+    if (T_new > 0 && (!new_k || !new_v)) return fail(CMC_ERR_INVALID_ARGUMENT, "%s: null new rows", fn);
+    if (misaligned(q) || misaligned(cme_k) || misaligned(cme_v) || misaligned(cme_ks) || misaligned(cme_vs) ||
+        misaligned(k_len) || misaligned(win_k) || misaligned(win_v) || misaligned(win_ks) || misaligned(win_vs) ||
+        misaligned(win_count) || misaligned(out) || misaligned(workspace) || misaligned(new_k) || misaligned(new_v))
+        return fail(CMC_ERR_UNSUPPORTED, "%s: every pointer must be 16-byte aligned", fn);
+    const bool fused = T_new > 0 && T_new <= cmc::kFusedRows4;
+    const cmc::DecodePlan pl = cmc::plan_decode4(B, Hq, Hkv, Dh, k, W, fused);
+    const size_t need = cmc_decode_q4_workspace_bytes(B, Hq, Hkv, Dh, k, W);
+    if (!workspace || workspace_bytes < need)
+        return fail(CMC_ERR_WORKSPACE_TOO_SMALL, "%s: workspace of %zu bytes needed, %zu given", fn, need,
+                    workspace ? workspace_bytes : (size_t)0);
+    if (T_new > 0 && !fused) {
+        if (cmc_status st = cmc_window_append_q4(win_k, win_v, win_ks, win_vs, win_count, new_k, new_v, new_dtype, B, Hkv,
+                                                 W, Dh, T_new, stream))
+            return st;
+        T_new = 0;
+    }
+    cmc::Decode4Params p{};
+    char *const counters = static_cast<char *>(workspace);
+    char *const partials = counters + pl.counter_bytes;
+    p.q = q;
+    p.cme_k = cme_k;
+    p.cme_v = cme_v;
+    p.cme_ks = cme_ks;
+    p.cme_vs = cme_vs;
+    p.k_len = k_len;
+    p.win_k = win_k;
+    p.win_v = win_v;
+    p.win_ks = win_ks;
+    p.win_vs = win_vs;
+    p.win_count = W > 0 ? win_count : nullptr;
+    p.new_k = new_k;
+    p.new_v = new_v;
+    p.new_bf16 = new_dtype == CMC_BF16;
+    p.out = out;
+    p.seq_counter = reinterpret_cast<unsigned *>(counters);
+    p.pair_counter = reinterpret_cast<unsigned *>(counters) + B;
+    p.part_ml = reinterpret_cast<float *>(partials);
+    p.part_acc = reinterpret_cast<float *>(partials + pl.ml_bytes);
+    p.k = k;
+    p.W = W;
+    p.B = B;
+    p.Hq = Hq;
+    p.Hkv = Hkv;
+    p.N = N;
+    p.T_new = T_new;
+    p.new_split = pl.own_append ? 1 : 0;
+    p.S = pl.S + p.new_split;
+    p.chunk = pl.chunk;
+    p.waves = pl.waves;
+    p.qscale = cmc::decode_qscale(scale);
+    hipError_t e = cmc::launch_decode4(p, G, Dh, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "decode launch");
+    return ok();
+}
+
+}  // namespace
+
+extern "C" {
+
+cmc_status cmc_gather_tier1_q4(const void *cme_k, const void *cme_v, cmc_dtype kv_dtype, const int32_t *idx,
+                               const int32_t *k_len, int idx_stride, int B, int Hkv, int N, int k, int Dh,
+                               uint8_t *out_k, uint8_t *out_v, uint8_t *out_ks, uint8_t *out_vs, void *stream) {
+    if (cmc_status st = check_float("gather_q4", kv_dtype)) return st;
+    if (cmc_status st = check_cache4("gather_q4", B, Hkv, Dh, "k", k)) return st;
+    if (N < 0) return fail(CMC_ERR_INVALID_ARGUMENT, "gather_q4: need N >= 0 (got N=%d)", N);
+    if (idx && idx_stride < k)
+        return fail(CMC_ERR_INVALID_ARGUMENT, "gather_q4: idx_stride=%d is below k=%d", idx_stride, k);
+    if (!idx && k > N) return fail(CMC_ERR_INVALID_ARGUMENT, "gather_q4: k=%d exceeds N=%d with idx == NULL", k, N);
+    if (k > 0 && N < 1) return fail(CMC_ERR_INVALID_ARGUMENT, "gather_q4: k=%d rows from an empty pool", k);
+    if (B == 0 || k == 0) return ok();
+    if (!cme_k || !cme_v || !out_k || !out_v || !out_ks || !out_vs)
+        return fail(CMC_ERR_INVALID_ARGUMENT, "gather_q4: null pointer");
+    if (misaligned(cme_k) || misaligned(cme_v) || misaligned(idx) || misaligned(k_len) || misaligned(out_k) ||
+        misaligned(out_v) || misaligned(out_ks) || misaligned(out_vs))
+        return fail(CMC_ERR_UNSUPPORTED, "gather_q4: every pointer must be 16-byte aligned");
+    cmc::Write4Params p{};
+    p.src_k = cme_k;
+    p.src_v = cme_v;
+    p.idx = idx;
+    p.count = const_cast<int32_t *>(k_len);  // read only
+    p.k = out_k;
+    p.v = out_v;
+    p.ks = out_ks;
+    p.vs = out_vs;
+    p.B = B;
+    p.Hkv = Hkv;
+    p.R = k;
+    p.src_rows = N;
+    p.idx_stride = idx_stride;
+    p.row_shift = log2_of(Dh / 8);
+    hipError_t e = cmc::launch_gather4(p, kv_dtype == CMC_BF16, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "gather_q4 launch");
+    return ok();
+}
+
+cmc_status cmc_window_append_q4(uint8_t *win_k, uint8_t *win_v, uint8_t *win_ks, uint8_t *win_vs, int32_t *win_count,
+                                const void *new_k, const void *new_v, cmc_dtype new_dtype, int B, int Hkv, int W, int Dh,
+                                int T_new, void *stream) {
+    if (cmc_status st = check_float("append_q4", new_dtype)) return st;
+    if (cmc_status st = check_cache4("append_q4", B, Hkv, Dh, "W", W)) return st;
+    if (W == 0 || B == 0) return ok();
+    if (T_new < 1 || T_new > W)
+        return fail(CMC_ERR_INVALID_ARGUMENT, "append_q4: need 1 <= T_new <= W (got T_new=%d W=%d)", T_new, W);
+    if (!win_k || !win_v || !win_ks || !win_vs || !win_count || !new_k || !new_v)
+        return fail(CMC_ERR_INVALID_ARGUMENT, "append_q4: null pointer");
+    if (misaligned(win_k) || misaligned(win_v) || misaligned(win_ks) || misaligned(win_vs) || misaligned(win_count) ||
+        misaligned(new_k) || misaligned(new_v))
+        return fail(CMC_ERR_UNSUPPORTED, "append_q4: every pointer must be 16-byte aligned");
+    cmc::Write4Params p{};
+    p.src_k = new_k;
+    p.src_v = new_v;
+    p.count = win_count;
+    p.k = win_k;
+    p.v = win_v;
+    p.ks = win_ks;
+    p.vs = win_vs;
+    p.B = B;
+    p.Hkv = Hkv;
+    p.R = W;
+    p.src_rows = T_new;
+    p.T_new = T_new;
+    p.row_shift = log2_of(Dh / 8);
+    hipError_t e = cmc::launch_append4(p, new_dtype == CMC_BF16, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "append_q4 launch");
+    return ok();
+}
+
+cmc_status cmc_cache_read_q4(const uint8_t *k4, const uint8_t *v4, const uint8_t *ks, const uint8_t *vs,
+                             const int32_t *count, int B, int Hkv, int R, int rows, int Dh, cmc_dtype out_dtype,
+                             void *out_k, void *out_v, void *stream) {
+    if (cmc_status st = check_float("cache_read_q4", out_dtype)) return st;
+    if (cmc_status st = check_cache4("cache_read_q4", B, Hkv, Dh, "R", R)) return st;
+    if (rows < 0 || rows > R)
+        return fail(CMC_ERR_INVALID_ARGUMENT, "cache_read_q4: need 0 <= rows <= R (got rows=%d R=%d)", rows, R);
+    if (B == 0 || rows == 0) return ok();
+    if (!k4 || !v4 || !ks || !vs || !out_k || !out_v)
+        return fail(CMC_ERR_INVALID_ARGUMENT, "cache_read_q4: null pointer");
+    if (misaligned(k4) || misaligned(v4) || misaligned(ks) || misaligned(vs) || misaligned(count) ||
+        misaligned(out_k) || misaligned(out_v))
+        return fail(CMC_ERR_UNSUPPORTED, "cache_read_q4: every pointer must be 16-byte aligned");
+    cmc::Read4Params p{k4, v4, ks, vs, count, out_k, out_v, B, Hkv, R, rows, log2_of(Dh / 8)};
+    hipError_t e = cmc::launch_read4(p, out_dtype == CMC_BF16, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "cache_read_q4 launch");
+    return ok();
+}
+
+size_t cmc_decode_q4_workspace_bytes(int B, int Hq, int Hkv, int Dh, int k, int W) {
+    if (B < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || k < 0 || W < 0 || !supported_dh(Dh)) return 0;
+    return std::max(cmc::plan_decode4(B, Hq, Hkv, Dh, k, W, false).total,
+                    cmc::plan_decode4(B, Hq, Hkv, Dh, k, W, true).total);
+}
+
+cmc_status cmc_two_tier_decode_q4(const float *q, const uint8_t *cme_k, const uint8_t *cme_v, const uint8_t *cme_ks,
+                                  const uint8_t *cme_vs, const int32_t *k_len, int k, const uint8_t *win_k,
+                                  const uint8_t *win_v, const uint8_t *win_ks, const uint8_t *win_vs,
+                                  const int32_t *win_count, int W, int B, int Hq, int Hkv, int Dh, int N, float scale,
+                                  float *out, void *workspace, size_t workspace_bytes, void *stream) {
+    // Nothing is appended (T_new = 0), so the window is only read.
+    return decode4_impl("decode_q4", q, cme_k, cme_v, cme_ks, cme_vs, k_len, k, const_cast<uint8_t *>(win_k),
+                        const_cast<uint8_t *>(win_v), const_cast<uint8_t *>(win_ks), const_cast<uint8_t *>(win_vs),
+                        const_cast<int32_t *>(win_count), W, nullptr, nullptr, 0, CMC_F32, B, Hq, Hkv, Dh, N, scale, out,
+                        workspace, workspace_bytes, stream);
+}
+
+cmc_status cmc_decode_step_q4(const float *q, const uint8_t *cme_k, const uint8_t *cme_v, const uint8_t *cme_ks,
+                              const uint8_t *cme_vs, const int32_t *k_len, int k, uint8_t *win_k, uint8_t *win_v,
+                              uint8_t *win_ks, uint8_t *win_vs, int32_t *win_count, int W, const void *new_k,
+                              const void *new_v, int T_new, cmc_dtype new_dtype, int B, int Hq, int Hkv, int Dh, int N,
+                              float scale, float *out, void *workspace, size_t workspace_bytes, void *stream) {
+    if (W > 0 && T_new < 1)
+        return fail(CMC_ERR_INVALID_ARGUMENT, "decode_step_q4: need 1 <= T_new <= W (got T_new=%d W=%d)", T_new, W);
+    return decode4_impl("decode_step_q4", q, cme_k, cme_v, cme_ks, cme_vs, k_len, k, win_k, win_v, win_ks, win_vs,
+                        win_count, W, new_k, new_v, T_new, new_dtype, B, Hq, Hkv, Dh, N, scale, out, workspace,
+                        workspace_bytes, stream);
+}
+
+// ---------------------------------------------------------- norm and rotation
+
+cmc_status cmc_norm_rope(const void *q, long long q_stride, const void *k, long long k_stride, const void *v,
+                         long long v_stride, cmc_dtype in_dtype, const int32_t *pos, const float *inv_freq, int rot,
+                         int interleaved, const float *q_weight, const float *k_weight, float eps, int B, int T, int Hq,
+                         int Hkv, int Dh, void *out_q, cmc_dtype q_dtype, void *out_k, void *out_v, cmc_dtype kv_dtype,
+                         void *stream) {
+    if (cmc_status st = check_float("norm_rope", in_dtype)) return st;
+    if (cmc_status st = check_float("norm_rope", q_dtype)) return st;
+    if (cmc_status st = check_float("norm_rope", kv_dtype)) return st;
+    if (B < 0 || T < 0 || Hq < 0 || Hkv < 0)
+        return fail(CMC_ERR_INVALID_ARGUMENT, "norm_rope: need B, T, Hq, Hkv >= 0 (got B=%d T=%d Hq=%d Hkv=%d)", B, T, Hq,
+                    Hkv);
+    if (!supported_dh(Dh)) return fail(CMC_ERR_UNSUPPORTED, "norm_rope: Dh=%d not in {64,128,256}", Dh);
+    if (rot < 0 || rot > Dh) return fail(CMC_ERR_INVALID_ARGUMENT, "norm_rope: rot=%d not in [0, Dh=%d]", rot, Dh);
+    if (rot % 16 != 0) return fail(CMC_ERR_UNSUPPORTED, "norm_rope: rot=%d must be a multiple of 16", rot);
+    if (Hq > 65535 || Hkv > 65535) return fail(CMC_ERR_UNSUPPORTED, "norm_rope: Hq and Hkv must be <= 65535");
+    if ((long long)B * T > INT_MAX) return fail(CMC_ERR_UNSUPPORTED, "norm_rope: B * T must be below 2^31");
+    if (!(eps >= 0.f) || isinf(eps)) return fail(CMC_ERR_INVALID_ARGUMENT, "norm_rope: need a finite eps >= 0");
+    if (v && !k) return fail(CMC_ERR_INVALID_ARGUMENT, "norm_rope: v without k");
+    if ((long long)B * T == 0 || (Hq == 0 && (!k || Hkv == 0))) return ok();
+    const long long vec = in_dtype == CMC_BF16 ? 8 : 4;  // elements in 16 bytes
+    const auto bad = [&](const void *x, long long stride, int heads) {
+        return x && heads > 0 && (stride < (long long)heads * Dh || stride % vec != 0);
+    };
+    if (bad(Hq > 0 ? q : nullptr, q_stride, Hq) || bad(k, k_stride, Hkv) || bad(v, v_stride, Hkv))
+        return fail(CMC_ERR_INVALID_ARGUMENT,
+                    "norm_rope: strides must hold a token's heads and be multiples of 16 bytes (got %lld, %lld, %lld "
+                    "elements)", q_stride, k_stride, v_stride);
+    if ((Hq > 0 && (!q || !out_q)) || (k && Hkv > 0 && !out_k) || (v && Hkv > 0 && !out_v))
+        return fail(CMC_ERR_INVALID_ARGUMENT, "norm_rope: null pointer");
+    if (rot > 0 && (!pos || !inv_freq))
+        return fail(CMC_ERR_INVALID_ARGUMENT, "norm_rope: pos and inv_freq must be non-null when rot > 0");
+    if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(pos) || misaligned(inv_freq) ||
+        misaligned(q_weight) || misaligned(k_weight) || misaligned(out_q) || misaligned(out_k) || misaligned(out_v))
+        return fail(CMC_ERR_UNSUPPORTED, "norm_rope: every pointer must be 16-byte aligned");
+    cmc::RopeParams p{};
+    p.q = q;
+    p.k = Hkv > 0 ? k : nullptr;
+    p.v = Hkv > 0 ? v : nullptr;
+    p.q_stride = q_stride;
+    p.k_stride = k_stride;
+    p.v_stride = v_stride;
+    p.pos = pos;
+    p.inv_freq = inv_freq;
+    p.q_weight = q_weight;
+    p.k_weight = k_weight;
+    p.out_q = out_q;
+    p.out_k = out_k;
+    p.out_v = out_v;
+    p.B = B;
+    p.T = T;
+    p.Hq = Hq;
+    p.Hkv = Hkv;
+    p.Dh = Dh;
+    p.rot = rot;
+    p.eps = eps;
+    p.interleaved = interleaved != 0;
+    hipError_t e = cmc::launch_norm_rope(p, in_dtype == CMC_BF16, q_dtype == CMC_BF16, kv_dtype == CMC_BF16,
+                                         static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "norm_rope launch");
+    return ok();
 }
 
 }  // extern "C"

@@ -1,0 +1,757 @@
+// Two-tier decode attention over the 4-bit cache (format: cache4.hpp): softmax
+// attention of one query token over [Tier-1 rows || ring slots], optionally fused
+// with the append of this step's rows, in one launch.
+//
+// Grid (S, Hkv, B), 4 or 8 waves.  A wave takes units of 32 rows and adds
+//   x_t = scale log2(e) <q, K_t>     p_t = 2^(x_t - m)
+//   l  += sum_t p_t                  acc += sum_t p_t V_t
+// with m a running maximum.  Both products run on MFMA (16x16x32, bf16 in, fp32
+// sums).  bf16 holds every code times its scale exactly, and the card widens two
+// codes with their scale in one instruction, so only q and p have to be split: into
+// three bf16 parts of 8 bits each, by cutting, which together are all of fp32's 24.
+//
+// Scores: A = 16 rows' K, B = q, a lane ends with the scores of one column for 4 + 4
+// rows.  Columns are (head, part): column c holds part c / G of head c % G (eight
+// heads have room for two parts and take a second MFMA for the third), and rotates
+// within the 16 lanes add the parts, from the widest down, so that all columns of a
+// head end with the same bits.
+// P V: the same lanes hold p in the A layout as it stands (rows = columns before), so
+// p crosses no lane.  A code byte holds two dims of one row, and widens to the two k
+// slots of a B word: with p in one slot and 0 in the other, a product gives one of
+// the two dims.  So rows are (head, dim parity, part), one MFMA takes 16 keys x 32
+// dims, and no code moves between lanes or bytes.  V's rows are loaded to match: lane
+// (c, q4) takes Dh / 16 consecutive dims of rows 4 q4 .. 4 q4 + 3 and 16 + 4 q4 ..
+// The same rows against ones give l, from the p that V was multiplied with.
+//
+// The maximum is moved only when a score passes it by more than 2 (p <= 4), which
+// after the first units is rare; that test needs no exchange between lanes.  Maxima
+// of 2^22 and more, where fp32 no longer resolves that, move with every unit and have
+// their weights' arguments subtracted first.
+//
+// Fused append: the last split (one of its own where the plan says so) writes the
+// appended rows, then attends over the ring units that hold them; every other split
+// leaves those units out.  Publication, merge and the count's advance are
+// decode_finish.hpp's.
+#include <type_traits>
+
+#include "cache4.hpp"
+#include "decode_common.hpp"
+
+namespace cmc {
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr float kMaxSlack = 2.f;  // how far a score may pass a running maximum below 2^22
+// Running maxima of 2^22 and more, where fp32 is spaced by a half and more, take the
+// weights' argument apart (Walk4::add).
+constexpr int kFarExp = 22;
+
+// x f and x f - m with the product rounded on its own: a maximum is such a product,
+// so its own difference is 0 (contracted, x f would enter with all its bits).
+__device__ __forceinline__ float rounded_product(float x, float f) {
+#pragma clang fp contract(off)
+    return x * f;
+}
+__device__ __forceinline__ float product_less(float x, float f, float m) {
+#pragma clang fp contract(off)
+    const float xf = x * f;
+    return xf - m;
+}
+
+// A constant loaded where it is used, on a rare path, instead of kept in a register.
+__device__ __forceinline__ float made_here(float c) {
+    asm("" : "+v"(c));
+    return c;
+}
+
+// Keeps loads after this point from being issued before it, and arithmetic on
+// the registers they go to from being moved behind it.
+__device__ __forceinline__ void in_order() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+__device__ __forceinline__ floatx4 mfma_bf16(const uint4 &a, const uint4 &b, const floatx4 &c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// x's leading 8 bits, as a float.
+__device__ __forceinline__ float cut(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+// Two parts of 8 bits side by side.
+__device__ __forceinline__ uint32_t pair_of(float lo, float hi) {
+    return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302);
+}
+
+// Units in flight per wave.
+template <int DH, int G>
+constexpr int kSets4 = G * DH > 1024 ? 1 : 2;
+
+template <int NW, int DH, int G>
+struct Walk4 {
+    static constexpr int KW = DH / 32;         // words of a K row per lane, and MFMAs per 16 rows
+    static constexpr int VB = DH / 32;         // bytes of a V row per lane (two dims each), and MFMAs per 16 rows
+    static constexpr int QP = G == 8 ? 2 : 1;  // MFMAs that q's parts take
+    static constexpr int PP = G == 8 ? 3 : G == 4 ? 2 : 1;  // and p's
+    static constexpr int NS = kSets4<DH, G>;
+    // Units on their way or being worked on, each in registers of its own.
+    struct Unit {
+        uint32_t k[2][KW];
+        uint32_t v[8][VB == 8 ? 2 : 1];
+        uint32_t ks[2], vs[8];  // scale bytes as loaded
+    } un[NS];
+    float4 qx[2 * KW];        // q as loaded
+    uint4 q[QP][KW];
+    float f;                  // |scale| log2(e) over q's power of two
+    float m;                  // of head r16 % G
+    float limit;              // the largest score that m may stay for
+    floatx4 l, acc[VB];       // rows 4 q4 + i: (head, dim parity, part)
+    int lane, r16, q4;
+
+    __device__ __forceinline__ void init() {
+        lane = threadIdx.x & 63;
+        r16 = lane & 15;
+        q4 = lane >> 4;
+        m = kNoMax;
+        limit = kNoMax;
+        l = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < VB; ++j) acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    // The unit's first `rows` rows, the others as zeros, by the buffer loads'
+    // bounds: loads without branches keep the compiler's wait counts exact, and a
+    // row costs no address arithmetic (its offset is the lane's and a constant).
+    static constexpr int kNonTemporal = 2;
+    __device__ __forceinline__ static __amdgpu_buffer_rsrc_t bytes_at(const uint8_t *at, int bytes) {
+        constexpr int untyped = 0x00027000;  // 32-bit elements, addressed by bytes
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(at), 0, bytes, untyped);
+    }
+    __device__ __forceinline__ void load_k(int set, const uint8_t *k, int rows) {
+        Unit &n = un[set];
+        const __amdgpu_buffer_rsrc_t from = bytes_at(k, rows * (DH / 2));
+        const int o = r16 * (DH / 2) + 4 * KW * q4;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int at = o + 16 * t * (DH / 2);
+            if constexpr (KW == 2) {
+                const auto x = __builtin_amdgcn_raw_buffer_load_b64(from, at, 0, 0);
+                n.k[t][0] = x[0];
+                n.k[t][1] = x[1];
+            } else {
+#pragma unroll
+                for (int i = 0; i < KW; i += 4) {
+                    const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(from, at + 4 * i, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) n.k[t][i + e] = x[e];
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void load_ks(int set, const uint8_t *ks, int rows) {
+        Unit &n = un[set];
+        const __amdgpu_buffer_rsrc_t from = bytes_at(ks, rows * (DH / 32));
+        const int o = r16 * (DH / 32) + (DH == 64 ? q4 >> 1 : DH == 128 ? q4 : 2 * q4);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int at = o + 16 * t * (DH / 32);
+            if constexpr (DH == 256) n.ks[t] = __builtin_amdgcn_raw_buffer_load_b16(from, at, 0, 0);
+            else n.ks[t] = __builtin_amdgcn_raw_buffer_load_b8(from, at, 0, 0);
+        }
+    }
+    __device__ __forceinline__ void load_v(int set, const uint8_t *v, int rows) {
+        Unit &n = un[set];
+        const __amdgpu_buffer_rsrc_t from = bytes_at(v, rows * (DH / 2));
+        const int o = 4 * q4 * (DH / 2) + VB * r16;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int at = o + ((j >> 2) * 16 + (j & 3)) * (DH / 2);
+            if constexpr (VB == 2) {
+                n.v[j][0] = __builtin_amdgcn_raw_buffer_load_b16(from, at, 0, kNonTemporal);
+            } else if constexpr (VB == 4) {
+                n.v[j][0] = __builtin_amdgcn_raw_buffer_load_b32(from, at, 0, kNonTemporal);
+            } else {
+                const auto x = __builtin_amdgcn_raw_buffer_load_b64(from, at, 0, kNonTemporal);
+                n.v[j][0] = x[0];
+                n.v[j][1] = x[1];
+            }
+        }
+    }
+    __device__ __forceinline__ void load_vs(int set, const uint8_t *vs, int rows) {
+        Unit &n = un[set];
+        const __amdgpu_buffer_rsrc_t from = bytes_at(vs, rows * (DH / 32));
+        const int o = 4 * q4 * (DH / 32) + r16 * DH / 512;  // the lane's dims begin at r16 Dh / 16
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            n.vs[j] = __builtin_amdgcn_raw_buffer_load_b8(from, o + ((j >> 2) * 16 + (j & 3)) * (DH / 32), 0, 0);
+    }
+
+    // The lane's quarter of its head's q.
+    __device__ __forceinline__ void request_q(const DecodeParams &p, int b, int kvh) {
+        const float *qp = p.q + ((size_t)b * p.Hq + (size_t)kvh * G + (r16 % G)) * DH + 8 * KW * q4;
+#pragma unroll
+        for (int i = 0; i < 2 * KW; ++i) qx[i] = *reinterpret_cast<const float4 *>(qp + 4 * i);
+    }
+    // q times a power of two, and its parts.  With 2^sum the size of scale log2(e) q, q
+    // is taken to 2^-12, so that a score's sum stays in range for any K, and f makes up
+    // for it; past 2^60 and below 2^-100, where it takes tiny or huge K to bring the
+    // scores back, q takes a share, so that neither f nor the products are subnormal.
+    __device__ __forceinline__ void split_q(const DecodeParams &p) {
+        float x[8 * KW];
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 2 * KW; ++i) {
+            x[4 * i] = qx[i].x;
+            x[4 * i + 1] = qx[i].y;
+            x[4 * i + 2] = qx[i].z;
+            x[4 * i + 3] = qx[i].w;
+        }
+#pragma unroll
+        for (int e = 0; e < 8 * KW; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+        const auto a = __builtin_amdgcn_permlane16_swap(top, top, false, false);
+        top = max((uint32_t)a[0], (uint32_t)a[1]);
+        const auto c = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+        top = max((uint32_t)c[0], (uint32_t)c[1]);
+        const int qe = (int)(top >> 23) - 127, se = __builtin_amdgcn_frexp_expf(p.qscale);
+        const int sum = qe + se;
+        const int to = sum > 60 ? min(sum - 72, 60) : sum < -100 ? max(sum + 88, -72) : -12;
+        f = ldexpf(__builtin_amdgcn_frexp_mantf(fabsf(p.qscale)), sum - to);
+        const float sign = copysignf(1.f, p.qscale);
+        const int part = r16 / G;
+#pragma unroll
+        for (int i = 0; i < KW; ++i) {
+            float y[2][8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float z = ldexpf(x[8 * i + e] * sign, to - qe);
+                const float hi = cut(z), r = z - hi, mid = cut(r), lo = r - mid;
+                if constexpr (G == 8) {
+                    y[0][e] = part == 0 ? hi : mid;
+                    y[1][e] = part == 0 ? lo : 0.f;
+                } else {
+                    y[0][e] = part == 0 ? hi : part == 1 ? mid : part == 2 ? lo : 0.f;
+                }
+            }
+#pragma unroll
+            for (int s = 0; s < QP; ++s)
+                q[s][i] = make_uint4(pair_of(y[s][0], y[s][1]), pair_of(y[s][2], y[s][3]), pair_of(y[s][4], y[s][5]),
+                                     pair_of(y[s][6], y[s][7]));
+        }
+    }
+
+    // Scores (over f) of rows 16 t + 4 q4 + i.
+    __device__ __forceinline__ void scores(int set, floatx4 (&c)[2]) const {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            c[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < KW; ++i) {
+                const uint32_t s = un[set].ks[t];
+                const uint4 k = bf16_word4(un[set].k[t][i], DH == 256 && i >= KW / 2 ? s << 15 : s << 23);
+#pragma unroll
+                for (int j = 0; j < QP; ++j) c[t] = mfma_bf16(k, q[j][i], c[t]);
+            }
+        }
+    }
+
+    // Has the sums finished here rather than behind the next loads, which would
+    // keep this unit's registers and put those loads in others, to be moved (and
+    // so waited for) at the end of a turn.
+    __device__ __forceinline__ void settle() {
+#pragma unroll
+        for (int j = 0; j < VB; ++j) asm volatile("" : "+v"(acc[j]));
+        asm volatile("" : "+v"(l));
+    }
+
+    // The unit's share of l and acc.  Rows n and up neither count in the maximum nor
+    // weigh anything.
+    __device__ __forceinline__ void add(int set, const floatx4 (&c)[2], int n) {
+        float x[8];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float y = c[t][i];
+                y += dpp_sum_operand<0x128>(y);
+                if constexpr (G <= 4) y += dpp_sum_operand<0x124>(y);
+                if constexpr (G <= 2) y += dpp_sum_operand<0x122>(y);
+                if constexpr (G == 1) y += dpp_sum_operand<0x121>(y);
+                x[4 * t + i] = y;
+            }
+        float top = rounded_product(fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
+                                          fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))), f);
+        const auto live = [&](int e) { return (e >> 2) * 16 + 4 * q4 + (e & 3) < n; };
+        if (__builtin_expect(n < kUnit4, 0)) {
+            top = made_here(kNoMax);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = live(e) ? fmaxf(top, rounded_product(x[e], f)) : top;
+        }
+        float mp = m, by = f;
+        if (__builtin_expect(__any(top > limit), 0)) {
+            const float mn = fmaxf(m, combine_xor32<OpMax>(combine_xor16<OpMax>(top)));
+            const float alpha = fast_exp2(m - mn);  // 0 from kNoMax, where l and acc are 0
+            const bool sums = __any(m != made_here(kNoMax));  // not at a wave's first unit
+            m = mn;
+            const bool far = __builtin_amdgcn_frexp_expf(m) > kFarExp;
+            limit = far ? -INFINITY : m + kMaxSlack;  // far maxima come here with every unit
+            if (sums) {
+                float al[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) al[i] = __shfl(alpha, 4 * q4 + i);  // of row 4 q4 + i
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    l[i] *= al[i];
+#pragma unroll
+                    for (int j = 0; j < VB; ++j) acc[j][i] *= al[i];
+                }
+            }
+            mp = far ? 0.f : m;
+            // Below 2^22 the argument x f - m is off by half the spacing of x f at most.
+            // Above, the exact product may lie far from the rounded one that m is.
+            if (__builtin_expect(__any(far), 0)) {
+                by = far ? 1.f : f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = far ? product_less(x[e], f, m) : x[e];
+            }
+        }
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = fast_exp2(fmaf(x[e], by, -mp));
+        if (__builtin_expect(n < kUnit4, 0)) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = live(e) ? w[e] : 0.f;
+        }
+        // p's parts, in the half of the word that the row's dim parity has; the other half
+        // is 0 (the last part of a p near 2^-126 is subnormal and has bits there to be cut).
+        const int down = (r16 / G) & 1 ? 0 : 16;
+        const int part = r16 / (2 * G);
+        const auto slot = [&](float y) { return __float_as_uint(y) >> down; };
+        uint32_t P[PP][8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float hi = cut(w[e]), r = w[e] - hi, mid = cut(r), lo = r - mid;
+            if constexpr (G == 8) {
+                P[0][e] = slot(hi);
+                P[1][e] = slot(mid);
+                P[2][e] = slot(cut(lo));
+            } else if constexpr (G == 4) {
+                P[0][e] = slot(part ? mid : hi);
+                P[1][e] = (__float_as_uint(lo) & (part ? 0u : 0xffff0000u)) >> down;
+            } else {
+                P[0][e] = slot(part == 0 ? hi : part == 1 ? mid : part == 2 ? cut(lo) : 0.f);
+            }
+        }
+        constexpr uint32_t one = 0x3f803f80u;
+        const uint4 ones = make_uint4(one, one, one, one);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            uint32_t s[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] = un[set].vs[4 * t + i] << 23;
+#pragma unroll
+            for (int h = 0; h < PP; ++h) {
+                const uint4 p = make_uint4(P[h][4 * t], P[h][4 * t + 1], P[h][4 * t + 2], P[h][4 * t + 3]);
+                l = mfma_bf16(p, ones, l);
+            }
+            const auto product = [&](auto byte) {
+                constexpr int J = decltype(byte)::value;
+                const uint4 y = make_uint4(bf16_pair4<J & 3>(un[set].v[4 * t][J >> 2], s[0]),
+                                           bf16_pair4<J & 3>(un[set].v[4 * t + 1][J >> 2], s[1]),
+                                           bf16_pair4<J & 3>(un[set].v[4 * t + 2][J >> 2], s[2]),
+                                           bf16_pair4<J & 3>(un[set].v[4 * t + 3][J >> 2], s[3]));
+#pragma unroll
+                for (int h = 0; h < PP; ++h) {
+                    const uint4 p = make_uint4(P[h][4 * t], P[h][4 * t + 1], P[h][4 * t + 2], P[h][4 * t + 3]);
+                    acc[J] = mfma_bf16(p, y, acc[J]);
+                }
+            };
+            product(std::integral_constant<int, 0>{});
+            product(std::integral_constant<int, 1>{});
+            if constexpr (VB >= 4) {
+                product(std::integral_constant<int, 2>{});
+                product(std::integral_constant<int, 3>{});
+            }
+            if constexpr (VB == 8) {
+                product(std::integral_constant<int, 4>{});
+                product(std::integral_constant<int, 5>{});
+                product(std::integral_constant<int, 6>{});
+                product(std::integral_constant<int, 7>{});
+            }
+        }
+    }
+
+    // A row-tile value (rows 4 q4 + i) summed over the parts: put(g, parity, value)
+    // on the lanes that hold one.
+    template <class Put>
+    __device__ __forceinline__ void over_parts(const floatx4 &a, Put &&put) const {
+        if constexpr (G == 8) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) put(4 * (q4 & 1) + i, q4 >> 1, a[i]);
+        } else if constexpr (G == 4) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float t = combine_xor32<OpSum>(a[i]);
+                if (q4 < 2) put(i, q4, t);
+            }
+        } else if constexpr (G == 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float t = combine_xor32<OpSum>(combine_xor16<OpSum>(a[i]));
+                if (q4 == 0) put(i & 1, i >> 1, t);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float t = combine_xor32<OpSum>(combine_xor16<OpSum>(a[i] + a[i + 2]));
+                if (q4 == 0) put(0, i, t);
+            }
+        }
+    }
+};
+
+template <int DH, int G>
+constexpr int kMinWaves4 = 2;
+
+// decode4_kernel's parameter list as it lies in the kernarg segment: each where its
+// alignment puts it, as in a struct.
+struct Args4 {
+    const void *cme_k, *cme_v;
+    void *win_k, *win_v;
+    int k, W, N, Hkv, chunk, info;
+    Decode4Params p;
+};
+typedef void (*Kernel4)(const void *, const void *, void *, void *, int, int, int, int, int, int, Decode4Params);
+static_assert(sizeof(Args4) == 4 * sizeof(void *) + 6 * sizeof(int) + sizeof(Decode4Params) &&
+                  std::is_trivially_copyable_v<Decode4Params>,
+              "Args4 holds Kernel4's parameters, in its order and without gaps");
+
+// The last parameter, loaded here and not before (the compiler would load it at
+// the kernel's start and wait for it there); fields that nothing uses are not.
+__device__ __forceinline__ Decode4Params late_params() {
+    typedef const __attribute__((address_space(4))) Args4 *Ptr;
+    Ptr at = (Ptr)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    Decode4Params p;
+    p.q = at->p.q;
+    p.cme_ks = at->p.cme_ks;
+    p.cme_vs = at->p.cme_vs;
+    p.win_ks = at->p.win_ks;
+    p.win_vs = at->p.win_vs;
+    p.win_count = at->p.win_count;
+    p.new_k = at->p.new_k;
+    p.new_v = at->p.new_v;
+    p.new_bf16 = at->p.new_bf16;
+    p.out = at->p.out;
+    p.part_ml = at->p.part_ml;
+    p.part_acc = at->p.part_acc;
+    p.pair_counter = at->p.pair_counter;
+    p.seq_counter = at->p.seq_counter;
+    p.Hq = at->p.Hq;
+    p.qscale = at->p.qscale;
+    p.cme_k = at->p.cme_k;
+    p.cme_v = at->p.cme_v;
+    p.idx = at->p.idx;
+    p.k_len = at->p.k_len;
+    p.win_k = at->p.win_k;
+    p.win_v = at->p.win_v;
+    p.k = at->p.k;
+    p.W = at->p.W;
+    p.B = at->p.B;
+    p.Hkv = at->p.Hkv;
+    p.N = at->p.N;
+    p.T_new = at->p.T_new;
+    p.S = at->p.S;
+    p.chunk = at->p.chunk;
+    p.new_split = at->p.new_split;
+    p.waves = at->p.waves;
+    return p;
+}
+
+// The ring units that an append of T_new rows at slot0 writes: consecutive from
+// first, round the ring's nu units.
+struct TouchedUnits {
+    int first, count, nu;
+    __device__ __forceinline__ void set(int slot0, int T_new, int W) {
+        nu = (int)(((unsigned)W + kUnit4 - 1u) / kUnit4);
+        first = slot0 / kUnit4;
+        const int room = W - slot0;  // slots up to the ring's end
+        if (T_new <= room) count = (slot0 + T_new - 1) / kUnit4 - first + 1;
+        else count = min(nu, nu - first + (T_new - room - 1) / kUnit4 + 1);
+    }
+    __device__ __forceinline__ int unit(int i) const { return first + i < nu ? first + i : first + i - nu; }
+    __device__ __forceinline__ bool has(int j) const {
+        const int d = j - first;
+        return (d < 0 ? d + nu : d) < count;
+    }
+};
+
+// Appended rows of one (sequence, kv head) into its ring.
+template <typename T, int DH, int NT>
+__device__ __forceinline__ void append_rows(const void *new_k, const void *new_v, size_t src, const Row4 &k, const Row4 &v,
+                                            int slot0, int T_new, int W) {
+    constexpr int shift = DH == 64 ? 3 : DH == 128 ? 4 : 5;
+    for (int i = threadIdx.x; i < T_new << (shift + 1); i += NT) {  // whole quads
+        const bool is_v = i >= T_new << shift;
+        const int e = is_v ? i - (T_new << shift) : i;
+        const int slot = slot0 + (e >> shift);
+        Raw8<T> raw;
+        raw.load(static_cast<const T *>(is_v ? new_v : new_k) + src + (size_t)e * 8);
+        (is_v ? v : k).put(slot < W ? slot : slot - W, e & ((1 << shift) - 1), shift, raw, true);
+    }
+}
+
+// The leading arguments (Args4's, one by one) arrive in SGPRs at wave launch,
+// as decode_kernel's do.
+template <int NW, int DH, int G>
+__global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kernel(const void *cme_k, const void *cme_v,
+                                                                                  void *win_k, void *win_v, int k,
+                                                                                  int W, int N, int Hkv, int chunk,
+                                                                                  int info, Decode4Params pm) {
+    const int S = info & 0xFF;
+    const bool own = (info >> 8) & 1;
+    const int s = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int kb = k;
+    if ((info >> 10) & 1) {  // k_len is given
+        const int v = pm.k_len[b];
+        kb = v < 0 ? 0 : (v > k ? k : v);
+    }
+    // Units: the pool's, then the ring's in physical slot order.
+    const int pool_units = (kb + kUnit4 - 1) / kUnit4;
+    const int units = pool_units + (int)(((unsigned)W + kUnit4 - 1) / kUnit4);
+    int u = s * chunk, end = min(u + chunk, units);
+    if (s >= S - 1 - (own ? 1 : 0)) end = units;
+    if (own && s == S - 1) u = units;
+
+    const size_t pair = (size_t)b * Hkv + kvh;
+    const uint8_t *pk = static_cast<const uint8_t *>(cme_k) + pair * (size_t)N * (DH / 2);
+    const uint8_t *pv = static_cast<const uint8_t *>(cme_v) + pair * (size_t)N * (DH / 2);
+    uint8_t *rk = static_cast<uint8_t *>(win_k) + pair * (size_t)W * (DH / 2);
+    uint8_t *rv = static_cast<uint8_t *>(win_v) + pair * (size_t)W * (DH / 2);
+    // A unit's place: its first row's codes, its number in its own array, and
+    // its live rows.
+    struct Place {
+        const uint8_t *k, *v;
+        int r, n;
+        bool pool;
+    };
+    const auto place = [&](int u, int ring_rows) {
+        const bool pool = u < pool_units;
+        const int r = pool ? u : u - pool_units;
+        const size_t o = (size_t)r * (kUnit4 * DH / 2);
+        return Place{(pool ? pk : rk) + o, (pool ? pv : rv) + o, r, min(kUnit4, (pool ? kb : ring_rows) - r * kUnit4), pool};
+    };
+    // The first unit is requested from the leading arguments alone, with all of
+    // the ring's slots as live: nothing waits for the others, nor for the count.
+    Walk4<NW, DH, G> st;
+    st.init();
+    u += wave;
+    const int u0 = u;
+    const bool some = u < end;
+    Place at{pk, pv, 0, 1, true};
+    if (some) {
+        at = place(u, W);
+        st.load_k(0, at.k, at.n);
+        st.load_v(0, at.v, at.n);
+    }
+    in_order();
+    Decode4Params p = late_params();
+    p.k = k;
+    p.W = W;
+    p.N = N;
+    p.Hkv = Hkv;
+    p.S = S;
+    p.T_new = (int)((unsigned)info >> 16);
+    const uint8_t *pks = p.cme_ks + pair * (size_t)N * (DH / 32), *pvs = p.cme_vs + pair * (size_t)N * (DH / 32);
+    uint8_t *rks = p.win_ks + pair * (size_t)W * (DH / 32), *rvs = p.win_vs + pair * (size_t)W * (DH / 32);
+    const auto scales_k = [&](const Place &at) { return (at.pool ? pks : rks) + (size_t)at.r * (kUnit4 * DH / 32); };
+    const auto scales_v = [&](const Place &at) { return (at.pool ? pvs : rvs) + (size_t)at.r * (kUnit4 * DH / 32); };
+
+    RingCount cnt{0, false};
+    int filled = 0;  // ring slots that hold a key of this step
+    TouchedUnits tu{0, 0, 1};
+    bool ready = false;
+    // q split, and what follows from the count, once both have been requested.
+    const auto start = [&]() {
+        ready = true;
+        st.split_q(p);
+        const int c = cnt.value();
+        filled = (int)min((long long)c + p.T_new, (long long)W);
+        if (p.T_new > 0 && W > 0) tu.set(c % W, p.T_new, W);
+        end = min(end, pool_units + (filled + kUnit4 - 1) / kUnit4);
+    };
+    const auto touched = [&](int u) { return u >= pool_units && tu.count > 0 && tu.has(u - pool_units); };
+    const auto after = [&](int u) {  // this wave's next unit, passing by those that are being appended to
+        do u += NW;
+        while (touched(u) && u < end);
+        return u;
+    };
+
+    // The units in turn through NS register sets.  In the loop each set's next
+    // unit is requested as soon as its registers are free, always: branches
+    // around loads would have the waits count for the path without them.  Where
+    // there is none left, the last unit is requested again, of which no row
+    // counts.  The last NS units are worked off after the loop.
+    constexpr int NS = kSets4<DH, G>;
+    if (some) {
+        int n[NS];
+        st.load_ks(0, scales_k(at), at.n);
+        st.load_vs(0, scales_v(at), at.n);
+        in_order();  // before q, whose wait so covers the scales' too
+        st.request_q(p, b, kvh);
+        cnt.load(W > 0 ? p.win_count : nullptr, b);
+        n[0] = at.n;
+#pragma unroll
+        for (int i = 1; i < NS; ++i) {
+            n[i] = 0;
+            if (u + NW < end) {
+                u += NW;
+                at = place(u, W);
+                in_order();
+                st.load_k(i, at.k, at.n);
+                st.load_ks(i, scales_k(at), at.n);
+                in_order();
+                st.load_v(i, at.v, at.n);
+                st.load_vs(i, scales_v(at), at.n);
+                n[i] = at.n;
+            }
+        }
+        start();
+        // A unit among them that is being appended to or not filled: once more
+        // from the first, as it should have been.
+        bool again = false;
+        for (int i = 0, v = u0; i < NS; ++i, v += NW)
+            again |= v >= pool_units && n[i] > 0 && (touched(v) || v >= end || place(v, filled).n != n[i]);
+        if (__builtin_expect(again, 0)) {
+            u = u0;
+            if (touched(u)) u = after(u);
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                if (i > 0 && u < end) u = after(u);
+                if (u < end) at = place(u, filled);
+                st.load_k(i, at.k, at.n);
+                st.load_ks(i, scales_k(at), at.n);
+                st.load_v(i, at.v, at.n);
+                st.load_vs(i, scales_v(at), at.n);
+                n[i] = u < end ? at.n : 0;
+            }
+            __builtin_amdgcn_s_waitcnt(0);  // so that the loop's waits need not allow for this path
+        }
+        u = u < end ? after(u) : u;
+#pragma unroll 1
+        while (u < end) {
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                floatx4 c[2];
+                st.scores(i, c);
+                const bool more = u < end;
+                if (more) at = place(u, filled);
+                in_order();
+                st.load_k(i, at.k, at.n);
+                st.load_ks(i, scales_k(at), at.n);
+                in_order();
+                st.add(i, c, n[i]);
+                st.settle();
+                in_order();
+                st.load_v(i, at.v, at.n);
+                st.load_vs(i, scales_v(at), at.n);
+                n[i] = more ? at.n : 0;
+                u = more ? after(u) : u;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            if (n[i] > 0) {
+                floatx4 c[2];
+                st.scores(i, c);
+                st.add(i, c, n[i]);
+            }
+        }
+    }
+    if (p.T_new > 0 && W > 0 && s == p.S - 1) {  // workgroup-uniform
+        if (!ready) {
+            st.request_q(p, b, kvh);
+            cnt.load(p.win_count, b);
+            start();
+        }
+        const int slot0 = cnt.value() % W;
+        const size_t src = pair * (size_t)p.T_new * DH;
+        const Row4 k_rows{rk, rks}, v_rows{rv, rvs};
+        if (p.new_bf16) append_rows<uint16_t, DH, NW * kWave>(p.new_k, p.new_v, src, k_rows, v_rows, slot0, p.T_new, W);
+        else append_rows<float, DH, NW * kWave>(p.new_k, p.new_v, src, k_rows, v_rows, slot0, p.T_new, W);
+        __syncthreads();  // the rows are in memory, for this workgroup's loads too
+        for (int i = wave; i < tu.count; i += NW) {
+            const int r = tu.unit(i);
+            if (r * kUnit4 >= filled) continue;
+            at = place(pool_units + r, filled);
+            st.load_k(0, at.k, at.n);
+            st.load_ks(0, scales_k(at), at.n);
+            st.load_v(0, at.v, at.n);
+            st.load_vs(0, scales_v(at), at.n);
+            floatx4 c[2];
+            st.scores(0, c);
+            st.add(0, c, at.n);
+        }
+    }
+    cnt.load(W > 0 ? p.win_count : nullptr, b);  // a wave without rows
+    const int cnt_now = cnt.value();
+
+    __shared__ __attribute__((aligned(16))) float s_acc[NW][G][DH];
+    __shared__ float s_m[NW][G], s_l[NW][G];
+    __shared__ int s_cnt[NW];
+#pragma unroll
+    for (int j = 0; j < DH / 32; ++j)
+        st.over_parts(st.acc[j], [&](int g, int odd, float x) { s_acc[wave][g][DH / 16 * st.r16 + 2 * j + odd] = x; });
+    st.over_parts(st.l, [&](int g, int odd, float x) {
+        if (st.r16 == 0 && odd == 0) s_l[wave][g] = x;
+    });
+    if (st.lane < G) s_m[wave][st.lane] = st.m;
+    if (st.lane == 0) s_cnt[wave] = cnt.raw;  // stored once the wave's count read has returned
+    __syncthreads();
+    constexpr int kThreads = NW * kWave;
+    constexpr bool kKeepNaN = true, kBySplits = true;
+    const bool bump = p.T_new > 0 && W > 0;
+    unsigned prev = ~0u;  // the sequence counter before this workgroup's arrival (one lane)
+#include "decode_finish.hpp"
+}
+
+template <int DH, int G>
+hipError_t launch2(const Decode4Params &p, hipStream_t stream) {
+    const dim3 grid(p.S, p.Hkv, p.B);
+    static_assert(std::is_same_v<decltype(&decode4_kernel<4, DH, G>), Kernel4>, "Args4 is taken from the kernel's list");
+    if (p.S < 1 || p.S > 0xFF || p.T_new < 0 || p.T_new > kFusedRows4 || (p.waves != 4 && p.waves != 8)) return hipErrorInvalidValue;
+    const int info = p.S | (p.new_split << 8) | ((p.k_len != nullptr) << 10) | (p.T_new << 16);
+#define CMC_LAUNCH(NW_)                                                                                      \
+    decode4_kernel<NW_, DH, G><<<grid, NW_ * kWave, 0, stream>>>(p.cme_k, p.cme_v, p.win_k, p.win_v, p.k, p.W, \
+                                                                 p.N, p.Hkv, p.chunk, info, p)
+    if (p.waves == 4) CMC_LAUNCH(4);
+    else CMC_LAUNCH(8);
+#undef CMC_LAUNCH
+    return hipGetLastError();
+}
+
+template <int DH>
+hipError_t launch_g(const Decode4Params &p, int G, hipStream_t stream) {
+    switch (G) {
+        case 1: return launch2<DH, 1>(p, stream);
+        case 2: return launch2<DH, 2>(p, stream);
+        case 4: return launch2<DH, 4>(p, stream);
+        case 8: return launch2<DH, 8>(p, stream);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_decode4(const Decode4Params &p, int G, int Dh, hipStream_t stream) {
+    if (p.B == 0) return hipSuccess;
+    switch (Dh) {
+        case 64: return launch_g<64>(p, G, stream);
+        case 128: return launch_g<128>(p, G, stream);
+        case 256: return launch_g<256>(p, G, stream);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace cmc

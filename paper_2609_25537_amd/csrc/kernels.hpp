@@ -124,6 +124,63 @@ DecodePlan plan_decode8(int B, int Hq, int Hkv, int Dh, int k, int W, bool appen
 constexpr int kFusedRows8 = 16;
 hipError_t launch_decode8(const Decode8Params &p, bool e4m3, int G, int Dh, hipStream_t stream);
 
+// The 4-bit cache (format: cache4.hpp).  Rows of Dh codes are counted in words of
+// eight: row_shift = log2(Dh / 8).
+struct Write4Params {
+    const void *src_k, *src_v;  // gather: [B][Hkv][src_rows][Dh] pool; append: [B][Hkv][T_new][Dh] rows
+    const int32_t *idx;         // gather: [B][idx_stride] pool rows, or nullptr: rows 0..R-1
+    int32_t *count;             // gather: [B] rows written, or nullptr: all R; append: [B] ring counts, advanced by T_new
+    uint8_t *k, *v;             // [B][Hkv][R][Dh / 2] codes
+    uint8_t *ks, *vs;           // [B][Hkv][R][Dh / 32] scales
+    int B, Hkv, R, src_rows, idx_stride, T_new;
+    int row_shift;
+};
+// Words (of K; V has as many) that an append leaves to one workgroup per sequence.
+constexpr int kAppendOneGroup4 = 1024;
+hipError_t launch_gather4(const Write4Params &p, bool bf16, hipStream_t stream);
+hipError_t launch_append4(const Write4Params &p, bool bf16, hipStream_t stream);
+
+struct Read4Params {
+    const uint8_t *k, *v;     // [B][Hkv][R][Dh / 2] codes
+    const uint8_t *ks, *vs;   // [B][Hkv][R][Dh / 32] scales
+    const int32_t *count;     // [B] rows ever written, or nullptr: R
+    void *out_k, *out_v;      // [B][Hkv][rows][Dh] fp32 or bf16
+    int B, Hkv, R, rows;      // the newest `rows` rows at most
+    int row_shift;
+};
+// Rows of a cache array: word indices of one (sequence, kv head) stay within 32 bits.
+constexpr int kCache4MaxRows = 1 << 26;
+hipError_t launch_read4(const Read4Params &p, bool bf16, hipStream_t stream);
+
+// Decode over the 4-bit cache, as Decode8Params; scales are bytes.
+struct Decode4Params : DecodeParams {
+    const uint8_t *cme_ks, *cme_vs;  // [B][Hkv][N][Dh / 32]
+    uint8_t *win_ks, *win_vs;        // [B][Hkv][W][Dh / 32]; written only for rows appended by this call
+    bool new_bf16;                   // type of new_k/v
+};
+// Rows a wave takes at a time; chunk and the plan count in these.
+constexpr int kUnit4 = 32;
+DecodePlan plan_decode4(int B, int Hq, int Hkv, int Dh, int k, int W, bool append);
+// Most appended rows that the decode kernel takes along; more are appended by a
+// launch of their own.
+constexpr int kFusedRows4 = 16;
+hipError_t launch_decode4(const Decode4Params &p, int G, int Dh, hipStream_t stream);
+
+// Norms of heads and their rotation by position.
+struct RopeParams {
+    const void *q, *k, *v;       // [B * T] tokens of Hq, Hkv, Hkv heads of Dh, tokens stride elements apart
+    long long q_stride, k_stride, v_stride;
+    const int32_t *pos;          // [B][T]
+    const float *inv_freq;       // [rot / 2]
+    const float *q_weight, *k_weight;  // [Dh], or nullptr: that array is not normed
+    void *out_q;                 // [B][T][Hq][Dh]
+    void *out_k, *out_v;         // [B][Hkv][T][Dh]
+    int B, T, Hq, Hkv, Dh, rot;
+    float eps;
+    bool interleaved;
+};
+hipError_t launch_norm_rope(const RopeParams &p, bool in_bf16, bool q_bf16, bool kv_bf16, hipStream_t stream);
+
 struct SelectParams {
     const void *sel_keys;     // [B][N][D] fp32 or bf16 (keys_bf16)
     const float *q_vec;       // [B][D]
