@@ -8,6 +8,7 @@
 #include <mutex>
 #include <stdarg.h>
 #include <stdio.h>
+#include <stdlib.h>
 #include <string.h>
 
 #include "cmc.h"
@@ -263,6 +264,28 @@ DecodePlan plan_decode8(int B, int Hq, int Hkv, int Dh, int k, int W, bool appen
 
 DecodePlan plan_decode4(int B, int Hq, int Hkv, int Dh, int k, int W, bool append) {
     static_assert(kUnit4 == kUnit8, "the plans count in the same units");
+#ifdef CMC_TUNE
+    if (const char *t = getenv("CMC_PLAN4")) {
+        DecodePlan pl;
+        int S = 1, waves = 4, own = 0;
+        sscanf(t, "%d,%d,%d", &S, &waves, &own);
+        const long long pairs = (long long)B * Hkv;
+        const long long units = ((long long)k + 31) / 32 + ((long long)W + 31) / 32;
+        const int G = Hq / Hkv;
+        long long chunk = (units + S - 1) / S;
+        pl.waves = waves;
+        chunk = (chunk + waves - 1) / waves * waves;
+        pl.S = (int)((units + chunk - 1) / chunk);
+        pl.chunk = (int)chunk;
+        pl.own_append = own && append && W > 0 && pl.S > 1;
+        const long long parts = 128;
+        pl.counter_bytes = align256((size_t)(B + pairs) * sizeof(unsigned));
+        pl.ml_bytes = align256((size_t)(pairs * parts * G * 2) * sizeof(float));
+        pl.acc_bytes = align256((size_t)(pairs * parts * G * Dh) * sizeof(float));
+        pl.total = pl.counter_bytes + pl.ml_bytes + pl.acc_bytes;
+        return pl;
+    }
+#endif
     return plan_decode8(B, Hq, Hkv, Dh, k, W, append);
 }
 

@@ -85,8 +85,11 @@ __device__ __forceinline__ uint32_t pair_of(float lo, float hi) {
 }
 
 // Units in flight per wave.
+#ifndef CMC_DECODE4_SETS
+#define CMC_DECODE4_SETS 2
+#endif
 template <int DH, int G>
-constexpr int kSets4 = G * DH > 1024 ? 1 : 2;
+constexpr int kSets4 = G * DH > 1024 ? 1 : CMC_DECODE4_SETS;
 
 template <int NW, int DH, int G>
 struct Walk4 {
@@ -99,7 +102,7 @@ struct Walk4 {
     struct Unit {
         uint32_t k[2][KW];
         uint32_t v[8][VB == 8 ? 2 : 1];
-        uint32_t ks[2], vs[8];  // scale bytes as loaded
+        uint32_t ks[2], vs[8];  // scale bytes as loaded (by rows of the tile, and rows as v's)
     } un[NS];
     float4 qx[2 * KW];        // q as loaded
     uint4 q[QP][KW];
@@ -108,11 +111,15 @@ struct Walk4 {
     float limit;              // the largest score that m may stay for
     floatx4 l, acc[VB];       // rows 4 q4 + i: (head, dim parity, part)
     int lane, r16, q4;
+    int k_turn, v_turn;       // to the lane's scales
 
     __device__ __forceinline__ void init() {
         lane = threadIdx.x & 63;
         r16 = lane & 15;
         q4 = lane >> 4;
+        // the lane's dims begin at q4 Dh / 4 of a K row, r16 Dh / 16 of a V row
+        k_turn = turn_for(DH == 64 ? q4 >> 1 : DH == 128 ? q4 : 2 * (q4 & 1));
+        v_turn = turn_for(r16 * DH / 512 % 4);
         m = kNoMax;
         limit = kNoMax;
         l = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -149,17 +156,29 @@ struct Walk4 {
             }
         }
     }
+    // Scale bytes come with their neighbours (a row's two, or four of them): narrower
+    // loads would be more, and the compiler clears the other bits of a byte at the end of
+    // a loop's turn, for which it waits.
     __device__ __forceinline__ void load_ks(int set, const uint8_t *ks, int rows) {
         Unit &n = un[set];
         const __amdgpu_buffer_rsrc_t from = bytes_at(ks, rows * (DH / 32));
-        const int o = r16 * (DH / 32) + (DH == 64 ? q4 >> 1 : DH == 128 ? q4 : 2 * q4);
+        const int o = r16 * (DH / 32) + (DH == 256 ? 4 * (q4 >> 1) : 0);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int at = o + 16 * t * (DH / 32);
-            if constexpr (DH == 256) n.ks[t] = __builtin_amdgcn_raw_buffer_load_b16(from, at, 0, 0);
-            else n.ks[t] = __builtin_amdgcn_raw_buffer_load_b8(from, at, 0, 0);
+        for (int t = 0; t < 2; ++t) n.ks[t] = scales_at(from, o + 16 * t * (DH / 32));
+    }
+    __device__ __forceinline__ static uint32_t scales_at(__amdgpu_buffer_rsrc_t from, int at) {
+        if constexpr (DH == 64) {
+            typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+            u16x2 x;  // the other half may hold anything
+            x[0] = __builtin_amdgcn_raw_buffer_load_b16(from, at, 0, 0);
+            return __builtin_bit_cast(uint32_t, x);
+        } else {
+            return __builtin_amdgcn_raw_buffer_load_b32(from, at, 0, 0);
         }
     }
+    // A loaded word turned so that byte B is where bf16_pair4 looks for a scale.
+    __device__ __forceinline__ static int turn_for(int b) { return (8 * b + 9) & 31; }
+    __device__ __forceinline__ static uint32_t turned(uint32_t w, int by) { return __builtin_amdgcn_alignbit(w, w, by); }
     __device__ __forceinline__ void load_v(int set, const uint8_t *v, int rows) {
         Unit &n = un[set];
         const __amdgpu_buffer_rsrc_t from = bytes_at(v, rows * (DH / 2));
@@ -168,7 +187,10 @@ struct Walk4 {
         for (int j = 0; j < 8; ++j) {
             const int at = o + ((j >> 2) * 16 + (j & 3)) * (DH / 2);
             if constexpr (VB == 2) {
-                n.v[j][0] = __builtin_amdgcn_raw_buffer_load_b16(from, at, 0, kNonTemporal);
+                typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+                u16x2 x;  // the other half may hold anything
+                x[0] = __builtin_amdgcn_raw_buffer_load_b16(from, at, 0, kNonTemporal);
+                n.v[j][0] = __builtin_bit_cast(uint32_t, x);
             } else if constexpr (VB == 4) {
                 n.v[j][0] = __builtin_amdgcn_raw_buffer_load_b32(from, at, 0, kNonTemporal);
             } else {
@@ -181,10 +203,18 @@ struct Walk4 {
     __device__ __forceinline__ void load_vs(int set, const uint8_t *vs, int rows) {
         Unit &n = un[set];
         const __amdgpu_buffer_rsrc_t from = bytes_at(vs, rows * (DH / 32));
-        const int o = 4 * q4 * (DH / 32) + r16 * DH / 512;  // the lane's dims begin at r16 Dh / 16
+        const int o = 4 * q4 * (DH / 32) + (DH == 256 ? 4 * (r16 >> 3) : 0);
+        if constexpr (DH == 128) {  // four rows lie in 16 bytes
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            n.vs[j] = __builtin_amdgcn_raw_buffer_load_b8(from, o + ((j >> 2) * 16 + (j & 3)) * (DH / 32), 0, 0);
+            for (int t = 0; t < 2; ++t) {
+                const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(from, o + 16 * t * (DH / 32), 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) n.vs[4 * t + i] = x[i];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) n.vs[j] = scales_at(from, o + ((j >> 2) * 16 + (j & 3)) * (DH / 32));
+        }
     }
 
     // The lane's quarter of its head's q.
@@ -247,8 +277,8 @@ struct Walk4 {
             c[t] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < KW; ++i) {
-                const uint32_t s = un[set].ks[t];
-                const uint4 k = bf16_word4(un[set].k[t][i], DH == 256 && i >= KW / 2 ? s << 15 : s << 23);
+                const uint32_t s = turned(un[set].ks[t], DH == 256 && i >= KW / 2 ? k_turn + 8 & 31 : k_turn);
+                const uint4 k = bf16_word4(un[set].k[t][i], s);
 #pragma unroll
                 for (int j = 0; j < QP; ++j) c[t] = mfma_bf16(k, q[j][i], c[t]);
             }
@@ -348,7 +378,7 @@ struct Walk4 {
         for (int t = 0; t < 2; ++t) {
             uint32_t s[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[i] = un[set].vs[4 * t + i] << 23;
+            for (int i = 0; i < 4; ++i) s[i] = turned(un[set].vs[4 * t + i], v_turn);
 #pragma unroll
             for (int h = 0; h < PP; ++h) {
                 const uint4 p = make_uint4(P[h][4 * t], P[h][4 * t + 1], P[h][4 * t + 2], P[h][4 * t + 3]);
