@@ -100,16 +100,18 @@ __device__ __forceinline__ uint32_t quantise4(const float (&x)[8], uint32_t &byt
 // log2(Dh / 8).
 struct Row4 {
     uint8_t *codes, *scales;
+    __device__ __forceinline__ void store(size_t row, int word, int shift, uint32_t w, uint32_t byte) const {
+        reinterpret_cast<uint32_t *>(codes)[(row << shift) + word] = w;
+        if ((word & 3) == 0) scales[(row << (shift - 2)) + (word >> 2)] = (uint8_t)byte;
+    }
     // To be called by whole quads of lanes.
     template <typename T>
-    __device__ __forceinline__ void put(size_t row, int word, int shift, const Raw8<T> &raw, bool store) const {
+    __device__ __forceinline__ void put(size_t row, int word, int shift, const Raw8<T> &raw, bool live) const {
         float x[8];
         raw.widen(x);
         uint32_t byte;
         const uint32_t w = quantise4(x, byte);
-        if (!store) return;
-        reinterpret_cast<uint32_t *>(codes)[(row << shift) + word] = w;
-        if ((word & 3) == 0) scales[(row << (shift - 2)) + (word >> 2)] = (uint8_t)byte;
+        if (live) store(row, word, shift, w, byte);
     }
 };
 

@@ -1074,7 +1074,7 @@ cmc_status decode4_impl(const char *fn, const float *q, const uint8_t *cme_k, co
         misaligned(k_len) || misaligned(win_k) || misaligned(win_v) || misaligned(win_ks) || misaligned(win_vs) ||
         misaligned(win_count) || misaligned(out) || misaligned(workspace) || misaligned(new_k) || misaligned(new_v))
         return fail(CMC_ERR_UNSUPPORTED, "%s: every pointer must be 16-byte aligned", fn);
-    const bool fused = T_new > 0 && T_new <= cmc::kFusedRows4;
+    const bool fused = T_new > 0 && T_new <= cmc::fused_rows4(Dh);
     const cmc::DecodePlan pl = cmc::plan_decode4(B, Hq, Hkv, Dh, k, W, fused);
     const size_t need = cmc_decode_q4_workspace_bytes(B, Hq, Hkv, Dh, k, W);
     if (!workspace || workspace_bytes < need)

@@ -28,9 +28,10 @@
 // of 2^22 and more, where fp32 no longer resolves that, move with every unit and have
 // their weights' arguments subtracted first.
 //
-// Fused append: the last split (one of its own where the plan says so) writes the
-// appended rows, then attends over the ring units that hold them; every other split
-// leaves those units out.  Publication, merge and the count's advance are
+// Fused append: every workgroup requests the appended rows with its first unit; those
+// whose part of the ring takes some of them quantise them before their walk, to memory
+// and to LDS, and take them from there in the units that hold them: nothing waits for a
+// store, and no unit is read twice.  Publication, merge and the count's advance are
 // decode_finish.hpp's.
 #include <type_traits>
 
@@ -73,15 +74,24 @@ __device__ __forceinline__ void in_order() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
+// A barrier that orders LDS alone: loads and stores to memory stay in flight.
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0) only: vmcnt and expcnt at their maxima
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 __device__ __forceinline__ floatx4 mfma_bf16(const uint4 &a, const uint4 &b, const floatx4 &c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
 // x's leading 8 bits, as a float.
 __device__ __forceinline__ float cut(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
-// Two parts of 8 bits side by side.
-__device__ __forceinline__ uint32_t pair_of(float lo, float hi) {
-    return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302);
+// The leading 8 bits of two numbers side by side, or (kNone) nothing.
+constexpr uint32_t kTops = 0x07060302, kNone = 0x0c0c0c0c;
+__device__ __forceinline__ uint32_t pair_of(float lo, float hi, uint32_t take) {
+    return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), take);
 }
 
 // Units in flight per wave.
@@ -90,6 +100,48 @@ __device__ __forceinline__ uint32_t pair_of(float lo, float hi) {
 #endif
 template <int DH, int G>
 constexpr int kSets4 = G * DH > 1024 ? 1 : CMC_DECODE4_SETS;
+
+// A word of eight dims of the appended rows for each thread, K's in the first half of the
+// workgroup and V's in the second, requested early (fp32 as two loads, bf16 as one and
+// one of nothing).
+template <int DH, int NT>
+struct NewRows {
+    static constexpr int kShift = DH == 64 ? 3 : DH == 128 ? 4 : 5;
+    uint4 r[2];
+    __device__ __forceinline__ static bool is_v() { return threadIdx.x >= NT / 2; }  // whole waves
+    __device__ __forceinline__ static int word() { return threadIdx.x & (NT / 2 - 1); }
+    __device__ __forceinline__ void request(const Decode4Params &p, size_t pair) {
+        constexpr int untyped = 0x00027000;
+        const int bytes = p.T_new * DH * (p.new_bf16 ? 2 : 4);
+        const char *at = static_cast<const char *>(is_v() ? p.new_v : p.new_k) + pair * (size_t)bytes;
+        at = reinterpret_cast<const char *>(uniform(reinterpret_cast<uint64_t>(at)));
+        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at), 0, bytes, untyped);
+        const int o = word() * (p.new_bf16 ? 16 : 32);
+        const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(from, o, 0, 0);
+        const u32x4 y = __builtin_amdgcn_raw_buffer_load_b128(from, p.new_bf16 ? bytes : o + 16, 0, 0);
+        r[0] = make_uint4(x[0], x[1], x[2], x[3]);
+        r[1] = make_uint4(y[0], y[1], y[2], y[3]);
+    }
+    __device__ __forceinline__ static uint64_t uniform(uint64_t x) {
+        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+        return (uint64_t)hi << 32 | lo;
+    }
+    __device__ __forceinline__ void widen(bool bf16, float (&x)[8]) const {
+        float a[4], b[4], c[8];
+        Vec16<float>::widen(r[0], a);
+        Vec16<float>::widen(r[1], b);
+        Vec16<uint16_t>::widen(r[0], c);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = bf16 ? c[e] : e < 4 ? a[e & 3] : b[e & 3];
+    }
+};
+
+// The appended rows in 4 bits as the ring holds them, [0] K's and [1] V's.
+template <int DH>
+struct NewCodes {
+    uint32_t codes[2][fused_rows4(DH)][DH / 8];
+    __attribute__((aligned(16))) uint8_t scales[2][fused_rows4(DH)][DH / 32];
+};
 
 template <int NW, int DH, int G>
 struct Walk4 {
@@ -217,6 +269,44 @@ struct Walk4 {
         }
     }
 
+    // A ring unit loaded before it was known which rows it holds: rows that were appended
+    // this call from LDS (row `first` of the ring is the unit's first, slot0 the first
+    // appended one's), and V's rows from n on, which weigh nothing but may hold NaN, as 0.
+    __device__ __forceinline__ void amend(int set, const NewCodes<DH> &fresh, int first, int slot0, int T_new, int W, int n) {
+        Unit &x = un[set];
+        const auto which = [&](int row) {  // among the appended rows
+            const int a = first + row - slot0;
+            return a < 0 ? a + W : a;
+        };
+        const auto scale_word = [&](int kv, int a, int at) -> uint32_t {
+            const uint8_t *from = &fresh.scales[kv][a][at];
+            if constexpr (DH == 64) return *reinterpret_cast<const uint16_t *>(from);
+            else return *reinterpret_cast<const uint32_t *>(from);
+        };
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int a = which(16 * t + r16);
+            if (a < T_new) {
+#pragma unroll
+                for (int i = 0; i < KW; ++i) x.k[t][i] = fresh.codes[0][a][KW * q4 + i];
+                x.ks[t] = scale_word(0, a, DH == 256 ? 4 * (q4 >> 1) : 0);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int row = (j >> 2) * 16 + 4 * q4 + (j & 3), a = which(row);
+            if (a < T_new) {
+                const uint8_t *from = reinterpret_cast<const uint8_t *>(fresh.codes[1][a]) + VB * r16;
+                if constexpr (VB == 2) x.v[j][0] = *reinterpret_cast<const uint16_t *>(from);
+                else
+#pragma unroll
+                    for (int i = 0; i < VB / 4; ++i) x.v[j][i] = reinterpret_cast<const uint32_t *>(from)[i];
+                x.vs[j] = scale_word(1, a, DH == 256 ? 4 * (r16 >> 3) : 0);
+            }
+            if (row >= n) x.vs[j] = 0;  // 2^-127 times any code
+        }
+    }
+
     // The lane's quarter of its head's q.
     __device__ __forceinline__ void request_q(const DecodeParams &p, int b, int kvh) {
         const float *qp = p.q + ((size_t)b * p.Hq + (size_t)kvh * G + (r16 % G)) * DH + 8 * KW * q4;
@@ -229,7 +319,6 @@ struct Walk4 {
     // scores back, q takes a share, so that neither f nor the products are subnormal.
     __device__ __forceinline__ void split_q(const DecodeParams &p) {
         float x[8 * KW];
-        uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < 2 * KW; ++i) {
             x[4 * i] = qx[i].x;
@@ -237,36 +326,46 @@ struct Walk4 {
             x[4 * i + 2] = qx[i].z;
             x[4 * i + 3] = qx[i].w;
         }
+        float top = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8 * KW; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
-        const auto a = __builtin_amdgcn_permlane16_swap(top, top, false, false);
-        top = max((uint32_t)a[0], (uint32_t)a[1]);
-        const auto c = __builtin_amdgcn_permlane32_swap(top, top, false, false);
-        top = max((uint32_t)c[0], (uint32_t)c[1]);
-        const int qe = (int)(top >> 23) - 127, se = __builtin_amdgcn_frexp_expf(p.qscale);
+        for (int e = 0; e < 8 * KW; ++e) top = fmaxf(top, fabsf(x[e]));
+        top = combine_xor32<OpMax>(combine_xor16<OpMax>(top));
+        const int qe = (int)(__float_as_uint(top) >> 23) - 127, se = __builtin_amdgcn_frexp_expf(p.qscale);
         const int sum = qe + se;
         const int to = sum > 60 ? min(sum - 72, 60) : sum < -100 ? max(sum + 88, -72) : -12;
         f = ldexpf(__builtin_amdgcn_frexp_mantf(fabsf(p.qscale)), sum - to);
-        const float sign = copysignf(1.f, p.qscale);
+        const int by = to - qe, most = min(max(by, -126), 127);
+        const float mul = ldexpf(copysignf(1.f, p.qscale), most);
+#pragma unroll
+        for (int e = 0; e < 8 * KW; ++e) x[e] *= mul;
+        if (__builtin_expect(__any(by != most), 0)) {
+#pragma unroll
+            for (int e = 0; e < 8 * KW; ++e) x[e] = ldexpf(x[e], by - most);
+        }
+        // The lane's part: x less the leading parts before it, of which pair_of takes the top.
         const int part = r16 / G;
+        const float less1 = part >= 1 ? 1.f : 0.f, less2 = part >= 2 ? 1.f : 0.f;
+        const uint32_t take = part < 3 ? kTops : kNone, take_lo = part == 0 ? kTops : kNone;
 #pragma unroll
         for (int i = 0; i < KW; ++i) {
-            float y[2][8];
+            float y[QP][8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float z = ldexpf(x[8 * i + e] * sign, to - qe);
-                const float hi = cut(z), r = z - hi, mid = cut(r), lo = r - mid;
+                const float z = x[8 * i + e], r = fmaf(-less1, cut(z), z);
                 if constexpr (G == 8) {
-                    y[0][e] = part == 0 ? hi : mid;
-                    y[1][e] = part == 0 ? lo : 0.f;
+                    const float mid = z - cut(z);
+                    y[0][e] = r;
+                    y[1][e] = mid - cut(mid);
                 } else {
-                    y[0][e] = part == 0 ? hi : part == 1 ? mid : part == 2 ? lo : 0.f;
+                    y[0][e] = fmaf(-less2, cut(r), r);
                 }
             }
 #pragma unroll
-            for (int s = 0; s < QP; ++s)
-                q[s][i] = make_uint4(pair_of(y[s][0], y[s][1]), pair_of(y[s][2], y[s][3]), pair_of(y[s][4], y[s][5]),
-                                     pair_of(y[s][6], y[s][7]));
+            for (int s = 0; s < QP; ++s) {
+                const uint32_t sel = s ? take_lo : take;
+                q[s][i] = make_uint4(pair_of(y[s][0], y[s][1], sel), pair_of(y[s][2], y[s][3], sel),
+                                     pair_of(y[s][4], y[s][5], sel), pair_of(y[s][6], y[s][7], sel));
+            }
         }
     }
 
@@ -352,24 +451,28 @@ struct Walk4 {
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[e] = live(e) ? w[e] : 0.f;
         }
-        // p's parts, in the half of the word that the row's dim parity has; the other half
-        // is 0 (the last part of a p near 2^-126 is subnormal and has bits there to be cut).
-        const int down = (r16 / G) & 1 ? 0 : 16;
+        // p's parts: the top of what the leading ones leave, in the half of the word that the
+        // row's dim parity has, or nothing.
         const int part = r16 / (2 * G);
-        const auto slot = [&](float y) { return __float_as_uint(y) >> down; };
+        const uint32_t half = (r16 / G) & 1 ? 0x03020c0cu : 0x0c0c0302u;
+        const uint32_t take = part < 3 ? half : kNone, take_lo = part == 0 ? half : kNone;
+        const float less1 = part >= 1 ? 1.f : 0.f, less2 = part >= 2 ? 1.f : 0.f;
+        const auto slot = [](float y, uint32_t take) { return __builtin_amdgcn_perm(0u, __float_as_uint(y), take); };
         uint32_t P[PP][8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float hi = cut(w[e]), r = w[e] - hi, mid = cut(r), lo = r - mid;
             if constexpr (G == 8) {
-                P[0][e] = slot(hi);
-                P[1][e] = slot(mid);
-                P[2][e] = slot(cut(lo));
+                const float r = w[e] - cut(w[e]);
+                P[0][e] = slot(w[e], half);
+                P[1][e] = slot(r, half);
+                P[2][e] = slot(r - cut(r), half);
             } else if constexpr (G == 4) {
-                P[0][e] = slot(part ? mid : hi);
-                P[1][e] = (__float_as_uint(lo) & (part ? 0u : 0xffff0000u)) >> down;
+                const float r = w[e] - cut(w[e]);
+                P[0][e] = slot(part ? r : w[e], half);
+                P[1][e] = slot(r - cut(r), take_lo);
             } else {
-                P[0][e] = slot(part == 0 ? hi : part == 1 ? mid : part == 2 ? cut(lo) : 0.f);
+                const float r = fmaf(-less1, cut(w[e]), w[e]);
+                P[0][e] = slot(fmaf(-less2, cut(r), r), take);
             }
         }
         constexpr uint32_t one = 0x3f803f80u;
@@ -493,7 +596,6 @@ __device__ __forceinline__ Decode4Params late_params() {
     p.T_new = at->p.T_new;
     p.S = at->p.S;
     p.chunk = at->p.chunk;
-    p.new_split = at->p.new_split;
     p.waves = at->p.waves;
     return p;
 }
@@ -516,21 +618,6 @@ struct TouchedUnits {
     }
 };
 
-// Appended rows of one (sequence, kv head) into its ring.
-template <typename T, int DH, int NT>
-__device__ __forceinline__ void append_rows(const void *new_k, const void *new_v, size_t src, const Row4 &k, const Row4 &v,
-                                            int slot0, int T_new, int W) {
-    constexpr int shift = DH == 64 ? 3 : DH == 128 ? 4 : 5;
-    for (int i = threadIdx.x; i < T_new << (shift + 1); i += NT) {  // whole quads
-        const bool is_v = i >= T_new << shift;
-        const int e = is_v ? i - (T_new << shift) : i;
-        const int slot = slot0 + (e >> shift);
-        Raw8<T> raw;
-        raw.load(static_cast<const T *>(is_v ? new_v : new_k) + src + (size_t)e * 8);
-        (is_v ? v : k).put(slot < W ? slot : slot - W, e & ((1 << shift) - 1), shift, raw, true);
-    }
-}
-
 // The leading arguments (Args4's, one by one) arrive in SGPRs at wave launch,
 // as decode_kernel's do.
 template <int NW, int DH, int G>
@@ -539,7 +626,6 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
                                                                                   int W, int N, int Hkv, int chunk,
                                                                                   int info, Decode4Params pm) {
     const int S = info & 0xFF;
-    const bool own = (info >> 8) & 1;
     const int s = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int kb = k;
@@ -550,9 +636,8 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
     // Units: the pool's, then the ring's in physical slot order.
     const int pool_units = (kb + kUnit4 - 1) / kUnit4;
     const int units = pool_units + (int)(((unsigned)W + kUnit4 - 1) / kUnit4);
-    int u = s * chunk, end = min(u + chunk, units);
-    if (s >= S - 1 - (own ? 1 : 0)) end = units;
-    if (own && s == S - 1) u = units;
+    int u = s * chunk, end = s == S - 1 ? units : min(u + chunk, units);
+    const int from = u;
 
     const size_t pair = (size_t)b * Hkv + kvh;
     const uint8_t *pk = static_cast<const uint8_t *>(cme_k) + pair * (size_t)N * (DH / 2);
@@ -577,14 +662,10 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
     Walk4<NW, DH, G> st;
     st.init();
     u += wave;
-    const int u0 = u;
-    const bool some = u < end;
-    Place at{pk, pv, 0, 1, true};
-    if (some) {
-        at = place(u, W);
-        st.load_k(0, at.k, at.n);
-        st.load_v(0, at.v, at.n);
-    }
+    Place at{pk, pv, 0, 0, true};
+    if (u < end) at = place(u, W);
+    st.load_k(0, at.k, at.n);
+    st.load_v(0, at.v, at.n);
     in_order();
     Decode4Params p = late_params();
     p.k = k;
@@ -598,134 +679,113 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
     const auto scales_k = [&](const Place &at) { return (at.pool ? pks : rks) + (size_t)at.r * (kUnit4 * DH / 32); };
     const auto scales_v = [&](const Place &at) { return (at.pool ? pvs : rvs) + (size_t)at.r * (kUnit4 * DH / 32); };
 
-    RingCount cnt{0, false};
-    int filled = 0;  // ring slots that hold a key of this step
-    TouchedUnits tu{0, 0, 1};
-    bool ready = false;
-    // q split, and what follows from the count, once both have been requested.
-    const auto start = [&]() {
-        ready = true;
-        st.split_q(p);
-        const int c = cnt.value();
-        filled = (int)min((long long)c + p.T_new, (long long)W);
-        if (p.T_new > 0 && W > 0) tu.set(c % W, p.T_new, W);
-        end = min(end, pool_units + (filled + kUnit4 - 1) / kUnit4);
-    };
-    const auto touched = [&](int u) { return u >= pool_units && tu.count > 0 && tu.has(u - pool_units); };
-    const auto after = [&](int u) {  // this wave's next unit, passing by those that are being appended to
-        do u += NW;
-        while (touched(u) && u < end);
-        return u;
-    };
-
-    // The units in turn through NS register sets.  In the loop each set's next
-    // unit is requested as soon as its registers are free, always: branches
-    // around loads would have the waits count for the path without them.  Where
-    // there is none left, the last unit is requested again, of which no row
-    // counts.  The last NS units are worked off after the loop.
+    // The units in turn through NS register sets.  Loads are requested always, of no
+    // rows where there is nothing to load: branches around them would have the waits
+    // count for the path without them.  In the loop each set's next unit is requested as
+    // soon as its registers are free; where there is none left, the last unit again, of
+    // which no row counts.  The last NS units are worked off after the loop.
     constexpr int NS = kSets4<DH, G>;
-    if (some) {
-        int n[NS];
-        st.load_ks(0, scales_k(at), at.n);
-        st.load_vs(0, scales_v(at), at.n);
-        in_order();  // before q, whose wait so covers the scales' too
-        st.request_q(p, b, kvh);
-        cnt.load(W > 0 ? p.win_count : nullptr, b);
-        n[0] = at.n;
+    int n[NS], mine[NS];  // a set's live rows, its unit
+    RingCount cnt{0, false};
+    NewRows<DH, NW * kWave> fresh;
+    st.load_ks(0, scales_k(at), at.n);
+    st.load_vs(0, scales_v(at), at.n);
+    fresh.request(p, pair);
+    in_order();  // before q, whose wait so covers the scales' and the new rows' too
+    st.request_q(p, b, kvh);
+    cnt.load(W > 0 ? p.win_count : nullptr, b);
+    n[0] = at.n;
+    mine[0] = u;
 #pragma unroll
-        for (int i = 1; i < NS; ++i) {
-            n[i] = 0;
-            if (u + NW < end) {
-                u += NW;
-                at = place(u, W);
-                in_order();
-                st.load_k(i, at.k, at.n);
-                st.load_ks(i, scales_k(at), at.n);
-                in_order();
-                st.load_v(i, at.v, at.n);
-                st.load_vs(i, scales_v(at), at.n);
-                n[i] = at.n;
-            }
-        }
-        start();
-        // A unit among them that is being appended to or not filled: once more
-        // from the first, as it should have been.
-        bool again = false;
-        for (int i = 0, v = u0; i < NS; ++i, v += NW)
-            again |= v >= pool_units && n[i] > 0 && (touched(v) || v >= end || place(v, filled).n != n[i]);
-        if (__builtin_expect(again, 0)) {
-            u = u0;
-            if (touched(u)) u = after(u);
+    for (int i = 1; i < NS; ++i) {
+        u += NW;
+        if (u < end) at = place(u, W);
+        n[i] = u < end ? at.n : 0;
+        mine[i] = u;
+        in_order();
+        st.load_k(i, at.k, n[i]);
+        st.load_ks(i, scales_k(at), n[i]);
+        in_order();
+        st.load_v(i, at.v, n[i]);
+        st.load_vs(i, scales_v(at), n[i]);
+    }
+    st.split_q(p);
+    // What follows from the count: the ring slots that hold a key of this step, and the
+    // units that take appended rows.
+    const int count = cnt.value();
+    const int filled = (int)min((long long)count + p.T_new, (long long)W);
+    end = min(end, pool_units + (filled + kUnit4 - 1) / kUnit4);
+    const bool appends = p.T_new > 0 && W > 0;
+    const int slot0 = appends ? count % W : 0;
+    TouchedUnits tu{0, 0, 1};
+    if (appends) tu.set(slot0, p.T_new, W);
+    const auto touched = [&](int u) { return u >= pool_units && tu.has(u - pool_units); };
+    bool amends[NS];
 #pragma unroll
-            for (int i = 0; i < NS; ++i) {
-                if (i > 0 && u < end) u = after(u);
-                if (u < end) at = place(u, filled);
-                st.load_k(i, at.k, at.n);
-                st.load_ks(i, scales_k(at), at.n);
-                st.load_v(i, at.v, at.n);
-                st.load_vs(i, scales_v(at), at.n);
-                n[i] = u < end ? at.n : 0;
-            }
-            __builtin_amdgcn_s_waitcnt(0);  // so that the loop's waits need not allow for this path
+    for (int i = 0; i < NS; ++i) {
+        const int live = mine[i] < pool_units ? n[i] : mine[i] < end ? min(kUnit4, filled - (mine[i] - pool_units) * kUnit4) : 0;
+        amends[i] = touched(mine[i]) || live != n[i];
+        n[i] = live;
+    }
+    // The appended rows that fall into this workgroup's units, to memory and to LDS.
+    __shared__ NewCodes<DH> s_new;
+    bool some_here = false;
+    const auto here = [&](int ring_unit) { return pool_units + ring_unit >= from && pool_units + ring_unit < end; };
+    for (int i = 0; i < tu.count; ++i) some_here |= here(tu.unit(i));
+    if (some_here) {  // workgroup-uniform
+        const int i = fresh.word(), row = i >> fresh.kShift, word = i & ((1 << fresh.kShift) - 1);
+        float x[8];
+        fresh.widen(p.new_bf16, x);
+        uint32_t byte;
+        const uint32_t w = quantise4(x, byte);
+        const int slot = slot0 + row < W ? slot0 + row : slot0 + row - W;
+        if (row < p.T_new && here(slot / kUnit4)) {
+            const bool v = fresh.is_v();
+            Row4{v ? rv : rk, v ? rvs : rks}.store(slot, word, fresh.kShift, w, byte);
+            s_new.codes[v][row][word] = w;
+            if ((word & 3) == 0) s_new.scales[v][row][word >> 2] = (uint8_t)byte;
         }
-        u = u < end ? after(u) : u;
+        lds_barrier();
+    }
+    const auto amend = [&](int i) {
+        if (__builtin_expect(amends[i], 0))
+            st.amend(i, s_new, (mine[i] - pool_units) * kUnit4, slot0, p.T_new, W, n[i]);
+    };
+    u += NW;
 #pragma unroll 1
-        while (u < end) {
-#pragma unroll
-            for (int i = 0; i < NS; ++i) {
-                floatx4 c[2];
-                st.scores(i, c);
-                const bool more = u < end;
-                if (more) at = place(u, filled);
-                in_order();
-                st.load_k(i, at.k, at.n);
-                st.load_ks(i, scales_k(at), at.n);
-                in_order();
-                st.add(i, c, n[i]);
-                st.settle();
-                in_order();
-                st.load_v(i, at.v, at.n);
-                st.load_vs(i, scales_v(at), at.n);
-                n[i] = more ? at.n : 0;
-                u = more ? after(u) : u;
-            }
-        }
+    while (u < end) {
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
-            if (n[i] > 0) {
-                floatx4 c[2];
-                st.scores(i, c);
-                st.add(i, c, n[i]);
-            }
-        }
-    }
-    if (p.T_new > 0 && W > 0 && s == p.S - 1) {  // workgroup-uniform
-        if (!ready) {
-            st.request_q(p, b, kvh);
-            cnt.load(p.win_count, b);
-            start();
-        }
-        const int slot0 = cnt.value() % W;
-        const size_t src = pair * (size_t)p.T_new * DH;
-        const Row4 k_rows{rk, rks}, v_rows{rv, rvs};
-        if (p.new_bf16) append_rows<uint16_t, DH, NW * kWave>(p.new_k, p.new_v, src, k_rows, v_rows, slot0, p.T_new, W);
-        else append_rows<float, DH, NW * kWave>(p.new_k, p.new_v, src, k_rows, v_rows, slot0, p.T_new, W);
-        __syncthreads();  // the rows are in memory, for this workgroup's loads too
-        for (int i = wave; i < tu.count; i += NW) {
-            const int r = tu.unit(i);
-            if (r * kUnit4 >= filled) continue;
-            at = place(pool_units + r, filled);
-            st.load_k(0, at.k, at.n);
-            st.load_ks(0, scales_k(at), at.n);
-            st.load_v(0, at.v, at.n);
-            st.load_vs(0, scales_v(at), at.n);
             floatx4 c[2];
-            st.scores(0, c);
-            st.add(0, c, at.n);
+            amend(i);
+            st.scores(i, c);
+            const bool more = u < end;
+            if (more) at = place(u, filled);
+            in_order();
+            st.load_k(i, at.k, at.n);
+            st.load_ks(i, scales_k(at), at.n);
+            in_order();
+            st.add(i, c, n[i]);
+            st.settle();
+            in_order();
+            st.load_v(i, at.v, at.n);
+            st.load_vs(i, scales_v(at), at.n);
+            n[i] = more ? at.n : 0;
+            mine[i] = u;
+            amends[i] = more && touched(u);
+            u += NW;
         }
     }
-    cnt.load(W > 0 ? p.win_count : nullptr, b);  // a wave without rows
-    const int cnt_now = cnt.value();
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+        if (n[i] > 0) {
+            floatx4 c[2];
+            amend(i);
+            st.scores(i, c);
+            st.add(i, c, n[i]);
+        }
+    }
+    const int cnt_now = count;
 
     __shared__ __attribute__((aligned(16))) float s_acc[NW][G][DH];
     __shared__ float s_m[NW][G], s_l[NW][G];
@@ -750,8 +810,8 @@ template <int DH, int G>
 hipError_t launch2(const Decode4Params &p, hipStream_t stream) {
     const dim3 grid(p.S, p.Hkv, p.B);
     static_assert(std::is_same_v<decltype(&decode4_kernel<4, DH, G>), Kernel4>, "Args4 is taken from the kernel's list");
-    if (p.S < 1 || p.S > 0xFF || p.T_new < 0 || p.T_new > kFusedRows4 || (p.waves != 4 && p.waves != 8)) return hipErrorInvalidValue;
-    const int info = p.S | (p.new_split << 8) | ((p.k_len != nullptr) << 10) | (p.T_new << 16);
+    if (p.S < 1 || p.S > 0xFF || p.T_new < 0 || p.T_new > fused_rows4(DH) || (p.waves != 4 && p.waves != 8)) return hipErrorInvalidValue;
+    const int info = p.S | ((p.k_len != nullptr) << 10) | (p.T_new << 16);
 #define CMC_LAUNCH(NW_)                                                                                      \
     decode4_kernel<NW_, DH, G><<<grid, NW_ * kWave, 0, stream>>>(p.cme_k, p.cme_v, p.win_k, p.win_v, p.k, p.W, \
                                                                  p.N, p.Hkv, p.chunk, info, p)

@@ -161,9 +161,10 @@ struct Decode4Params : DecodeParams {
 // Rows a wave takes at a time; chunk and the plan count in these.
 constexpr int kUnit4 = 32;
 DecodePlan plan_decode4(int B, int Hq, int Hkv, int Dh, int k, int W, bool append);
-// Most appended rows that the decode kernel takes along; more are appended by a
+// Most appended rows that the decode kernel takes along, with a word of eight dims of K
+// for half of a workgroup's threads and one of V for the others; more are appended by a
 // launch of their own.
-constexpr int kFusedRows4 = 16;
+constexpr int fused_rows4(int Dh) { return 4 * 64 / 2 * 8 / Dh; }
 hipError_t launch_decode4(const Decode4Params &p, int G, int Dh, hipStream_t stream);
 
 // Norms of heads and their rotation by position.
