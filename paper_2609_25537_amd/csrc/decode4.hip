@@ -101,6 +101,15 @@ __device__ __forceinline__ uint32_t pair_of(float lo, float hi, uint32_t take) {
 template <int DH, int G>
 constexpr int kSets4 = G * DH > 1024 ? 1 : CMC_DECODE4_SETS;
 
+// The codes and scales of a Tier-1 block's or a ring's rows, bounded by the live ones.
+struct Array4 {
+    __amdgpu_buffer_rsrc_t k, v, ks, vs;
+};
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *at, int bytes) {
+    constexpr int untyped = 0x00027000;  // 32-bit elements, addressed by bytes
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(at), 0, bytes, untyped);
+}
+
 // A word of eight dims of the appended rows for each thread, K's in the first half of the
 // workgroup and V's in the second, requested early (fp32 as two loads, bf16 as one and
 // one of nothing).
@@ -110,12 +119,11 @@ struct NewRows {
     uint4 r[2];
     __device__ __forceinline__ static bool is_v() { return threadIdx.x >= NT / 2; }  // whole waves
     __device__ __forceinline__ static int word() { return threadIdx.x & (NT / 2 - 1); }
-    __device__ __forceinline__ void request(const Decode4Params &p, size_t pair) {
-        constexpr int untyped = 0x00027000;
-        const int bytes = p.T_new * DH * (p.new_bf16 ? 2 : 4);
+    __device__ __forceinline__ void request(const Decode4Params &p, int T_new, size_t pair) {
+        const int bytes = T_new * DH * (p.new_bf16 ? 2 : 4);
         const char *at = static_cast<const char *>(is_v() ? p.new_v : p.new_k) + pair * (size_t)bytes;
         at = reinterpret_cast<const char *>(uniform(reinterpret_cast<uint64_t>(at)));
-        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at), 0, bytes, untyped);
+        const __amdgpu_buffer_rsrc_t from = buffer_of(at, bytes);
         const int o = word() * (p.new_bf16 ? 16 : 32);
         const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(from, o, 0, 0);
         const u32x4 y = __builtin_amdgcn_raw_buffer_load_b128(from, p.new_bf16 ? bytes : o + 16, 0, 0);
@@ -179,29 +187,23 @@ struct Walk4 {
         for (int j = 0; j < VB; ++j) acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // The unit's first `rows` rows, the others as zeros, by the buffer loads'
-    // bounds: loads without branches keep the compiler's wait counts exact, and a
-    // row costs no address arithmetic (its offset is the lane's and a constant).
+    // A unit's rows are at a scalar offset in the buffers of its array, whose bounds are
+    // the array's live rows: rows past them come as zeros, and neither a row nor a unit
+    // costs address arithmetic per lane.
     static constexpr int kNonTemporal = 2;
-    __device__ __forceinline__ static __amdgpu_buffer_rsrc_t bytes_at(const uint8_t *at, int bytes) {
-        constexpr int untyped = 0x00027000;  // 32-bit elements, addressed by bytes
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(at), 0, bytes, untyped);
-    }
-    __device__ __forceinline__ void load_k(int set, const uint8_t *k, int rows) {
+    __device__ __forceinline__ void load_k(int set, const Array4 &from, int unit) {
         Unit &n = un[set];
-        const __amdgpu_buffer_rsrc_t from = bytes_at(k, rows * (DH / 2));
-        const int o = r16 * (DH / 2) + 4 * KW * q4;
+        const int o = r16 * (DH / 2) + 4 * KW * q4, at = unit * (kUnit4 * DH / 2);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int at = o + 16 * t * (DH / 2);
             if constexpr (KW == 2) {
-                const auto x = __builtin_amdgcn_raw_buffer_load_b64(from, at, 0, 0);
+                const auto x = __builtin_amdgcn_raw_buffer_load_b64(from.k, o + 16 * t * (DH / 2), at, 0);
                 n.k[t][0] = x[0];
                 n.k[t][1] = x[1];
             } else {
 #pragma unroll
                 for (int i = 0; i < KW; i += 4) {
-                    const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(from, at + 4 * i, 0, 0);
+                    const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(from.k, o + 16 * t * (DH / 2) + 4 * i, at, 0);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) n.k[t][i + e] = x[e];
                 }
@@ -211,61 +213,57 @@ struct Walk4 {
     // Scale bytes come with their neighbours (a row's two, or four of them): narrower
     // loads would be more, and the compiler clears the other bits of a byte at the end of
     // a loop's turn, for which it waits.
-    __device__ __forceinline__ void load_ks(int set, const uint8_t *ks, int rows) {
-        Unit &n = un[set];
-        const __amdgpu_buffer_rsrc_t from = bytes_at(ks, rows * (DH / 32));
+    __device__ __forceinline__ void load_ks(int set, const Array4 &from, int unit) {
         const int o = r16 * (DH / 32) + (DH == 256 ? 4 * (q4 >> 1) : 0);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) n.ks[t] = scales_at(from, o + 16 * t * (DH / 32));
+        for (int t = 0; t < 2; ++t) un[set].ks[t] = scales_at(from.ks, o + 16 * t * (DH / 32), unit * (kUnit4 * DH / 32));
     }
-    __device__ __forceinline__ static uint32_t scales_at(__amdgpu_buffer_rsrc_t from, int at) {
+    __device__ __forceinline__ static uint32_t scales_at(__amdgpu_buffer_rsrc_t from, int o, int at) {
         if constexpr (DH == 64) {
             typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
             u16x2 x;  // the other half may hold anything
-            x[0] = __builtin_amdgcn_raw_buffer_load_b16(from, at, 0, 0);
+            x[0] = __builtin_amdgcn_raw_buffer_load_b16(from, o, at, 0);
             return __builtin_bit_cast(uint32_t, x);
         } else {
-            return __builtin_amdgcn_raw_buffer_load_b32(from, at, 0, 0);
+            return __builtin_amdgcn_raw_buffer_load_b32(from, o, at, 0);
         }
     }
-    // A loaded word turned so that byte B is where bf16_pair4 looks for a scale.
+    // A loaded word turned so that byte b is where bf16_pair4 looks for a scale.
     __device__ __forceinline__ static int turn_for(int b) { return (8 * b + 9) & 31; }
     __device__ __forceinline__ static uint32_t turned(uint32_t w, int by) { return __builtin_amdgcn_alignbit(w, w, by); }
-    __device__ __forceinline__ void load_v(int set, const uint8_t *v, int rows) {
+    __device__ __forceinline__ void load_v(int set, const Array4 &from, int unit) {
         Unit &n = un[set];
-        const __amdgpu_buffer_rsrc_t from = bytes_at(v, rows * (DH / 2));
-        const int o = 4 * q4 * (DH / 2) + VB * r16;
+        const int o = 4 * q4 * (DH / 2) + VB * r16, at = unit * (kUnit4 * DH / 2);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int at = o + ((j >> 2) * 16 + (j & 3)) * (DH / 2);
+            const int e = o + ((j >> 2) * 16 + (j & 3)) * (DH / 2);
             if constexpr (VB == 2) {
                 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
                 u16x2 x;  // the other half may hold anything
-                x[0] = __builtin_amdgcn_raw_buffer_load_b16(from, at, 0, kNonTemporal);
+                x[0] = __builtin_amdgcn_raw_buffer_load_b16(from.v, e, at, kNonTemporal);
                 n.v[j][0] = __builtin_bit_cast(uint32_t, x);
             } else if constexpr (VB == 4) {
-                n.v[j][0] = __builtin_amdgcn_raw_buffer_load_b32(from, at, 0, kNonTemporal);
+                n.v[j][0] = __builtin_amdgcn_raw_buffer_load_b32(from.v, e, at, kNonTemporal);
             } else {
-                const auto x = __builtin_amdgcn_raw_buffer_load_b64(from, at, 0, kNonTemporal);
+                const auto x = __builtin_amdgcn_raw_buffer_load_b64(from.v, e, at, kNonTemporal);
                 n.v[j][0] = x[0];
                 n.v[j][1] = x[1];
             }
         }
     }
-    __device__ __forceinline__ void load_vs(int set, const uint8_t *vs, int rows) {
+    __device__ __forceinline__ void load_vs(int set, const Array4 &from, int unit) {
         Unit &n = un[set];
-        const __amdgpu_buffer_rsrc_t from = bytes_at(vs, rows * (DH / 32));
-        const int o = 4 * q4 * (DH / 32) + (DH == 256 ? 4 * (r16 >> 3) : 0);
+        const int o = 4 * q4 * (DH / 32) + (DH == 256 ? 4 * (r16 >> 3) : 0), at = unit * (kUnit4 * DH / 32);
         if constexpr (DH == 128) {  // four rows lie in 16 bytes
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(from, o + 16 * t * (DH / 32), 0, 0);
+                const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(from.vs, o + 16 * t * (DH / 32), at, 0);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) n.vs[4 * t + i] = x[i];
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) n.vs[j] = scales_at(from, o + ((j >> 2) * 16 + (j & 3)) * (DH / 32));
+            for (int j = 0; j < 8; ++j) n.vs[j] = scales_at(from.vs, o + ((j >> 2) * 16 + (j & 3)) * (DH / 32), at);
         }
     }
 
@@ -644,40 +642,32 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
     const uint8_t *pv = static_cast<const uint8_t *>(cme_v) + pair * (size_t)N * (DH / 2);
     uint8_t *rk = static_cast<uint8_t *>(win_k) + pair * (size_t)W * (DH / 2);
     uint8_t *rv = static_cast<uint8_t *>(win_v) + pair * (size_t)W * (DH / 2);
-    // A unit's place: its first row's codes, its number in its own array, and
-    // its live rows.
-    struct Place {
-        const uint8_t *k, *v;
-        int r, n;
-        bool pool;
-    };
-    const auto place = [&](int u, int ring_rows) {
-        const bool pool = u < pool_units;
-        const int r = pool ? u : u - pool_units;
-        const size_t o = (size_t)r * (kUnit4 * DH / 2);
-        return Place{(pool ? pk : rk) + o, (pool ? pv : rv) + o, r, min(kUnit4, (pool ? kb : ring_rows) - r * kUnit4), pool};
-    };
-    // The first unit is requested from the leading arguments alone, with all of
-    // the ring's slots as live: nothing waits for the others, nor for the count.
+    // Wave w takes units w, w + NW, ...: unit u is number u - first of its array `a`, of
+    // `rows` live rows.  The first unit's codes are requested from the leading arguments
+    // alone, with all of the ring's slots as live: nothing waits for the others, nor for
+    // the count.
     Walk4<NW, DH, G> st;
     st.init();
     u += wave;
-    Place at{pk, pv, 0, 0, true};
-    if (u < end) at = place(u, W);
-    st.load_k(0, at.k, at.n);
-    st.load_v(0, at.v, at.n);
+    bool ring = u >= pool_units;
+    int first = ring ? pool_units : 0, rows = ring ? W : kb;
+    Array4 a;
+    const auto codes = [&](int rows) {
+        a.k = buffer_of(ring ? rk : pk, rows * (DH / 2));
+        a.v = buffer_of(ring ? rv : pv, rows * (DH / 2));
+    };
+    codes(u < end ? rows : 0);
+    st.load_k(0, a, u - first);
+    st.load_v(0, a, u - first);
     in_order();
-    Decode4Params p = late_params();
-    p.k = k;
-    p.W = W;
-    p.N = N;
-    p.Hkv = Hkv;
-    p.S = S;
-    p.T_new = (int)((unsigned)info >> 16);
-    const uint8_t *pks = p.cme_ks + pair * (size_t)N * (DH / 32), *pvs = p.cme_vs + pair * (size_t)N * (DH / 32);
-    uint8_t *rks = p.win_ks + pair * (size_t)W * (DH / 32), *rvs = p.win_vs + pair * (size_t)W * (DH / 32);
-    const auto scales_k = [&](const Place &at) { return (at.pool ? pks : rks) + (size_t)at.r * (kUnit4 * DH / 32); };
-    const auto scales_v = [&](const Place &at) { return (at.pool ? pvs : rvs) + (size_t)at.r * (kUnit4 * DH / 32); };
+    const int T_new = (int)((unsigned)info >> 16);
+    const Decode4Params early = late_params();
+    const uint8_t *pks = early.cme_ks + pair * (size_t)N * (DH / 32), *pvs = early.cme_vs + pair * (size_t)N * (DH / 32);
+    uint8_t *rks = early.win_ks + pair * (size_t)W * (DH / 32), *rvs = early.win_vs + pair * (size_t)W * (DH / 32);
+    const auto scales = [&](int rows) {
+        a.ks = buffer_of(ring ? rks : pks, rows * (DH / 32));
+        a.vs = buffer_of(ring ? rvs : pvs, rows * (DH / 32));
+    };
 
     // The units in turn through NS register sets.  Loads are requested always, of no
     // rows where there is nothing to load: branches around them would have the waits
@@ -688,37 +678,42 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
     int n[NS], mine[NS];  // a set's live rows, its unit
     RingCount cnt{0, false};
     NewRows<DH, NW * kWave> fresh;
-    st.load_ks(0, scales_k(at), at.n);
-    st.load_vs(0, scales_v(at), at.n);
-    fresh.request(p, pair);
+    scales(u < end ? rows : 0);
+    st.load_ks(0, a, u - first);
+    st.load_vs(0, a, u - first);
+    fresh.request(early, T_new, pair);
     in_order();  // before q, whose wait so covers the scales' and the new rows' too
-    st.request_q(p, b, kvh);
-    cnt.load(W > 0 ? p.win_count : nullptr, b);
-    n[0] = at.n;
+    st.request_q(early, b, kvh);
+    cnt.load(W > 0 ? early.win_count : nullptr, b);
+    n[0] = u < end ? min(kUnit4, rows - (u - first) * kUnit4) : 0;
     mine[0] = u;
 #pragma unroll
     for (int i = 1; i < NS; ++i) {
         u += NW;
-        if (u < end) at = place(u, W);
-        n[i] = u < end ? at.n : 0;
+        ring = u >= pool_units;
+        first = ring ? pool_units : 0;
+        rows = ring ? W : kb;
+        codes(u < end ? rows : 0);
+        scales(u < end ? rows : 0);
+        n[i] = u < end ? min(kUnit4, rows - (u - first) * kUnit4) : 0;
         mine[i] = u;
         in_order();
-        st.load_k(i, at.k, n[i]);
-        st.load_ks(i, scales_k(at), n[i]);
+        st.load_k(i, a, u - first);
+        st.load_ks(i, a, u - first);
         in_order();
-        st.load_v(i, at.v, n[i]);
-        st.load_vs(i, scales_v(at), n[i]);
+        st.load_v(i, a, u - first);
+        st.load_vs(i, a, u - first);
     }
-    st.split_q(p);
+    st.split_q(early);
     // What follows from the count: the ring slots that hold a key of this step, and the
     // units that take appended rows.
     const int count = cnt.value();
-    const int filled = (int)min((long long)count + p.T_new, (long long)W);
+    const int filled = (int)min((long long)count + T_new, (long long)W);
     end = min(end, pool_units + (filled + kUnit4 - 1) / kUnit4);
-    const bool appends = p.T_new > 0 && W > 0;
+    const bool appends = T_new > 0 && W > 0;
     const int slot0 = appends ? count % W : 0;
     TouchedUnits tu{0, 0, 1};
-    if (appends) tu.set(slot0, p.T_new, W);
+    if (appends) tu.set(slot0, T_new, W);
     const auto touched = [&](int u) { return u >= pool_units && tu.has(u - pool_units); };
     bool amends[NS];
 #pragma unroll
@@ -735,11 +730,11 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
     if (some_here) {  // workgroup-uniform
         const int i = fresh.word(), row = i >> fresh.kShift, word = i & ((1 << fresh.kShift) - 1);
         float x[8];
-        fresh.widen(p.new_bf16, x);
+        fresh.widen(early.new_bf16, x);
         uint32_t byte;
         const uint32_t w = quantise4(x, byte);
         const int slot = slot0 + row < W ? slot0 + row : slot0 + row - W;
-        if (row < p.T_new && here(slot / kUnit4)) {
+        if (row < T_new && here(slot / kUnit4)) {
             const bool v = fresh.is_v();
             Row4{v ? rv : rk, v ? rvs : rks}.store(slot, word, fresh.kShift, w, byte);
             s_new.codes[v][row][word] = w;
@@ -749,9 +744,18 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
     }
     const auto amend = [&](int i) {
         if (__builtin_expect(amends[i], 0))
-            st.amend(i, s_new, (mine[i] - pool_units) * kUnit4, slot0, p.T_new, W, n[i]);
+            st.amend(i, s_new, (mine[i] - pool_units) * kUnit4, slot0, T_new, W, n[i]);
     };
     u += NW;
+    const auto enter = [&](bool in_ring) {
+        ring = in_ring;
+        first = ring ? pool_units : 0;
+        rows = ring ? filled : kb;
+        codes(rows);
+        scales(rows);
+    };
+    if (u < end) enter(u >= pool_units);
+    int at = u - first, left = 0;
 #pragma unroll 1
     while (u < end) {
 #pragma unroll
@@ -760,17 +764,21 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
             amend(i);
             st.scores(i, c);
             const bool more = u < end;
-            if (more) at = place(u, filled);
+            if (more) {
+                if (__builtin_expect(!ring && u >= pool_units, 0)) enter(true);
+                at = u - first;
+            }
+            left = more ? rows - at * kUnit4 : 0;
             in_order();
-            st.load_k(i, at.k, at.n);
-            st.load_ks(i, scales_k(at), at.n);
+            st.load_k(i, a, at);
+            st.load_ks(i, a, at);
             in_order();
             st.add(i, c, n[i]);
             st.settle();
             in_order();
-            st.load_v(i, at.v, at.n);
-            st.load_vs(i, scales_v(at), at.n);
-            n[i] = more ? at.n : 0;
+            st.load_v(i, a, at);
+            st.load_vs(i, a, at);
+            n[i] = min(kUnit4, left);
             mine[i] = u;
             amends[i] = more && touched(u);
             u += NW;
@@ -785,6 +793,14 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
             st.add(i, c, n[i]);
         }
     }
+    // The rest of the arguments, which so take no registers during the walk.
+    Decode4Params p = late_params();
+    p.k = k;
+    p.W = W;
+    p.N = N;
+    p.Hkv = Hkv;
+    p.S = S;
+    p.T_new = T_new;
     const int cnt_now = count;
 
     __shared__ __attribute__((aligned(16))) float s_acc[NW][G][DH];

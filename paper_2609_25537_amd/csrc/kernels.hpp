@@ -148,8 +148,8 @@ struct Read4Params {
     int B, Hkv, R, rows;      // the newest `rows` rows at most
     int row_shift;
 };
-// Rows of a cache array: word indices of one (sequence, kv head) stay within 32 bits.
-constexpr int kCache4MaxRows = 1 << 26;
+// Rows of a cache array: byte offsets in one (sequence, kv head)'s stay within 32 bits.
+constexpr int kCache4MaxRows = 1 << 24;
 hipError_t launch_read4(const Read4Params &p, bool bf16, hipStream_t stream);
 
 // Decode over the 4-bit cache, as Decode8Params; scales are bytes.

@@ -11,7 +11,7 @@ from tests.test_abi_streams import MAIN, Stream, made  # noqa: F401  (a fixture)
 
 INV, UNS, WS, OK = cmc.CMC_ERR_INVALID_ARGUMENT, cmc.CMC_ERR_UNSUPPORTED, cmc.CMC_ERR_WORKSPACE_TOO_SMALL, cmc.CMC_OK
 FAKE = 1 << 20  # 16-byte aligned non-null address, never dereferenced: the calls fail validation first
-MANY = (1 << 26) + 1
+MANY = (1 << 24) + 1
 
 
 def _gather(**kw):

@@ -521,7 +521,7 @@ def test_empty_batch():
 def test_offsets_past_32_bits():
     """The longest cache of one head: rows near its end are written, read back and
     attended where they lie (4 GiB of codes an array)."""
-    R, Dh = 1 << 26, 128
+    R, Dh = 1 << 24, 128
     say("longest 4-bit cache")
     ring = [torch.zeros(1, 1, R, Dh // 2, dtype=torch.uint8, device=DEV) for _ in range(2)]
     ring += [torch.ones(1, 1, R, Dh // 32, dtype=torch.uint8, device=DEV) for _ in range(2)]
