@@ -5,16 +5,19 @@
 // Grid (S, Hkv, B), 4 or 8 waves.  A wave takes units of 32 rows and adds
 //   x_t = scale log2(e) <q, K_t>     p_t = 2^(x_t - m)
 //   l  += sum_t p_t                  acc += sum_t p_t V_t
-// with m a running maximum.  Both products run on MFMA with fp32 sums, with the cache's
-// values as they are; q and p are taken apart into parts that together hold fp32's 24
-// bits.
+// with m a running maximum.  Both products run on MFMA (16x16x32, bf16 in, fp32
+// sums).  bf16 holds every code times its scale exactly, and the card widens two
+// codes with their scale in one instruction, so only q and p have to be split: into
+// three bf16 parts of 8 bits each, by cutting, which together are all of fp32's 24.
 //
-// Scores (Query): A = 16 rows' K, B = q, a lane ends with the scores of one column for
-// 4 + 4 rows; column c is of head c % G.
-// P V: bf16 holds every code times its scale exactly, and the card widens two codes with
-// their scale in one instruction; p is three bf16 parts of 8 bits, by cutting.  The same
-// lanes hold p in the A layout as it stands (rows = columns before), so p crosses no
-// lane.  A code byte holds two dims of one row, and widens to the two k slots of a B word: with p in one slot and 0 in the other, a product gives one of
+// Scores: A = 16 rows' K, B = q, a lane ends with the scores of one column for 4 + 4
+// rows.  Columns are (head, part): column c holds part c / G of head c % G (eight
+// heads have room for two parts and take a second MFMA for the third), and rotates
+// within the 16 lanes add the parts, from the widest down, so that all columns of a
+// head end with the same bits.
+// P V: the same lanes hold p in the A layout as it stands (rows = columns before), so
+// p crosses no lane.  A code byte holds two dims of one row, and widens to the two k
+// slots of a B word: with p in one slot and 0 in the other, a product gives one of
 // the two dims.  So rows are (head, dim parity, part), one MFMA takes 16 keys x 32
 // dims, and no code moves between lanes or bytes.  V's rows are loaded to match: lane
 // (c, q4) takes Dh / 16 consecutive dims of rows 4 q4 .. 4 q4 + 3 and 16 + 4 q4 ..
@@ -148,159 +151,26 @@ struct NewCodes {
     __attribute__((aligned(16))) uint8_t scales[2][fused_rows4(DH)][DH / 32];
 };
 
-// A word of scale bytes turned so that byte b is where bf16_pair4 looks for a scale.
-__device__ __forceinline__ int turn_for(int b) { return (8 * b + 9) & 31; }
-__device__ __forceinline__ uint32_t turned(uint32_t w, int by) { return __builtin_amdgcn_alignbit(w, w, by); }
-
-// Scores of 16 + 16 rows against q, a lane's K words and scales as they were loaded.
-//
-// Heads of 64 and 128: the card multiplies 4-bit codes with their scales as they are
-// (16x16x128, 4 bits by 6).  q is taken apart into five parts of 6 bits (e2m3), each
-// with a power of two of its own for 32 dims: the first holds an element to 4 bits of
-// the largest of the 32, each of the others to 5 more, 24 in all.  Columns are heads,
-// 16 / G times over.  With heads of 64 the 128 dims are those of a row of each tile, of
-// which one product takes the first alone, one the second.
-template <int DH, int G>
-struct Query {
-    static constexpr int kParts = 5, kBits = 5;
-    typedef uint32_t Six __attribute__((ext_vector_type(6)));
-    typedef int Eight __attribute__((ext_vector_type(8)));
-    Six part[kParts];
-    uint32_t scale[2];  // the parts' scale bytes
-    __device__ __forceinline__ void split(float (&x)[32], int) {
-        float top = 0.f;
-#pragma unroll
-        for (int e = 0; e < 32; ++e) top = fmaxf(top, fabsf(x[e]));
-        // the largest at 2 to 4 scales, where e2m3 is spaced by a quarter of the scale
-        const int s0 = (int)(__float_as_uint(top) >> 23) - 1;
-        scale[0] = scale[1] = 0;
-#pragma unroll
-        for (int p = 0; p < kParts; ++p) {
-            typedef float Half __attribute__((ext_vector_type(16)));
-            typedef float All __attribute__((ext_vector_type(32)));
-            const int s = max(s0 - kBits * p, 1);
-            scale[p >> 2] |= (uint32_t)s << (8 * (p & 3));
-            const float by = __uint_as_float((uint32_t)s << 23);
-            Half even, odd;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                even[e] = x[2 * e];
-                odd[e] = x[2 * e + 1];
-            }
-            part[p] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, by);
-            if (p + 1 < kParts) {
-                const All back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(part[p], by);
-#pragma unroll
-                for (int e = 0; e < 32; ++e) x[e] -= back[e];
-            }
-        }
-    }
-    template <int P>
-    __device__ __forceinline__ floatx4 take(const Eight &a, uint32_t ks, const floatx4 &c) const {
-        constexpr int e2m1 = 4, e2m3 = 2;
-        const Eight b = {(int)part[P][0], (int)part[P][1], (int)part[P][2], (int)part[P][3], (int)part[P][4], (int)part[P][5], 0, 0};
-        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, e2m1, e2m3, 0, (int)ks, P & 3, (int)scale[P >> 2]);
-    }
-    template <int KT>
-    __device__ __forceinline__ void scores(const uint32_t (&k)[KT][4], const uint32_t (&ks)[KT], int turn, int q4,
-                                           floatx4 (&c)[2]) const {
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            constexpr bool both = KT == 1;  // both tiles' rows in one word: the other's as 0
-            const int i = both ? 0 : t;
-            const uint32_t mine = !both || (q4 >> 1) == t ? ~0u : 0u;
-            const Eight a = {(int)(k[i][0] & mine), (int)(k[i][1] & mine), (int)(k[i][2] & mine), (int)(k[i][3] & mine), 0, 0, 0, 0};
-            const uint32_t s = ks[i] >> turn;
-            c[t] = take<0>(a, s, floatx4{0.f, 0.f, 0.f, 0.f});
-            c[t] = take<1>(a, s, c[t]);
-            c[t] = take<2>(a, s, c[t]);
-            c[t] = take<3>(a, s, c[t]);
-            c[t] = take<4>(a, s, c[t]);
-        }
-    }
-};
-
-// Heads of 256, whose parts would fill too many registers: codes widened to bf16 with
-// their scales (exact), q as three bf16 parts, by cutting, which are all of fp32's 24
-// bits.  Column c holds part c / G of head c % G (eight heads have room for two parts
-// and take a second MFMA for the third); rotates within the 16 lanes add the parts,
-// from the widest down, so that all columns of a head end with the same bits.
-template <int G>
-struct Query<256, G> {
-    static constexpr int QP = G == 8 ? 2 : 1;  // MFMAs that the parts take
-    uint4 part[QP][8];
-    __device__ __forceinline__ void split(float (&x)[64], int r16) {
-        // The lane's part: x less the leading parts before it, of which pair_of takes the top.
-        const int mine = r16 / G;
-        const float less1 = mine >= 1 ? 1.f : 0.f, less2 = mine >= 2 ? 1.f : 0.f;
-        const uint32_t take = mine < 3 ? kTops : kNone, take_lo = mine == 0 ? kTops : kNone;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float y[QP][8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float z = x[8 * i + e], r = fmaf(-less1, cut(z), z);
-                if constexpr (G == 8) {
-                    const float mid = z - cut(z);
-                    y[0][e] = r;
-                    y[1][e] = mid - cut(mid);
-                } else {
-                    y[0][e] = fmaf(-less2, cut(r), r);
-                }
-            }
-#pragma unroll
-            for (int s = 0; s < QP; ++s) {
-                const uint32_t sel = s ? take_lo : take;
-                part[s][i] = make_uint4(pair_of(y[s][0], y[s][1], sel), pair_of(y[s][2], y[s][3], sel),
-                                        pair_of(y[s][4], y[s][5], sel), pair_of(y[s][6], y[s][7], sel));
-            }
-        }
-    }
-    __device__ __forceinline__ void scores(const uint32_t (&k)[2][8], const uint32_t (&ks)[2], int turn, int,
-                                           floatx4 (&c)[2]) const {
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            c[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint4 w = bf16_word4(k[t][i], turned(ks[t], i >= 4 ? (turn + 8) & 31 : turn));
-#pragma unroll
-                for (int j = 0; j < QP; ++j) c[t] = mfma_bf16(w, part[j][i], c[t]);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float y = c[t][i];
-                y += dpp_sum_operand<0x128>(y);
-                if constexpr (G <= 4) y += dpp_sum_operand<0x124>(y);
-                if constexpr (G <= 2) y += dpp_sum_operand<0x122>(y);
-                if constexpr (G == 1) y += dpp_sum_operand<0x121>(y);
-                c[t][i] = y;
-            }
-        }
-    }
-};
-
 template <int NW, int DH, int G>
 struct Walk4 {
-    static constexpr int KW = DH == 256 ? 8 : 4;  // words of a K row per lane
-    static constexpr int KT = DH == 64 ? 1 : 2;   // and rows
+    static constexpr int KW = DH / 32;         // words of a K row per lane, and MFMAs per 16 rows
     static constexpr int VB = DH / 32;         // bytes of a V row per lane (two dims each), and MFMAs per 16 rows
-    static constexpr int PP = G == 8 ? 3 : G == 4 ? 2 : 1;  // MFMAs that p's parts take
+    static constexpr int QP = G == 8 ? 2 : 1;  // MFMAs that q's parts take
+    static constexpr int PP = G == 8 ? 3 : G == 4 ? 2 : 1;  // and p's
     static constexpr int NS = kSets4<DH, G>;
     // Units on their way or being worked on, each in registers of its own.
     struct Unit {
-        uint32_t k[KT][KW];
+        uint32_t k[2][KW];
         uint32_t v[8][VB == 8 ? 2 : 1];
-        uint32_t ks[KT], vs[8];  // scale bytes as loaded (by rows of the tile, and rows as v's)
+        uint32_t ks[2], vs[8];  // scale bytes as loaded (by rows of the tile, and rows as v's)
     } un[NS];
     float4 qx[2 * KW];        // q as loaded
-    Query<DH, G> q;
+    uint4 q[QP][KW];
     float f;                  // |scale| log2(e) over q's power of two
     float m;                  // of head r16 % G
     float limit;              // the largest score that m may stay for
     floatx4 l, acc[VB];       // rows 4 q4 + i: (head, dim parity, part)
     int lane, r16, q4;
-    int k_word;               // the lane's first word of a K row
     int k_turn, v_turn;       // to the lane's scales
 
     __device__ __forceinline__ void init() {
@@ -308,8 +178,7 @@ struct Walk4 {
         r16 = lane & 15;
         q4 = lane >> 4;
         // the lane's dims begin at q4 Dh / 4 of a K row, r16 Dh / 16 of a V row
-        k_word = DH == 64 ? 4 * (q4 & 1) : KW * q4;
-        k_turn = DH == 256 ? turn_for(2 * (q4 & 1)) : DH == 128 ? 8 * q4 : 8 * (q4 & 1);
+        k_turn = turn_for(DH == 64 ? q4 >> 1 : DH == 128 ? q4 : 2 * (q4 & 1));
         v_turn = turn_for(r16 * DH / 512 % 4);
         m = kNoMax;
         limit = kNoMax;
@@ -324,25 +193,30 @@ struct Walk4 {
     static constexpr int kNonTemporal = 2;
     __device__ __forceinline__ void load_k(int set, const Array4 &from, int unit) {
         Unit &n = un[set];
-        const int o = k_row(0) * (DH / 2) + 4 * k_word, at = unit * (kUnit4 * DH / 2);
+        const int o = r16 * (DH / 2) + 4 * KW * q4, at = unit * (kUnit4 * DH / 2);
 #pragma unroll
-        for (int t = 0; t < KT; ++t)
+        for (int t = 0; t < 2; ++t) {
+            if constexpr (KW == 2) {
+                const auto x = __builtin_amdgcn_raw_buffer_load_b64(from.k, o + 16 * t * (DH / 2), at, 0);
+                n.k[t][0] = x[0];
+                n.k[t][1] = x[1];
+            } else {
 #pragma unroll
-            for (int i = 0; i < KW; i += 4) {
-                const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(from.k, o + 16 * t * (DH / 2) + 4 * i, at, 0);
+                for (int i = 0; i < KW; i += 4) {
+                    const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(from.k, o + 16 * t * (DH / 2) + 4 * i, at, 0);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) n.k[t][i + e] = x[e];
+                    for (int e = 0; e < 4; ++e) n.k[t][i + e] = x[e];
+                }
             }
+        }
     }
-    // The row that the lane's K word t is of.
-    __device__ __forceinline__ int k_row(int t) const { return DH == 64 ? 16 * (q4 >> 1) + r16 : 16 * t + r16; }
     // Scale bytes come with their neighbours (a row's two, or four of them): narrower
     // loads would be more, and the compiler clears the other bits of a byte at the end of
     // a loop's turn, for which it waits.
     __device__ __forceinline__ void load_ks(int set, const Array4 &from, int unit) {
-        const int o = k_row(0) * (DH / 32) + (DH == 256 ? 4 * (q4 >> 1) : 0);
+        const int o = r16 * (DH / 32) + (DH == 256 ? 4 * (q4 >> 1) : 0);
 #pragma unroll
-        for (int t = 0; t < KT; ++t) un[set].ks[t] = scales_at(from.ks, o + 16 * t * (DH / 32), unit * (kUnit4 * DH / 32));
+        for (int t = 0; t < 2; ++t) un[set].ks[t] = scales_at(from.ks, o + 16 * t * (DH / 32), unit * (kUnit4 * DH / 32));
     }
     __device__ __forceinline__ static uint32_t scales_at(__amdgpu_buffer_rsrc_t from, int o, int at) {
         if constexpr (DH == 64) {
@@ -354,6 +228,9 @@ struct Walk4 {
             return __builtin_amdgcn_raw_buffer_load_b32(from, o, at, 0);
         }
     }
+    // A loaded word turned so that byte b is where bf16_pair4 looks for a scale.
+    __device__ __forceinline__ static int turn_for(int b) { return (8 * b + 9) & 31; }
+    __device__ __forceinline__ static uint32_t turned(uint32_t w, int by) { return __builtin_amdgcn_alignbit(w, w, by); }
     __device__ __forceinline__ void load_v(int set, const Array4 &from, int unit) {
         Unit &n = un[set];
         const int o = 4 * q4 * (DH / 2) + VB * r16, at = unit * (kUnit4 * DH / 2);
@@ -392,7 +269,7 @@ struct Walk4 {
 
     // A ring unit loaded before it was known which rows it holds: rows that were appended
     // this call from LDS (row `first` of the ring is the unit's first, slot0 the first
-    // appended one's), and rows from n on, which weigh nothing but may hold NaN, as 0.
+    // appended one's), and V's rows from n on, which weigh nothing but may hold NaN, as 0.
     __device__ __forceinline__ void amend(int set, const NewCodes<DH> &fresh, int first, int slot0, int T_new, int W, int n) {
         Unit &x = un[set];
         const auto which = [&](int row) {  // among the appended rows
@@ -405,14 +282,13 @@ struct Walk4 {
             else return *reinterpret_cast<const uint32_t *>(from);
         };
 #pragma unroll
-        for (int t = 0; t < KT; ++t) {
-            const int row = k_row(t), a = which(row);
+        for (int t = 0; t < 2; ++t) {
+            const int a = which(16 * t + r16);
             if (a < T_new) {
 #pragma unroll
-                for (int i = 0; i < KW; ++i) x.k[t][i] = fresh.codes[0][a][k_word + i];
+                for (int i = 0; i < KW; ++i) x.k[t][i] = fresh.codes[0][a][KW * q4 + i];
                 x.ks[t] = scale_word(0, a, DH == 256 ? 4 * (q4 >> 1) : 0);
             }
-            if (row >= n) x.ks[t] = 0;  // 2^-127 times any code
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -425,13 +301,13 @@ struct Walk4 {
                     for (int i = 0; i < VB / 4; ++i) x.v[j][i] = reinterpret_cast<const uint32_t *>(from)[i];
                 x.vs[j] = scale_word(1, a, DH == 256 ? 4 * (r16 >> 3) : 0);
             }
-            if (row >= n) x.vs[j] = 0;
+            if (row >= n) x.vs[j] = 0;  // 2^-127 times any code
         }
     }
 
-    // The lane's part of its head's q.
+    // The lane's quarter of its head's q.
     __device__ __forceinline__ void request_q(const DecodeParams &p, int b, int kvh) {
-        const float *qp = p.q + ((size_t)b * p.Hq + (size_t)kvh * G + (r16 % G)) * DH + 8 * k_word;
+        const float *qp = p.q + ((size_t)b * p.Hq + (size_t)kvh * G + (r16 % G)) * DH + 8 * KW * q4;
 #pragma unroll
         for (int i = 0; i < 2 * KW; ++i) qx[i] = *reinterpret_cast<const float4 *>(qp + 4 * i);
     }
@@ -448,25 +324,14 @@ struct Walk4 {
             x[4 * i + 2] = qx[i].z;
             x[4 * i + 3] = qx[i].w;
         }
-        // The largest magnitude's bits, NaN above infinity: of positive numbers by signed
-        // order, of negative ones by unsigned.
-        int up = 0;
-        uint32_t down = 0;
+        float top = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8 * KW; ++e) {
-            up = max(up, __float_as_int(x[e]));
-            down = max(down, __float_as_uint(x[e]));
-        }
-        uint32_t top = max((uint32_t)up, down & 0x7fffffffu);
-        const auto a = __builtin_amdgcn_permlane16_swap(top, top, false, false);
-        top = max((uint32_t)a[0], (uint32_t)a[1]);
-        const auto c = __builtin_amdgcn_permlane32_swap(top, top, false, false);
-        top = max((uint32_t)c[0], (uint32_t)c[1]);
-        const int qe = (int)(top >> 23) - 127, se = __builtin_amdgcn_frexp_expf(p.qscale);
+        for (int e = 0; e < 8 * KW; ++e) top = fmaxf(top, fabsf(x[e]));
+        top = combine_xor32<OpMax>(combine_xor16<OpMax>(top));
+        const int qe = (int)(__float_as_uint(top) >> 23) - 127, se = __builtin_amdgcn_frexp_expf(p.qscale);
         const int sum = qe + se;
         const int to = sum > 60 ? min(sum - 72, 60) : sum < -100 ? max(sum + 88, -72) : -12;
         f = ldexpf(__builtin_amdgcn_frexp_mantf(fabsf(p.qscale)), sum - to);
-        f = top < 0x7f800000u ? f : __uint_as_float(0x7fc00000u);  // q is not finite: all of the head is NaN
         const int by = to - qe, most = min(max(by, -126), 127);
         const float mul = ldexpf(copysignf(1.f, p.qscale), most);
 #pragma unroll
@@ -475,11 +340,47 @@ struct Walk4 {
 #pragma unroll
             for (int e = 0; e < 8 * KW; ++e) x[e] = ldexpf(x[e], by - most);
         }
-        q.split(x, r16);
+        // The lane's part: x less the leading parts before it, of which pair_of takes the top.
+        const int part = r16 / G;
+        const float less1 = part >= 1 ? 1.f : 0.f, less2 = part >= 2 ? 1.f : 0.f;
+        const uint32_t take = part < 3 ? kTops : kNone, take_lo = part == 0 ? kTops : kNone;
+#pragma unroll
+        for (int i = 0; i < KW; ++i) {
+            float y[QP][8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float z = x[8 * i + e], r = fmaf(-less1, cut(z), z);
+                if constexpr (G == 8) {
+                    const float mid = z - cut(z);
+                    y[0][e] = r;
+                    y[1][e] = mid - cut(mid);
+                } else {
+                    y[0][e] = fmaf(-less2, cut(r), r);
+                }
+            }
+#pragma unroll
+            for (int s = 0; s < QP; ++s) {
+                const uint32_t sel = s ? take_lo : take;
+                q[s][i] = make_uint4(pair_of(y[s][0], y[s][1], sel), pair_of(y[s][2], y[s][3], sel),
+                                     pair_of(y[s][4], y[s][5], sel), pair_of(y[s][6], y[s][7], sel));
+            }
+        }
     }
 
-    // Scores (over f) of rows 16 t + 4 q4 + i, the same in every column of a head.
-    __device__ __forceinline__ void scores(int set, floatx4 (&c)[2]) const { q.scores(un[set].k, un[set].ks, k_turn, q4, c); }
+    // Scores (over f) of rows 16 t + 4 q4 + i.
+    __device__ __forceinline__ void scores(int set, floatx4 (&c)[2]) const {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            c[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < KW; ++i) {
+                const uint32_t s = turned(un[set].ks[t], DH == 256 && i >= KW / 2 ? k_turn + 8 & 31 : k_turn);
+                const uint4 k = bf16_word4(un[set].k[t][i], s);
+#pragma unroll
+                for (int j = 0; j < QP; ++j) c[t] = mfma_bf16(k, q[j][i], c[t]);
+            }
+        }
+    }
 
     // Has the sums finished here rather than behind the next loads, which would
     // keep this unit's registers and put those loads in others, to be moved (and
@@ -495,7 +396,16 @@ struct Walk4 {
     __device__ __forceinline__ void add(int set, const floatx4 (&c)[2], int n) {
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = c[e >> 2][e & 3];
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float y = c[t][i];
+                y += dpp_sum_operand<0x128>(y);
+                if constexpr (G <= 4) y += dpp_sum_operand<0x124>(y);
+                if constexpr (G <= 2) y += dpp_sum_operand<0x122>(y);
+                if constexpr (G == 1) y += dpp_sum_operand<0x121>(y);
+                x[4 * t + i] = y;
+            }
         float top = rounded_product(fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
                                           fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))), f);
         const auto live = [&](int e) { return (e >> 2) * 16 + 4 * q4 + (e & 3) < n; };
