@@ -8,7 +8,6 @@
 #include <mutex>
 #include <stdarg.h>
 #include <stdio.h>
-#include <stdlib.h>
 #include <string.h>
 
 #include "cmc.h"
@@ -262,31 +261,40 @@ DecodePlan plan_decode8(int B, int Hq, int Hkv, int Dh, int k, int W, bool appen
     return pl;
 }
 
-DecodePlan plan_decode4(int B, int Hq, int Hkv, int Dh, int k, int W, bool append) {
-    static_assert(kUnit4 == kUnit8, "the plans count in the same units");
-#ifdef CMC_TUNE
-    if (const char *t = getenv("CMC_PLAN4")) {
-        DecodePlan pl;
-        int S = 1, waves = 4, own = 0;
-        sscanf(t, "%d,%d,%d", &S, &waves, &own);
-        const long long pairs = (long long)B * Hkv;
-        const long long units = ((long long)k + 31) / 32 + ((long long)W + 31) / 32;
-        const int G = Hq / Hkv;
-        long long chunk = (units + S - 1) / S;
-        pl.waves = waves;
-        chunk = (chunk + waves - 1) / waves * waves;
-        pl.S = (int)((units + chunk - 1) / chunk);
-        pl.chunk = (int)chunk;
-        pl.own_append = own && append && W > 0 && pl.S > 1;
-        const long long parts = 128;
-        pl.counter_bytes = align256((size_t)(B + pairs) * sizeof(unsigned));
-        pl.ml_bytes = align256((size_t)(pairs * parts * G * 2) * sizeof(float));
-        pl.acc_bytes = align256((size_t)(pairs * parts * G * Dh) * sizeof(float));
-        pl.total = pl.counter_bytes + pl.ml_bytes + pl.acc_bytes;
-        return pl;
+// Decode over the 4-bit cache.  A unit of 32 rows costs a wave alone on its SIMD about
+// 0.65 us, more than its bytes do, so a long axis is split over all CUs; a join costs
+// about 1.7 us and 0.06 us per split that the last workgroup reads.
+//
+// - Up to 12 units, or from 160 pairs on, no split: 8 pairs of 7 units 6.8 us in one
+//   workgroup each and 8.2 in two; 160 pairs of 24 units 11.8 and 13.2.
+// - Else a wave's units and the number of splits grow alike, as the root of the length,
+//   with one workgroup per CU at most.  8 pairs: 24 units 8.2 us in 6 splits (3: 8.9),
+//   130 units 9.7 in 11 (17: 10.0, 7: 10.7), 1026 units 16.7 in 29 (43: 18.6, 20: 18.5);
+//   64 pairs: 24 units 10.1 in 3 (6: 10.7), 136 units 15.6 in 4 (7: 15.8, 3: 17.3).
+// - Eight waves only for a pair's whole axis, where a CU has one workgroup and each wave
+//   enough to walk: 256 pairs of 144 units 30.8 us (4 waves 32.9), of 48 units 17.3 (16.6);
+//   eight query heads, 192 pairs of 50 units, 16.9 (18.0).
+constexpr long long kMaxSplits4 = 127;
+DecodePlan plan_decode4(int B, int Hq, int Hkv, int Dh, int k, int W) {
+    const long long pairs = (long long)B * Hkv;
+    const long long units = ((long long)k + kUnit4 - 1) / kUnit4 + ((long long)W + kUnit4 - 1) / kUnit4;
+    const int G = Hq / Hkv;
+    DecodePlan pl;
+    long long S = 1, chunk = std::max(1LL, units);
+    if (units > 12 && pairs > 0 && pairs < 160) {
+        const long long most = std::min(256 / pairs, kMaxSplits4);
+        const long long share = (long long)(sqrt((double)units) / 4), least = (units + 4 * most - 1) / (4 * most);
+        chunk = 4 * std::max(std::max(1LL, share), least);
+        S = (units + chunk - 1) / chunk;
     }
-#endif
-    return plan_decode8(B, Hq, Hkv, Dh, k, W, append);
+    pl.waves = S == 1 && pairs <= 256 && units >= (Dh == 64 || G == 8 ? 48 : 64) ? 8 : 4;
+    pl.S = (int)S;
+    pl.chunk = (int)((chunk + pl.waves - 1) / pl.waves * pl.waves);
+    pl.counter_bytes = align256((size_t)(B + pairs) * sizeof(unsigned));
+    pl.ml_bytes = S > 1 ? align256((size_t)(pairs * S * G * 2) * sizeof(float)) : 0;
+    pl.acc_bytes = S > 1 ? align256((size_t)(pairs * S * G * Dh) * sizeof(float)) : 0;
+    pl.total = pl.counter_bytes + pl.ml_bytes + pl.acc_bytes;
+    return pl;
 }
 
 }  // namespace cmc
@@ -1075,7 +1083,7 @@ cmc_status decode4_impl(const char *fn, const float *q, const uint8_t *cme_k, co
         misaligned(win_count) || misaligned(out) || misaligned(workspace) || misaligned(new_k) || misaligned(new_v))
         return fail(CMC_ERR_UNSUPPORTED, "%s: every pointer must be 16-byte aligned", fn);
     const bool fused = T_new > 0 && T_new <= cmc::fused_rows4(Dh);
-    const cmc::DecodePlan pl = cmc::plan_decode4(B, Hq, Hkv, Dh, k, W, fused);
+    const cmc::DecodePlan pl = cmc::plan_decode4(B, Hq, Hkv, Dh, k, W);
     const size_t need = cmc_decode_q4_workspace_bytes(B, Hq, Hkv, Dh, k, W);
     if (!workspace || workspace_bytes < need)
         return fail(CMC_ERR_WORKSPACE_TOO_SMALL, "%s: workspace of %zu bytes needed, %zu given", fn, need,
@@ -1115,8 +1123,7 @@ cmc_status decode4_impl(const char *fn, const float *q, const uint8_t *cme_k, co
     p.Hkv = Hkv;
     p.N = N;
     p.T_new = T_new;
-    p.new_split = pl.own_append ? 1 : 0;
-    p.S = pl.S + p.new_split;
+    p.S = pl.S;
     p.chunk = pl.chunk;
     p.waves = pl.waves;
     p.qscale = cmc::decode_qscale(scale);
@@ -1218,8 +1225,7 @@ cmc_status cmc_cache_read_q4(const uint8_t *k4, const uint8_t *v4, const uint8_t
 
 size_t cmc_decode_q4_workspace_bytes(int B, int Hq, int Hkv, int Dh, int k, int W) {
     if (B < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || k < 0 || W < 0 || !supported_dh(Dh)) return 0;
-    return std::max(cmc::plan_decode4(B, Hq, Hkv, Dh, k, W, false).total,
-                    cmc::plan_decode4(B, Hq, Hkv, Dh, k, W, true).total);
+    return cmc::plan_decode4(B, Hq, Hkv, Dh, k, W).total;
 }
 
 cmc_status cmc_two_tier_decode_q4(const float *q, const uint8_t *cme_k, const uint8_t *cme_v, const uint8_t *cme_ks,

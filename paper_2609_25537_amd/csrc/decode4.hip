@@ -94,12 +94,9 @@ __device__ __forceinline__ uint32_t pair_of(float lo, float hi, uint32_t take) {
     return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), take);
 }
 
-// Units in flight per wave.
-#ifndef CMC_DECODE4_SETS
-#define CMC_DECODE4_SETS 2
-#endif
+// Units in flight per wave; with eight heads of 256 the registers hold one.
 template <int DH, int G>
-constexpr int kSets4 = G * DH > 1024 ? 1 : CMC_DECODE4_SETS;
+constexpr int kSets4 = G * DH > 1024 ? 1 : 2;
 
 // The codes and scales of a Tier-1 block's or a ring's rows, bounded by the live ones.
 struct Array4 {

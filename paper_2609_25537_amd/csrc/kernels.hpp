@@ -160,7 +160,7 @@ struct Decode4Params : DecodeParams {
 };
 // Rows a wave takes at a time; chunk and the plan count in these.
 constexpr int kUnit4 = 32;
-DecodePlan plan_decode4(int B, int Hq, int Hkv, int Dh, int k, int W, bool append);
+DecodePlan plan_decode4(int B, int Hq, int Hkv, int Dh, int k, int W);
 // Most appended rows that the decode kernel takes along, with a word of eight dims of K
 // for half of a workgroup's threads and one of V for the others; more are appended by a
 // launch of their own.
