@@ -2,8 +2,12 @@
 //
 // Rows are independent, so a thread takes eight dims of a K row and the same of
 // its V row, 16-byte loads of bf16; four neighbouring lanes hold the 32 dims of a
-// scale and find their maximum with two lane exchanges.  Bound by memory; small
-// calls by latency.
+// scale and find their maximum with two lane exchanges.
+//
+// Bound by memory: a gather of 350 of 4096 fp32 rows for each of 64 x 8 heads, 207 MB,
+// 44.3 us, 4.7 TB/s (the same rows side by side 5.1); reading these back as bf16, 117 MB,
+// 18.4 us.  Small calls are bound by latency: 2.3 us for a gather of 256 rows of one
+// sequence, 2.9 for an append of a row to 64 x 8 rings, 2.1 for 256 rows read back.
 #include <algorithm>
 
 #include "cache4.hpp"
@@ -13,7 +17,13 @@ namespace cmc {
 
 namespace {
 
-constexpr int kWriteTrip = 2;  // words of each array that a thread requests at once
+// Words of each array that a thread requests at once, and whether past the caches.  A
+// gather waits for an index first and is quickest with many threads: 256 rows of one
+// sequence 2.3 us (two words 2.8, four 3.7), 64 sequences 44.3 (45.4, 46.5), not faster past the
+// caches (45.2).  An append of 1024 rows to 8 x 8 rings 11.9 us (one word 12.4, through the
+// caches 12.7).
+template <bool RING>
+constexpr int kWriteTrip = RING ? 2 : 1;
 
 // Rows of one (sequence, kv head): a Tier-1 block's, from the pool through the
 // index list, or (RING) the appended ones, to their ring slots.
@@ -30,17 +40,17 @@ __global__ __launch_bounds__(256) void write_rows4_kernel(Write4Params p) {
         rows = p.count ? min(max(p.count[b], 0), p.R) : p.R;
     }
     const uint32_t words = (uint32_t)rows << shift;
-    const uint32_t i0 = blockIdx.x * (256u * kWriteTrip) + threadIdx.x;
+    const uint32_t i0 = blockIdx.x * (256u * kWriteTrip<RING>) + threadIdx.x;
     if (i0 - threadIdx.x >= words) return;  // uniform
     const T *src[2] = {static_cast<const T *>(p.src_k) + ((head * p.src_rows) << shift) * 8,
                        static_cast<const T *>(p.src_v) + ((head * p.src_rows) << shift) * 8};
     const Row4 dst[2] = {{p.k + ((head * p.R) << shift) * 4, p.ks + ((head * p.R) << (shift - 2))},
                          {p.v + ((head * p.R) << shift) * 4, p.vs + ((head * p.R) << (shift - 2))}};
-    Raw8<T> raw[kWriteTrip][2];
-    uint32_t row[kWriteTrip];
-    int word[kWriteTrip];
+    Raw8<T> raw[kWriteTrip<RING>][2];
+    uint32_t row[kWriteTrip<RING>];
+    int word[kWriteTrip<RING>];
 #pragma unroll
-    for (int u = 0; u < kWriteTrip; ++u) {
+    for (int u = 0; u < kWriteTrip<RING>; ++u) {
         const uint32_t i = min(i0 + u * 256u, words - 1);  // a row is whole quads, so quads stay together
         row[u] = i >> shift;
         word[u] = (int)(i & ((1u << shift) - 1));
@@ -49,10 +59,10 @@ __global__ __launch_bounds__(256) void write_rows4_kernel(Write4Params p) {
             if (p.idx) from = (size_t)min(max(p.idx[(size_t)b * p.idx_stride + row[u]], 0), p.src_rows - 1);
         }
 #pragma unroll
-        for (int x = 0; x < 2; ++x) raw[u][x].load(src[x] + ((from << shift) + word[u]) * 8);
+        for (int x = 0; x < 2; ++x) raw[u][x].template load<RING>(src[x] + ((from << shift) + word[u]) * 8);
     }
 #pragma unroll
-    for (int u = 0; u < kWriteTrip; ++u) {
+    for (int u = 0; u < kWriteTrip<RING>; ++u) {
         size_t to = row[u];
         if constexpr (RING) {
             to += slot0;
@@ -77,8 +87,8 @@ __global__ __launch_bounds__(1024) void append_rows4_kernel(Write4Params p) {
         const size_t at = (head0 + h) * p.R;
         const size_t from = (((head0 << shift) * p.T_new) + i) * 8;
         Raw8<T> k, v;
-        k.load(static_cast<const T *>(p.src_k) + from);
-        v.load(static_cast<const T *>(p.src_v) + from);
+        k.template load<false>(static_cast<const T *>(p.src_k) + from);
+        v.template load<false>(static_cast<const T *>(p.src_v) + from);
         const int slot = slot0 + t < p.R ? slot0 + t : slot0 + t - p.R;
         Row4{p.k + (at << shift) * 4, p.ks + (at << (shift - 2))}.put(slot, word, shift, k, true);
         Row4{p.v + (at << shift) * 4, p.vs + (at << (shift - 2))}.put(slot, word, shift, v, true);
@@ -125,7 +135,7 @@ __global__ __launch_bounds__(256) void read_rows4_kernel(Read4Params p) {
 template <typename T, bool RING>
 hipError_t launch_rows(const Write4Params &p, int rows, hipStream_t stream) {
     const long long words = (long long)rows << p.row_shift;  // 2^31 at most
-    const dim3 grid((unsigned)((words + 256 * kWriteTrip - 1) / (256 * kWriteTrip)), p.Hkv, p.B);
+    const dim3 grid((unsigned)((words + 256 * kWriteTrip<RING> - 1) / (256 * kWriteTrip<RING>)), p.Hkv, p.B);
     write_rows4_kernel<T, RING><<<grid, 256, 0, stream>>>(p);
     return hipGetLastError();
 }

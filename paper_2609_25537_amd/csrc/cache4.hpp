@@ -50,9 +50,15 @@ template <typename T>
 struct Raw8 {
     static constexpr int M = Vec16<T>::N, N = 8 / M;
     uint4 r[N];
+    // STREAM: past the caches.
+    template <bool STREAM>
     __device__ __forceinline__ void load(const T *p) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) r[i] = reinterpret_cast<const uint4 *>(p)[i];
+        for (int i = 0; i < N; ++i) {
+            const u32x4 *const at = reinterpret_cast<const u32x4 *>(p) + i;
+            const u32x4 x = STREAM ? __builtin_nontemporal_load(at) : *at;
+            r[i] = make_uint4(x[0], x[1], x[2], x[3]);
+        }
     }
     __device__ __forceinline__ void widen(float (&x)[8]) const {
 #pragma unroll
