@@ -1142,10 +1142,10 @@ _rope_call = None
 def _heads(name, x, B, T, Dh):
     """Checks of one projection part [B][T][H][Dh]; returns (heads, token stride).  Heads
     are dense, tokens evenly spaced (a slice of a wider projection is)."""
-    s, st = x.shape, x.stride()
+    s = x.shape
     if not (len(s) == 4 and s[0] == B and s[1] == T and s[3] == Dh):
         raise ValueError(f"{name} [B][T][H][Dh]")
-    H = s[2]
+    H, st = s[2], x.stride()
     token = st[1] if T > 1 else st[0] if B > 1 else H * Dh
     if x.numel() and not (st[3] == 1 and (H == 1 or st[2] == Dh) and (B == 1 or T == 1 or st[0] == T * token)):
         raise ValueError(f"{name}: heads must be dense and tokens evenly spaced")
@@ -1175,41 +1175,47 @@ def cmc_norm_rope(q, k, v, pos, inv_freq, q_weight=None, k_weight=None, eps: flo
         raise ValueError("pos [B][T] int32")
     if not (inv_freq.dim() == 1 and inv_freq.dtype is f32 and inv_freq.is_contiguous()):
         raise ValueError("inv_freq [rot / 2] fp32")
-    for w in (q_weight, k_weight):
-        if w is not None and not (w.shape == (Dh,) and w.dtype is f32 and w.is_contiguous()):
-            raise ValueError("weights [Dh] fp32")
+    if ((q_weight is not None and not (q_weight.shape == (Dh,) and q_weight.dtype is f32 and q_weight.is_contiguous()))
+            or (k_weight is not None
+                and not (k_weight.shape == (Dh,) and k_weight.dtype is f32 and k_weight.is_contiguous()))):
+        raise ValueError("weights [Dh] fp32")
     Hq = Hkv = qs = ks = vs = 0
+    away = pos.get_device() != dev or inv_freq.get_device() != dev
     if q is not None:
         Hq, qs = _heads("q", q, B, T, Dh)
         if out_q is None:
             out_q = _make(stream, torch.empty, (B, T, Hq, Dh), dtype=q_dtype or f32, device=q.device)
         elif not (out_q.shape == (B, T, Hq, Dh) and out_q.is_contiguous()):
             raise ValueError("out_q must be contiguous [B][T][Hq][Dh]")
+        away = away or q.get_device() != dev or out_q.get_device() != dev
     else:
         out_q = None
     if k is not None:
+        if k.dtype is not dtype:
+            raise ValueError("q, k and v must be of one type")
         Hkv, ks = _heads("k", k, B, T, Dh)
         shape = (B, Hkv, T, Dh)
         if out_k is None:
             out_k = _make(stream, torch.empty, shape, dtype=kv_dtype or dtype, device=k.device)
         elif not (out_k.shape == shape and out_k.is_contiguous()):
             raise ValueError("out_k must be contiguous [B][Hkv][T][Dh]")
+        away = away or k.get_device() != dev or out_k.get_device() != dev
     else:
         out_k = None
     if v is not None:
+        if v.dtype is not dtype:
+            raise ValueError("q, k and v must be of one type")
         Hv, vs = _heads("v", v, B, T, Dh)
         if out_v is None:
             out_v = _make(stream, torch.empty_like, out_k)
         if not (Hv == Hkv and out_v.shape == shape and out_v.dtype is out_k.dtype and out_v.is_contiguous()):
             raise ValueError("v must match k, and out_v out_k")
+        away = away or v.get_device() != dev or out_v.get_device() != dev
     else:
         out_v = None
-    for x in (q, k, v):
-        if x is not None and x.dtype is not dtype:
-            raise ValueError("q, k and v must be of one type")
-    for x in (q, k, v, pos, inv_freq, q_weight, k_weight, out_q, out_k, out_v):
-        if x is not None and x.get_device() != dev:
-            _elsewhere(dev, x)
+    if (away or (q_weight is not None and q_weight.get_device() != dev)
+            or (k_weight is not None and k_weight.get_device() != dev)):
+        _elsewhere(dev, q, k, v, pos, inv_freq, q_weight, k_weight, out_q, out_k, out_v)
     if _rope_call is None:
         _rope_call = lib().cmc_norm_rope
     rc = _rope_call(
