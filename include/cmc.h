@@ -597,7 +597,7 @@ cmc_status cmc_two_tier_decode_q8(const float *q, const void *cme_k, const void 
 
 /*
  * One decode step: cmc_window_append_q8, then cmc_two_tier_decode_q8 over the
- * updated cache; in a single launch for up to 16 rows.  The ring's codes, scales
+ * updated cache; in a single launch for up to 1024 / Dh rows.  The ring's codes, scales
  * and counts are those of the two calls; out is the same attention over the
  * same keys, up to the order of the sums.  With W == 0 there is no Tier-2 and the
  * new rows are ignored.
@@ -630,14 +630,14 @@ cmc_status cmc_decode_step_q8(const float *q, const void *cme_k, const void *cme
  *   s = the least byte >= 1 with a <= 6 * 2^(s - 127)
  *   code = x / 2^(s - 127) rounded to nearest even (error at most 1/4 of the scale
  *          where the value is below 2 scales, 1/2 below 4, 1 up to 6)
- * with infinities stored as +-6 scales (elements of 7/8 of 2^128 and more round to 2^128, which reads
- * back as infinity and is past the decode's limits); a NaN makes its 32 dims NaN (s = 255, codes
- * 0).  Rows do not depend on each other, so appends leave the others as they are, and
+ * with infinities stored as +-6 scales (elements of 7/8 of 2^128 and more round to
+ * 2^128, which reads back as infinity and is past the decode's limits); a NaN makes its
+ * 32 dims NaN (s = 255, codes 0).  Rows do not depend on each other, so appends leave the others as they are, and
  * rows appended in one call or in several come out the same.  The decode and the
  * read-back take any codes and scales, e.g. of a cache made elsewhere.
  *
- * Common limits: Hkv >= 1, B and Hkv <= 65535, Dh in {64, 128, 256}, at most 2^26
- * rows an array, else CMC_ERR_UNSUPPORTED.
+ * Common limits: Hkv >= 1, B and Hkv <= 65535, Dh in {64, 128, 256}, at most 2^24
+ * rows of a (sequence, kv head) in an array, else CMC_ERR_UNSUPPORTED.
  */
 
 /*
@@ -724,7 +724,7 @@ cmc_status cmc_two_tier_decode_q4(const float *q, const uint8_t *cme_k, const ui
 
 /*
  * One decode step: cmc_window_append_q4, then cmc_two_tier_decode_q4 over the
- * updated cache; in a single launch for up to 16 rows.  The ring's codes, scales and
+ * updated cache; in a single launch for up to 1024 / Dh rows.  The ring's codes, scales and
  * counts are those of the two calls; out is the same attention over the same keys, up
  * to the order of the sums.  With W == 0 there is no Tier-2 and the new rows are
  * ignored.

@@ -33,6 +33,16 @@
 // and to LDS, and take them from there in the units that hold them: nothing waits for a
 // store, and no unit is read twice.  Publication, merge and the count's advance are
 // decode_finish.hpp's.
+//
+// Bound, at 8 kv heads of 128 and 32 heads: full batches by memory over the launch's own
+// 7 us (64 sequences of 1536 keys, 109 MB, 25.0 us; of 4608 keys 59.7, 6.2 TB/s at the
+// slope; 16 x 16 heads of 256 over 3048 keys, 212 MB, 37.4 us, 5.7 TB/s), few sequences
+// by the chain of one unit's instructions, about 0.65 us for a wave alone on its SIMD
+// and 0.47 a unit for two (one sequence of 768 keys 8.3 us, of 32808 keys 16.1; 24
+// ragged sequences of 64 heads 16.0).  Measured and slower: more units in flight than two,
+// 12 waves, the next unit's scores between this one's (one workgroup's 32768 keys 135 us
+// against 126), and K multiplied as codes and scales with q in five parts of 6 bits (64
+// sequences 25.7 us, with heads of 64 20.1 against 18.0).
 #include <type_traits>
 
 #include "cache4.hpp"
@@ -102,9 +112,9 @@ constexpr int kSets4 = G * DH > 1024 ? 1 : 2;
 struct Array4 {
     __amdgpu_buffer_rsrc_t k, v, ks, vs;
 };
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *at, int bytes) {
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *at, uint32_t bytes) {
     constexpr int untyped = 0x00027000;  // 32-bit elements, addressed by bytes
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(at), 0, bytes, untyped);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(at), 0, (int)bytes, untyped);
 }
 
 // A word of eight dims of the appended rows for each thread, K's in the first half of the
@@ -650,20 +660,21 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
     int first = ring ? pool_units : 0, rows = ring ? W : kb;
     Array4 a;
     const auto codes = [&](int rows) {
-        a.k = buffer_of(ring ? rk : pk, rows * (DH / 2));
-        a.v = buffer_of(ring ? rv : pv, rows * (DH / 2));
+        a.k = buffer_of(ring ? rk : pk, (uint32_t)rows * (DH / 2));  // 2^31 at most
+        a.v = buffer_of(ring ? rv : pv, (uint32_t)rows * (DH / 2));
     };
     codes(u < end ? rows : 0);
-    st.load_k(0, a, u - first);
-    st.load_v(0, a, u - first);
+    int at = u < end ? u - first : 0;  // in range, or at the start of an empty buffer
+    st.load_k(0, a, at);
+    st.load_v(0, a, at);
     in_order();
     const int T_new = (int)((unsigned)info >> 16);
     const Decode4Params early = late_params();
     const uint8_t *pks = early.cme_ks + pair * (size_t)N * (DH / 32), *pvs = early.cme_vs + pair * (size_t)N * (DH / 32);
     uint8_t *rks = early.win_ks + pair * (size_t)W * (DH / 32), *rvs = early.win_vs + pair * (size_t)W * (DH / 32);
     const auto scales = [&](int rows) {
-        a.ks = buffer_of(ring ? rks : pks, rows * (DH / 32));
-        a.vs = buffer_of(ring ? rvs : pvs, rows * (DH / 32));
+        a.ks = buffer_of(ring ? rks : pks, (uint32_t)rows * (DH / 32));
+        a.vs = buffer_of(ring ? rvs : pvs, (uint32_t)rows * (DH / 32));
     };
 
     // The units in turn through NS register sets.  Loads are requested always, of no
@@ -676,13 +687,13 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
     RingCount cnt{0, false};
     NewRows<DH, NW * kWave> fresh;
     scales(u < end ? rows : 0);
-    st.load_ks(0, a, u - first);
-    st.load_vs(0, a, u - first);
+    st.load_ks(0, a, at);
+    st.load_vs(0, a, at);
     fresh.request(early, T_new, pair);
     in_order();  // before q, whose wait so covers the scales' and the new rows' too
     st.request_q(early, b, kvh);
     cnt.load(W > 0 ? early.win_count : nullptr, b);
-    n[0] = u < end ? min(kUnit4, rows - (u - first) * kUnit4) : 0;
+    n[0] = u < end ? min(kUnit4, rows - at * kUnit4) : 0;
     mine[0] = u;
 #pragma unroll
     for (int i = 1; i < NS; ++i) {
@@ -692,14 +703,15 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
         rows = ring ? W : kb;
         codes(u < end ? rows : 0);
         scales(u < end ? rows : 0);
-        n[i] = u < end ? min(kUnit4, rows - (u - first) * kUnit4) : 0;
+        at = u < end ? u - first : 0;
+        n[i] = u < end ? min(kUnit4, rows - at * kUnit4) : 0;
         mine[i] = u;
         in_order();
-        st.load_k(i, a, u - first);
-        st.load_ks(i, a, u - first);
+        st.load_k(i, a, at);
+        st.load_ks(i, a, at);
         in_order();
-        st.load_v(i, a, u - first);
-        st.load_vs(i, a, u - first);
+        st.load_v(i, a, at);
+        st.load_vs(i, a, at);
     }
     st.split_q(early);
     // What follows from the count: the ring slots that hold a key of this step, and the
@@ -752,7 +764,8 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
         scales(rows);
     };
     if (u < end) enter(u >= pool_units);
-    int at = u - first, left = 0;
+    at = u - first;
+    int left = 0;
 #pragma unroll 1
     while (u < end) {
 #pragma unroll

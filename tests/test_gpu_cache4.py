@@ -340,7 +340,8 @@ def test_attend_counts(k, W, counts, k_len):
 @pytest.mark.parametrize("B,Hkv,G,Dh,k,W", [
     (1, 8, 4, 128, 256, 512), (1, 8, 4, 128, 40, 6000), (3, 1, 8, 64, 7, 3000), (12, 8, 2, 64, 100, 200), (17, 8, 1, 128, 300, 100),
     (20, 8, 4, 64, 120, 300), (33, 8, 4, 128, 40, 130), (50, 8, 2, 128, 64, 64), (70, 8, 1, 64, 33, 95), (5, 13, 8, 256, 200, 700),
-    (2, 4, 8, 256, 1000, 2000), (40, 1, 8, 256, 33, 500),
+    (2, 4, 8, 256, 1000, 2000), (40, 1, 8, 256, 33, 500), (1, 1, 8, 128, 5000, 9000), (1, 1, 2, 64, 3, 20000), (1, 1, 1, 256, 200, 184),
+    (1, 1, 1, 128, 0, 385), (20, 8, 8, 128, 500, 1100), (19, 8, 4, 64, 300, 700), (32, 8, 1, 256, 100, 2000), (33, 8, 4, 128, 100, 2000),
 ])
 def test_attend_plans(B, Hkv, G, Dh, k, W):
     rng = np.random.default_rng(B * Hkv)
@@ -491,6 +492,36 @@ def test_step(kv, B, Hq, Hkv, Dh, k, W, counts):
         assert (ws[:4 * (B + B * Hkv)] == 0).all()  # counters ready for the next call
 
 
+@pytest.mark.parametrize("kv", ["bf16", "f32"])
+@pytest.mark.parametrize("Dh,more", [(64, 0), (128, 0), (256, 0), (64, 1), (128, 1), (256, 1)])
+@pytest.mark.parametrize("B,Hkv,G,k,W,counts", [(2, 2, 4, 40, 50, [45, 7]), (1, 2, 8, 500, 700, [1395]), (1, 1, 1, 0, 17, [16]),
+                                               (41, 4, 2, 1500, 600, [599, 600, 0, 31, 1196])])
+def test_step_of_as_many_rows_as_one_launch_takes(kv, Dh, more, B, Hkv, G, k, W, counts):
+    """1024 / Dh rows, round the ring's end and over several workgroups' units, in four
+    waves and in eight; and one more."""
+    T = 1024 // Dh + more
+    say("q4 step", kv, Dh, T, B, Hkv, G, k, W)
+    rng = np.random.default_rng(T + W)
+    tier, tv = make(rng, B, Hkv, k, Dh)
+    ring, _ = make(rng, B, Hkv, W, Dh)
+    counts = [counts[b % len(counts)] for b in range(B)]
+    cnt = i32(counts)
+    want = [raw(x).copy() for x in ring]
+    new = [rows(rng, (B, Hkv, T, Dh), kv) for _ in range(2)]
+    q = torch.from_numpy(rng.standard_normal((B, Hkv * G, Dh))).to(torch.float32).to(DEV)
+    out = cmc.cmc_decode_step_q4(q, *tier, k, *ring, cnt, *[dev(x, FLOAT[kv]) for x in new], Dh ** -0.5)
+    for b in range(B):
+        for h in range(Hkv):
+            for i in range(2):
+                q4_ref.append(want[i][b, h], want[2 + i][b, h], counts[b], new[i][b, h])
+        counts[b] += T
+    assert raw(cnt).tolist() == counts
+    for x, w in zip(ring, want):
+        assert (raw(x) == w).all()
+    rv = np.stack([q4_ref.values(q4_ref.unpack(want[i]), want[2 + i].astype(np.int64)) for i in range(2)])
+    check(out, q, tv, rv, [k] * B, counts, Dh ** -0.5)
+
+
 def test_step_fills_an_empty_ring_that_held_nan():
     """Slots never written hold NaN; the step's own rows are the only ones attended."""
     ring, cnt = cache(2, 2, 50, 128), i32([0, 0])
@@ -518,28 +549,33 @@ def test_empty_batch():
     assert cmc.cmc_gather_tier1_q4(new, new, None, 1)[0].shape == (0, 2, 1, 64)
 
 
-def test_offsets_past_32_bits():
-    """The longest cache of one head: rows near its end are written, read back and
-    attended where they lie (4 GiB of codes an array)."""
-    R, Dh = 1 << 24, 128
-    say("longest 4-bit cache")
-    ring = [torch.zeros(1, 1, R, Dh // 2, dtype=torch.uint8, device=DEV) for _ in range(2)]
-    ring += [torch.ones(1, 1, R, Dh // 32, dtype=torch.uint8, device=DEV) for _ in range(2)]
+@pytest.mark.parametrize("Hkv,Dh", [(1, 128), (3, 256)])
+def test_offsets_past_32_bits(Hkv, Dh):
+    """The longest caches: rows near their end are written, read back and attended where
+    they lie (three heads of 256 are 6 GiB of codes an array, the last past 32 bits)."""
+    R = 1 << 24
+    say("longest 4-bit cache", Hkv, Dh)
+    ring = [torch.zeros(1, Hkv, R, Dh // 2, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    ring += [torch.ones(1, Hkv, R, Dh // 32, dtype=torch.uint8, device=DEV) for _ in range(2)]
     cnt = i32([R - 3])
-    new = torch.randn(1, 1, 3, Dh, device=DEV)
+    new = torch.randn(1, Hkv, 3, Dh, device=DEV)
     cmc.cmc_window_append_q4(*ring, cnt, new[:, :, :2].contiguous(), new[:, :, :2].contiguous())
-    q = 40 * new[:, 0, 2:].contiguous()  # far ahead of the zero rows
-    out = cmc.cmc_decode_step_q4(q, *cache(1, 1, 0, Dh), 0, *ring, cnt, new[:, :, 2:].contiguous(), new[:, :, 2:].contiguous(), 1.0)
+    q = 40 * new[:, :, 2].contiguous()  # far ahead of the zero rows
+    last = new[:, :, 2:].contiguous()
+    out = cmc.cmc_decode_step_q4(q, *cache(1, Hkv, 0, Dh), 0, *ring, cnt, last, last, 1.0)
     k, v = cmc.cmc_cache_read_q4(*ring, count=cnt, rows=3, dtype=torch.float32)
     assert cnt.item() == R
-    c, s = q4_ref.quantise(host(new)[0, 0])
-    val = q4_ref.values(c, s)
-    assert (host(k)[0, 0] == val).all() and (host(v)[0, 0] == val).all()
-    want, bound = q4_ref.attend(host(q)[0, 0], np.concatenate([val, np.zeros((1, Dh))]), np.concatenate([val, np.zeros((1, Dh))]), 1.0)
-    assert (np.abs(host(out)[0, 0] - want) <= bound + 1e-9).all()
-    pool = torch.randn(1, 1, 8, Dh, device=DEV).to(torch.bfloat16)
+    zero = np.zeros((1, Dh))
+    for h in range(Hkv):
+        val = q4_ref.values(*q4_ref.quantise(host(new)[0, h]))
+        assert (host(k)[0, h] == val).all() and (host(v)[0, h] == val).all()
+        rows = np.concatenate([val, zero])
+        want, bound = q4_ref.attend(host(q)[0, h], rows, rows, 1.0)
+        assert (np.abs(host(out)[0, h] - want) <= bound + 1e-9).all()
+    pool = torch.randn(1, Hkv, 8, Dh, device=DEV).to(torch.bfloat16)
     idx = torch.zeros(1, R, dtype=torch.int32, device=DEV)
     idx[0, -2:] = torch.tensor([5, 7])
     cmc.cmc_gather_tier1_q4(pool, pool, idx, R, out_k=ring[0], out_v=ring[1], out_ks=ring[2], out_vs=ring[3])
-    wc, ws = quantised(host(pool)[0, 0][[0, 5, 7]])
-    assert (raw(ring[0][0, 0, -3:]) == wc).all() and (raw(ring[3][0, 0, -3:]) == ws).all()
+    for h in range(Hkv):
+        wc, ws = quantised(host(pool)[0, h][[0, 5, 7]])
+        assert (raw(ring[0][0, h, -3:]) == wc).all() and (raw(ring[3][0, h, -3:]) == ws).all()

@@ -177,17 +177,23 @@ def test_separate_tensors_equal_slices():
     assert all(torch.equal(x, y) for x, y in zip(a, b))
 
 
-def test_larger_launches_give_the_same_bits():
-    """Four tokens to a workgroup, or one."""
+@pytest.mark.parametrize("Hq,Hkv,Dh,interleaved,kinds", [(5, 3, 64, False, ("bf16", "f32")), (48, 8, 64, False, ("bf16", "bf16")),
+                                                        (48, 8, 64, True, ("f32", "bf16")), (90, 1, 256, False, ("f32", "f32"))])
+def test_larger_launches_give_the_same_bits(Hq, Hkv, Dh, interleaved, kinds):
+    """Outputs that pass the caches and such as do not; a token's heads in one workgroup
+    and in several."""
     rng = np.random.default_rng(9)
-    q, k, v = projection(rng, 1, 2050, 5, 3, 64, "bf16")
+    q, k, v = projection(rng, 1, 2050, Hq, Hkv, Dh, kinds[0])
     f, tf = freqs(48)
     pos = torch.arange(2050, dtype=torch.int32, device=DEV).view(1, 2050) * 7
-    w = torch.rand(64, device=DEV)
-    a = cmc.cmc_norm_rope(q, k, v, pos, tf, q_weight=w, k_weight=w)
+    how = dict(q_weight=torch.rand(Dh, device=DEV), k_weight=torch.rand(Dh, device=DEV), interleaved=interleaved,
+               q_dtype=FLOAT[kinds[1]], kv_dtype=torch.bfloat16)
+    a = cmc.cmc_norm_rope(q, k, v, pos, tf, **how)
     for lo, hi in ((0, 900), (900, 2050)):
-        b = cmc.cmc_norm_rope(q[:, lo:hi], k[:, lo:hi], v[:, lo:hi], pos[:, lo:hi].contiguous(), tf, q_weight=w, k_weight=w)
+        b = cmc.cmc_norm_rope(q[:, lo:hi], k[:, lo:hi], v[:, lo:hi], pos[:, lo:hi].contiguous(), tf, **how)
         assert torch.equal(b[0], a[0][:, lo:hi]) and torch.equal(b[1], a[1][:, :, lo:hi]) and torch.equal(b[2], a[2][:, :, lo:hi])
+    few = cmc.cmc_norm_rope(q[:, :, :3], k, None, pos, tf, **how)
+    assert torch.equal(few[0], a[0][:, :, :3]) and torch.equal(few[1], a[1]) and few[2] is None
 
 
 # ------------------------------------------------------------- all together
