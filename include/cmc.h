@@ -755,7 +755,8 @@ cmc_status cmc_decode_step_q4(const float *q, const uint8_t *cme_k, const uint8_
  *   q, k, v    in_dtype (fp32 or bf16): B * T tokens of Hq, Hkv and Hkv heads of Dh,
  *              consecutive tokens q_stride, k_stride, v_stride elements apart (e.g.
  *              the three parts of one projection's rows)
- *   pos        [B][T] int32
+ *   pos        [B][T] int32; 4-byte alignment is enough, so it may be a step of a longer
+ *              list
  *   inv_freq   [rot / 2] fp32
  *   q_weight, k_weight  [Dh] fp32, or NULL: that array is not normed
  *   out_q      [B][T][Hq][Dh] q_dtype (fp32 or bf16); with T = 1 and fp32 the q of

@@ -1285,9 +1285,10 @@ cmc_status cmc_norm_rope(const void *q, long long q_stride, const void *k, long 
         return fail(CMC_ERR_INVALID_ARGUMENT, "norm_rope: null pointer");
     if (rot > 0 && (!pos || !inv_freq))
         return fail(CMC_ERR_INVALID_ARGUMENT, "norm_rope: pos and inv_freq must be non-null when rot > 0");
-    if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(pos) || misaligned(inv_freq) ||
-        misaligned(q_weight) || misaligned(k_weight) || misaligned(out_q) || misaligned(out_k) || misaligned(out_v))
-        return fail(CMC_ERR_UNSUPPORTED, "norm_rope: every pointer must be 16-byte aligned");
+    if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(inv_freq) || misaligned(q_weight) ||
+        misaligned(k_weight) || misaligned(out_q) || misaligned(out_k) || misaligned(out_v) ||
+        (reinterpret_cast<uintptr_t>(pos) & 3u))
+        return fail(CMC_ERR_UNSUPPORTED, "norm_rope: every pointer must be 16-byte aligned (pos 4-byte)");
     cmc::RopeParams p{};
     p.q = q;
     p.k = Hkv > 0 ? k : nullptr;

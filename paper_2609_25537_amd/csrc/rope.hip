@@ -74,7 +74,8 @@ template <typename T, int DH, bool FAR>
 __global__ __launch_bounds__(kMostThreads) void norm_rope_kernel(RopeParams p, int heads, bool q_bf16, bool kv_bf16) {
     constexpr int L = DH / 16;  // lanes to a head
     __shared__ __attribute__((aligned(16))) float s_cos[DH / 2], s_sin[DH / 2];
-    const size_t token = blockIdx.x;
+    const size_t token = (size_t)blockIdx.z * gridDim.x + blockIdx.x;
+    if (token >= (size_t)p.B * p.T) return;  // uniform
     const int half = p.rot >> 1;
     const int j = threadIdx.x % L;
     const bool apart = !p.interleaved && j < p.rot / 16;
@@ -188,7 +189,9 @@ hipError_t launch_type(const RopeParams &p, bool q_bf16, bool kv_bf16, hipStream
     const int groups = (all * lanes + kMostThreads - 1) / kMostThreads;
     const int heads = (all + groups - 1) / groups;
     const int threads = (heads * lanes + 63) / 64 * 64;
-    const dim3 grid(p.B * p.T, groups);
+    // A grid holds less than 2^32 threads a dimension.
+    const int total = p.B * p.T, row = std::min(total, 1 << 22);
+    const dim3 grid(row, groups, (total + row - 1LL) / row);
     // Non-temporal stores: 2048 tokens of 32 + 16 heads to bf16 10.9 us (13.0 without),
     // but with fp32 queries, whose lanes write every other 16 bytes at a time, 36 (17.9).
     const bool far = kv_bf16 && (q_bf16 || !p.q) && (long long)p.B * p.T * all * p.Dh >= 1 << 23;

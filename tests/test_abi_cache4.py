@@ -113,7 +113,7 @@ def _rope(**kw):
     (dict(Hq=65536), UNS), (dict(Hkv=65536), UNS), (dict(B=1 << 16, T=1 << 15), UNS), (dict(eps=-1.0), INV),
     (dict(eps=float("inf")), INV), (dict(eps=float("nan")), INV), (dict(qs=1023), INV), (dict(ks=516), INV), (dict(vs=256), INV),
     (dict(q=None), INV), (dict(oq=None), INV), (dict(k=None), INV), (dict(ok=None), INV), (dict(ov=None), INV),
-    (dict(pos=None), INV), (dict(f=None), INV), (dict(q=FAKE + 8), UNS), (dict(pos=FAKE + 4), UNS), (dict(f=FAKE + 4), UNS),
+    (dict(pos=None), INV), (dict(f=None), INV), (dict(q=FAKE + 8), UNS), (dict(pos=FAKE + 2), UNS), (dict(f=FAKE + 4), UNS),
     (dict(kw_=FAKE + 8), UNS), (dict(ov=FAKE + 2), UNS),
 ])
 def test_rope_refusals(kw, code):

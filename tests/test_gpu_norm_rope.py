@@ -196,6 +196,21 @@ def test_larger_launches_give_the_same_bits(Hq, Hkv, Dh, interleaved, kinds):
     assert torch.equal(few[0], a[0][:, :, :3]) and torch.equal(few[1], a[1]) and few[2] is None
 
 
+def test_more_threads_than_a_grid_dimension_holds():
+    """2^26 + 5 tokens of one head: 2^32 threads and more, and offsets past 32 bits."""
+    T = (1 << 26) + 5
+    say("rope", T)
+    q = torch.empty(1, T, 1, 64, dtype=torch.bfloat16, device=DEV)
+    q.view(-1)[:64 * 1000].normal_()
+    q[:, -1000:] = torch.randn(1, 1000, 1, 64, device=DEV).to(torch.bfloat16)
+    pos = torch.arange(T, dtype=torch.int32, device=DEV).view(1, T)
+    _, tf = freqs(64)
+    got = cmc.cmc_norm_rope(q, None, None, pos, tf, q_dtype=torch.bfloat16)[0]
+    for at in (slice(0, 1000), slice(T - 1000, T)):
+        few = cmc.cmc_norm_rope(q[:, at], None, None, pos[:, at].contiguous(), tf, q_dtype=torch.bfloat16)[0]
+        assert torch.equal(got[:, at], few)
+
+
 # ------------------------------------------------------------- all together
 
 def flow_inputs(seed, steps=3):
