@@ -98,11 +98,11 @@ __device__ __forceinline__ floatx4 mfma_bf16(const uint4 &a, const uint4 &b, con
 
 // x's leading 8 bits, as a float.
 __device__ __forceinline__ float cut(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
-// The leading 8 bits of two numbers side by side, or (kNone) nothing.
-constexpr uint32_t kTops = 0x07060302, kNone = 0x0c0c0c0c;
-__device__ __forceinline__ uint32_t pair_of(float lo, float hi, uint32_t take) {
-    return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), take);
+// The leading 8 bits of two numbers side by side.
+__device__ __forceinline__ uint32_t pair_of(float lo, float hi) {
+    return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302);
 }
+constexpr uint32_t kNone = 0x0c0c0c0c;  // a permute's selector of zeros
 
 // Units in flight per wave; with eight heads of 256 the registers hold one.
 template <int DH, int G>
@@ -158,6 +158,34 @@ struct NewCodes {
     __attribute__((aligned(16))) uint8_t scales[2][fused_rows4(DH)][DH / 32];
 };
 
+// q's parts and the factors of its heads, shared by the workgroup's waves: part p of
+// head g, bf16, the last part zeros.  Rows are padded so that a wave's columns lie in
+// different banks.
+template <int DH, int G>
+struct Queries {
+    __attribute__((aligned(16))) uint16_t part[4][G][DH + 8];
+    float f[G];  // |scale| log2(e) over q's power of two
+};
+
+// Exchange between lanes i and i ^ 4 (or i ^ 8) of 16: the lanes with the bit clear keep x
+// and take the other's x as y, those with it set keep y and take the other's y as x.  Two of
+// these transpose a square of dwords over four lanes.
+__device__ __forceinline__ void cross4(uint32_t &x, uint32_t &y) {
+    const int a = (int)x, b = (int)y;
+    x = (uint32_t)__builtin_amdgcn_update_dpp(a, b, 0x114, 0xF, 0xA, false);  // from lane - 4
+    y = (uint32_t)__builtin_amdgcn_update_dpp(b, a, 0x104, 0xF, 0x5, false);  // from lane + 4
+}
+__device__ __forceinline__ void cross8(uint32_t &x, uint32_t &y) {
+    const int a = (int)x, b = (int)y;
+    x = (uint32_t)__builtin_amdgcn_update_dpp(a, b, 0x128, 0xF, 0xC, false);
+    y = (uint32_t)__builtin_amdgcn_update_dpp(b, a, 0x128, 0xF, 0x3, false);
+}
+// Of a quad's lane I, to all four.
+template <int I>
+__device__ __forceinline__ uint32_t of_quad_lane(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, I * 0x55, 0xF, 0xF, true);
+}
+
 template <int NW, int DH, int G>
 struct Walk4 {
     static constexpr int KW = DH / 32;         // words of a K row per lane, and MFMAs per 16 rows
@@ -165,28 +193,39 @@ struct Walk4 {
     static constexpr int QP = G == 8 ? 2 : 1;  // MFMAs that q's parts take
     static constexpr int PP = G == 8 ? 3 : G == 4 ? 2 : 1;  // and p's
     static constexpr int NS = kSets4<DH, G>;
-    // Units on their way or being worked on, each in registers of its own.
+    static constexpr int KLoads = DH / 64;     // loads of a unit's K, 16 bytes a lane
+    static constexpr int VLoads = DH == 256 ? 4 : 2, VWords = DH == 64 ? 2 : 4;  // and of its V
+    // Units on their way or being worked on, each in registers of its own, as loaded.
     struct Unit {
-        uint32_t k[2][KW];
-        uint32_t v[8][VB == 8 ? 2 : 1];
-        uint32_t ks[2], vs[8];  // scale bytes as loaded (by rows of the tile, and rows as v's)
+        uint32_t k[KLoads][4], v[VLoads][VWords], ks, vs[DH == 128 ? 8 : DH == 256 ? 4 : 2];
     } un[NS];
-    float4 qx[2 * KW];        // q as loaded
+    static constexpr int NH = (G + NW - 1) / NW, QE = DH / 64;  // a wave's heads of q, and its lanes' elements of each
+    float qx[NH][QE];         // q as loaded
     uint4 q[QP][KW];
-    float f;                  // |scale| log2(e) over q's power of two
+    float f;                  // of head r16 % G
     float m;                  // of head r16 % G
     float limit;              // the largest score that m may stay for
     floatx4 l, acc[VB];       // rows 4 q4 + i: (head, dim parity, part)
     int lane, r16, q4;
     int k_turn, v_turn;       // to the lane's scales
 
+    // Where things lie in a unit.  Row x of tile t in both products (its lanes' scores are
+    // of rows 4 q4 + i) is row 8 (x / 4) + 4 t + x % 4: a lane group's eight rows follow one
+    // another.
+    __device__ __forceinline__ int k_row(int t) const { return 8 * (r16 >> 2) + 4 * t + (r16 & 3); }
+    __device__ __forceinline__ int v_row(int e) const { return 8 * q4 + e; }  // e = 4 t + i
+    // The lane's first dim of q and of a K row, and of a V row.
+    __device__ __forceinline__ int k_dim() const { return DH == 64 ? 32 * (q4 & 1) + 16 * (q4 >> 1) : 8 * KW * q4; }
+    __device__ __forceinline__ int v_dim() const {
+        return DH == 256 ? 32 * (r16 & 7) + 16 * (r16 >> 3) : DH / 4 * (r16 & 3) + DH / 16 * (r16 >> 2);
+    }
+
     __device__ __forceinline__ void init() {
         lane = threadIdx.x & 63;
         r16 = lane & 15;
         q4 = lane >> 4;
-        // the lane's dims begin at q4 Dh / 4 of a K row, r16 Dh / 16 of a V row
-        k_turn = turn_for(DH == 64 ? q4 >> 1 : DH == 128 ? q4 : 2 * (q4 & 1));
-        v_turn = turn_for(r16 * DH / 512 % 4);
+        k_turn = turn_for(DH == 64 ? q4 & 1 : DH == 128 ? q4 : 2 * (q4 & 1));
+        v_turn = turn_for(DH == 64 ? (r16 & 3) >> 1 : r16 & 3);
         m = kNoMax;
         limit = kNoMax;
         l = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -194,36 +233,42 @@ struct Walk4 {
         for (int j = 0; j < VB; ++j) acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // A unit's rows are at a scalar offset in the buffers of its array, whose bounds are
-    // the array's live rows: rows past them come as zeros, and neither a row nor a unit
-    // costs address arithmetic per lane.
+    // Loads.  A unit's rows are at a scalar offset in the buffers of its array, whose bounds
+    // are the array's live rows: rows past them come as zeros, and neither a row nor a unit
+    // costs address arithmetic per lane.  A load takes the CU's address unit 16 cycles,
+    // however little its lanes ask for, and 14 of them a unit (4 bytes of V, the scales of a row
+    // each) were what it waited for: so lanes take 16 bytes where they can, of other rows
+    // or dims than they need, and exchange them.
     static constexpr int kNonTemporal = 2;
-    __device__ __forceinline__ void load_k(int set, const Array4 &from, int unit) {
-        Unit &n = un[set];
-        const int o = r16 * (DH / 2) + 4 * KW * q4, at = unit * (kUnit4 * DH / 2);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            if constexpr (KW == 2) {
-                const auto x = __builtin_amdgcn_raw_buffer_load_b64(from.k, o + 16 * t * (DH / 2), at, 0);
-                n.k[t][0] = x[0];
-                n.k[t][1] = x[1];
-            } else {
-#pragma unroll
-                for (int i = 0; i < KW; i += 4) {
-                    const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(from.k, o + 16 * t * (DH / 2) + 4 * i, at, 0);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) n.k[t][i + e] = x[e];
-                }
-            }
-        }
+    template <int CACHE = 0>
+    __device__ __forceinline__ static void load_words(uint32_t (&to)[4], __amdgpu_buffer_rsrc_t from, int o, int at) {
+        const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(from, o, at, CACHE);
+        to[0] = x[0];
+        to[1] = x[1];
+        to[2] = x[2];
+        to[3] = x[3];
     }
-    // Scale bytes come with their neighbours (a row's two, or four of them): narrower
-    // loads would be more, and the compiler clears the other bits of a byte at the end of
+    template <int CACHE = 0>
+    __device__ __forceinline__ static void load_words(uint32_t (&to)[2], __amdgpu_buffer_rsrc_t from, int o, int at) {
+        const auto x = __builtin_amdgcn_raw_buffer_load_b64(from, o, at, CACHE);
+        to[0] = x[0];
+        to[1] = x[1];
+    }
+    // Heads of 64 as one: half a row for each lane, tile 0's in the lower half of the wave.
+    static constexpr int KPer = KLoads == 1 ? 1 : KLoads / 2;  // loads of a tile
+    __device__ __forceinline__ int raw_k_row(int j) const { return k_row(DH == 64 ? q4 >> 1 : j / KPer); }
+    __device__ __forceinline__ int raw_k_word(int j) const { return DH == 64 ? 4 * (q4 & 1) : KW * q4 + 4 * (j % KPer); }
+    __device__ __forceinline__ void load_k(int set, const Array4 &from, int unit) {
+        const int at = unit * (kUnit4 * DH / 2), o = raw_k_row(0) * (DH / 2) + 4 * raw_k_word(0);
+#pragma unroll
+        for (int j = 0; j < KLoads; ++j)
+            load_words(un[set].k[j], from.k, o + j / KPer * 4 * (DH / 2) + 16 * (j % KPer), at);
+    }
+    // Odd lane groups load tile 1's for both.  Scale bytes come with their neighbours (a
+    // row's two, or four of them): the compiler clears the other bits of a byte at the end of
     // a loop's turn, for which it waits.
     __device__ __forceinline__ void load_ks(int set, const Array4 &from, int unit) {
-        const int o = r16 * (DH / 32) + (DH == 256 ? 4 * (q4 >> 1) : 0);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) un[set].ks[t] = scales_at(from.ks, o + 16 * t * (DH / 32), unit * (kUnit4 * DH / 32));
+        un[set].ks = scales_at(from.ks, k_row(q4 & 1) * (DH / 32) + (DH == 256 ? 4 * (q4 >> 1) : 0), unit * (kUnit4 * DH / 32));
     }
     __device__ __forceinline__ static uint32_t scales_at(__amdgpu_buffer_rsrc_t from, int o, int at) {
         if constexpr (DH == 64) {
@@ -238,39 +283,33 @@ struct Walk4 {
     // A loaded word turned so that byte b is where bf16_pair4 looks for a scale.
     __device__ __forceinline__ static int turn_for(int b) { return (8 * b + 9) & 31; }
     __device__ __forceinline__ static uint32_t turned(uint32_t w, int by) { return __builtin_amdgcn_alignbit(w, w, by); }
+    // Four lanes (heads of 256: two, and twice as many loads) hold four (two) rows' chunks of
+    // 32 dims (of 64: 16) and want a part of each row's.
+    __device__ __forceinline__ int raw_v_row(int j) const { return DH == 256 ? 8 * q4 + 2 * j + (r16 >> 3) : 8 * q4 + 4 * j + (r16 >> 2); }
+    __device__ __forceinline__ int raw_v_word() const { return VWords * (r16 & (DH == 256 ? 7 : 3)); }
     __device__ __forceinline__ void load_v(int set, const Array4 &from, int unit) {
-        Unit &n = un[set];
-        const int o = 4 * q4 * (DH / 2) + VB * r16, at = unit * (kUnit4 * DH / 2);
+        const int o = raw_v_row(0) * (DH / 2) + 4 * raw_v_word(), at = unit * (kUnit4 * DH / 2);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int e = o + ((j >> 2) * 16 + (j & 3)) * (DH / 2);
-            if constexpr (VB == 2) {
-                typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-                u16x2 x;  // the other half may hold anything
-                x[0] = __builtin_amdgcn_raw_buffer_load_b16(from.v, e, at, kNonTemporal);
-                n.v[j][0] = __builtin_bit_cast(uint32_t, x);
-            } else if constexpr (VB == 4) {
-                n.v[j][0] = __builtin_amdgcn_raw_buffer_load_b32(from.v, e, at, kNonTemporal);
-            } else {
-                const auto x = __builtin_amdgcn_raw_buffer_load_b64(from.v, e, at, kNonTemporal);
-                n.v[j][0] = x[0];
-                n.v[j][1] = x[1];
-            }
-        }
+        for (int j = 0; j < VLoads; ++j)
+            load_words<kNonTemporal>(un[set].v[j], from.v, o + j * (8 / VLoads) * (DH / 2), at);
     }
+    // The scales of a lane group's eight rows: of heads of 128 each lane has all of them, else
+    // each lane of a quad two rows'.
+    __device__ __forceinline__ int raw_vs_row() const { return 8 * q4 + (DH == 128 ? 0 : 2 * (r16 & 3)); }
     __device__ __forceinline__ void load_vs(int set, const Array4 &from, int unit) {
-        Unit &n = un[set];
-        const int o = 4 * q4 * (DH / 32) + (DH == 256 ? 4 * (r16 >> 3) : 0), at = unit * (kUnit4 * DH / 32);
-        if constexpr (DH == 128) {  // four rows lie in 16 bytes
+        uint32_t (&to)[DH == 128 ? 8 : DH == 256 ? 4 : 2] = un[set].vs;
+        const int o = raw_vs_row() * (DH / 32), at = unit * (kUnit4 * DH / 32);
+        if constexpr (DH == 64) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(from.vs, o + 16 * t * (DH / 32), at, 0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) n.vs[4 * t + i] = x[i];
-            }
+            for (int e = 0; e < 2; ++e) to[e] = scales_at(from.vs, o + e * (DH / 32), at);
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) n.vs[j] = scales_at(from.vs, o + ((j >> 2) * 16 + (j & 3)) * (DH / 32), at);
+            for (int i = 0; i < (DH == 128 ? 2 : 1); ++i) {
+                uint32_t w[4];
+                load_words(w, from.vs, o + 16 * i, at);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) to[4 * i + e] = w[e];
+            }
         }
     }
 
@@ -283,110 +322,179 @@ struct Walk4 {
             const int a = first + row - slot0;
             return a < 0 ? a + W : a;
         };
-        const auto scale_word = [&](int kv, int a, int at) -> uint32_t {
-            const uint8_t *from = &fresh.scales[kv][a][at];
-            if constexpr (DH == 64) return *reinterpret_cast<const uint16_t *>(from);
-            else return *reinterpret_cast<const uint32_t *>(from);
+        const auto codes = [&](auto &to, int kv, int row, int word) {
+            const int a = which(row);
+            if (a < T_new) {
+#pragma unroll
+                for (int i = 0; i < (int)(sizeof(to) / 4); ++i) to[i] = fresh.codes[kv][a][word + i];
+            }
+        };
+        const auto scale_word = [&](uint32_t &to, int kv, int row, int at) {
+            const int a = which(row);
+            if (a < T_new) {
+                const uint8_t *from = &fresh.scales[kv][a][at];
+                if constexpr (DH == 64) to = *reinterpret_cast<const uint16_t *>(from);
+                else to = *reinterpret_cast<const uint32_t *>(from);
+            }
         };
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int a = which(16 * t + r16);
-            if (a < T_new) {
+        for (int j = 0; j < KLoads; ++j) codes(x.k[j], 0, raw_k_row(j), raw_k_word(j));
+        scale_word(x.ks, 0, k_row(q4 & 1), DH == 256 ? 4 * (q4 >> 1) : 0);
 #pragma unroll
-                for (int i = 0; i < KW; ++i) x.k[t][i] = fresh.codes[0][a][KW * q4 + i];
-                x.ks[t] = scale_word(0, a, DH == 256 ? 4 * (q4 >> 1) : 0);
+        for (int j = 0; j < VLoads; ++j) codes(x.v[j], 1, raw_v_row(j), raw_v_word());
+        constexpr int rows = DH == 128 ? 8 : 2, words = DH == 256 ? 2 : 1;
+#pragma unroll
+        for (int e = 0; e < rows; ++e)
+#pragma unroll
+            for (int i = 0; i < words; ++i) {
+                uint32_t &to = x.vs[words * e + i];
+                scale_word(to, 1, raw_vs_row() + e, 4 * i);
+                if (raw_vs_row() + e >= n) to = 0;  // 2^-127 times any code
             }
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int row = (j >> 2) * 16 + 4 * q4 + (j & 3), a = which(row);
-            if (a < T_new) {
-                const uint8_t *from = reinterpret_cast<const uint8_t *>(fresh.codes[1][a]) + VB * r16;
-                if constexpr (VB == 2) x.v[j][0] = *reinterpret_cast<const uint16_t *>(from);
-                else
-#pragma unroll
-                    for (int i = 0; i < VB / 4; ++i) x.v[j][i] = reinterpret_cast<const uint32_t *>(from)[i];
-                x.vs[j] = scale_word(1, a, DH == 256 ? 4 * (r16 >> 3) : 0);
-            }
-            if (row >= n) x.vs[j] = 0;  // 2^-127 times any code
-        }
     }
 
-    // The lane's quarter of its head's q.
-    __device__ __forceinline__ void request_q(const DecodeParams &p, int b, int kvh) {
-        const float *qp = p.q + ((size_t)b * p.Hq + (size_t)kvh * G + (r16 % G)) * DH + 8 * KW * q4;
+    // A head of q for each wave (two, where there are eight for four), QE elements a lane.
+    __device__ __forceinline__ void request_q(const DecodeParams &p, int b, int kvh, int wave) {
 #pragma unroll
-        for (int i = 0; i < 2 * KW; ++i) qx[i] = *reinterpret_cast<const float4 *>(qp + 4 * i);
+        for (int h = 0; h < NH; ++h) {
+            const float *qp = p.q + ((size_t)b * p.Hq + (size_t)kvh * G + min(wave + NW * h, G - 1)) * DH + QE * lane;
+            typedef float Run __attribute__((ext_vector_type(QE == 1 ? 2 : QE)));
+            if constexpr (QE == 1) {
+                qx[h][0] = *qp;
+            } else {
+                const Run x = *reinterpret_cast<const Run *>(qp);
+#pragma unroll
+                for (int e = 0; e < QE; ++e) qx[h][e] = x[e];
+            }
+        }
     }
     // q times a power of two, and its parts.  With 2^sum the size of scale log2(e) q, q
     // is taken to 2^-12, so that a score's sum stays in range for any K, and f makes up
     // for it; past 2^60 and below 2^-100, where it takes tiny or huge K to bring the
     // scores back, q takes a share, so that neither f nor the products are subnormal.
-    __device__ __forceinline__ void split_q(const DecodeParams &p) {
-        float x[8 * KW];
+    __device__ __forceinline__ void split_q(const DecodeParams &p, int wave, Queries<DH, G> &to_all) {
 #pragma unroll
-        for (int i = 0; i < 2 * KW; ++i) {
-            x[4 * i] = qx[i].x;
-            x[4 * i + 1] = qx[i].y;
-            x[4 * i + 2] = qx[i].z;
-            x[4 * i + 3] = qx[i].w;
-        }
-        float top = 0.f;
+        for (int h = 0; h < NH; ++h) {
+            const int g = wave + NW * h;
+            if (g >= G) break;  // wave-uniform
+            float x[QE], top = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8 * KW; ++e) top = fmaxf(top, fabsf(x[e]));
-        top = combine_xor32<OpMax>(combine_xor16<OpMax>(top));
-        const int qe = (int)(__float_as_uint(top) >> 23) - 127, se = __builtin_amdgcn_frexp_expf(p.qscale);
-        const int sum = qe + se;
-        const int to = sum > 60 ? min(sum - 72, 60) : sum < -100 ? max(sum + 88, -72) : -12;
-        f = ldexpf(__builtin_amdgcn_frexp_mantf(fabsf(p.qscale)), sum - to);
-        const int by = to - qe, most = min(max(by, -126), 127);
-        const float mul = ldexpf(copysignf(1.f, p.qscale), most);
+            for (int e = 0; e < QE; ++e) {
+                x[e] = qx[h][e];
+                top = fmaxf(top, fabsf(x[e]));
+            }
+            top = lane_reduce<OpMax, 1, 64>(top);
+            const int qe = (int)(__float_as_uint(top) >> 23) - 127, se = __builtin_amdgcn_frexp_expf(p.qscale);
+            const int sum = qe + se;
+            const int to = sum > 60 ? min(sum - 72, 60) : sum < -100 ? max(sum + 88, -72) : -12;
+            const float factor = ldexpf(__builtin_amdgcn_frexp_mantf(fabsf(p.qscale)), sum - to);
+            const int by = to - qe, most = min(max(by, -126), 127);
+            const float mul = ldexpf(copysignf(1.f, p.qscale), most);
+            uint32_t y[3][QE];
 #pragma unroll
-        for (int e = 0; e < 8 * KW; ++e) x[e] *= mul;
-        if (__builtin_expect(__any(by != most), 0)) {
+            for (int e = 0; e < QE; ++e) {
+                x[e] *= mul;
+                if (__builtin_expect(by != most, 0)) x[e] = ldexpf(x[e], by - most);
+                const float r = x[e] - cut(x[e]);
+                y[0][e] = __float_as_uint(x[e]);
+                y[1][e] = __float_as_uint(r);
+                y[2][e] = __float_as_uint(r - cut(r));
+            }
 #pragma unroll
-            for (int e = 0; e < 8 * KW; ++e) x[e] = ldexpf(x[e], by - most);
-        }
-        // The lane's part: x less the leading parts before it, of which pair_of takes the top.
-        const int part = r16 / G;
-        const float less1 = part >= 1 ? 1.f : 0.f, less2 = part >= 2 ? 1.f : 0.f;
-        const uint32_t take = part < 3 ? kTops : kNone, take_lo = part == 0 ? kTops : kNone;
-#pragma unroll
-        for (int i = 0; i < KW; ++i) {
-            float y[QP][8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float z = x[8 * i + e], r = fmaf(-less1, cut(z), z);
-                if constexpr (G == 8) {
-                    const float mid = z - cut(z);
-                    y[0][e] = r;
-                    y[1][e] = mid - cut(mid);
+            for (int s = 0; s < 4; ++s) {
+                uint16_t *const at = &to_all.part[s][g][QE * lane];
+                if constexpr (QE == 1) {
+                    *at = s < 3 ? (uint16_t)(y[s % 3][0] >> 16) : (uint16_t)0;
                 } else {
-                    y[0][e] = fmaf(-less2, cut(r), r);
+#pragma unroll
+                    for (int e = 0; e < QE; e += 2)
+                        *reinterpret_cast<uint32_t *>(at + e) =
+                            s < 3 ? pair_of(__uint_as_float(y[s % 3][e]), __uint_as_float(y[s % 3][e + 1])) : 0u;
                 }
             }
-#pragma unroll
-            for (int s = 0; s < QP; ++s) {
-                const uint32_t sel = s ? take_lo : take;
-                q[s][i] = make_uint4(pair_of(y[s][0], y[s][1], sel), pair_of(y[s][2], y[s][3], sel),
-                                     pair_of(y[s][4], y[s][5], sel), pair_of(y[s][6], y[s][7], sel));
-            }
+            if (lane == 0) to_all.f[g] = factor;
         }
     }
+    // The lane's columns: part r16 / G of head r16 % G, the third of eight heads for itself.
+    __device__ __forceinline__ void take_q(const Queries<DH, G> &from) {
+        const int head = r16 % G, part = r16 / G;
+#pragma unroll
+        for (int s = 0; s < QP; ++s)
+#pragma unroll
+            for (int i = 0; i < KW; ++i)
+                q[s][i] = *reinterpret_cast<const uint4 *>(&from.part[s ? 2 + part : min(part, 3)][head][k_dim() + 8 * i]);
+        f = from.f[head];
+    }
 
-    // Scores (over f) of rows 16 t + 4 q4 + i.
+    // Scores (over f) of rows 8 q4 + 4 t + i.
     __device__ __forceinline__ void scores(int set, floatx4 (&c)[2]) const {
+        const Unit &x = un[set];
+        const auto ks = __builtin_amdgcn_permlane16_swap(x.ks, x.ks, false, false);
+        uint32_t k[2][KW];
+        if constexpr (DH == 64) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const auto w = __builtin_amdgcn_permlane32_swap(x.k[0][i], x.k[0][2 + i], false, false);
+                k[0][i] = w[0];
+                k[1][i] = w[1];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < KLoads; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) k[j / KPer][4 * (j % KPer) + e] = x.k[j][e];
+        }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             c[t] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < KW; ++i) {
-                const uint32_t s = turned(un[set].ks[t], DH == 256 && i >= KW / 2 ? k_turn + 8 & 31 : k_turn);
-                const uint4 k = bf16_word4(un[set].k[t][i], s);
+                const uint32_t s = turned(ks[t], DH == 256 && i >= KW / 2 ? k_turn + 8 & 31 : k_turn);
+                const uint4 w = bf16_word4(k[t][i], s);
 #pragma unroll
-                for (int j = 0; j < QP; ++j) c[t] = mfma_bf16(k, q[j][i], c[t]);
+                for (int j = 0; j < QP; ++j) c[t] = mfma_bf16(w, q[j][i], c[t]);
             }
         }
+    }
+
+    // V's codes of tile t: a row's in a word (of heads of 256 two, of 64 a half: rows 2 h and
+    // 2 h + 1 in word h).
+    __device__ __forceinline__ void rows_of_v(int set, int t, uint32_t (&w)[DH == 256 ? 8 : DH == 128 ? 4 : 2]) const {
+        const auto &x = un[set].v;
+        if constexpr (DH == 64) {
+            uint32_t a = x[t][0], b = x[t][1];
+            cross8(a, b);  // the lane's words of rows r, 2 + r, with r the lane's bit 2
+            const uint32_t take = r16 & 4 ? 0x03020706u : 0x05040100u;  // the upper halves or the lower
+            const auto halves = [&](uint32_t own) {
+                int o = __builtin_amdgcn_update_dpp(0, (int)own, 0x114, 0xF, 0xA, false);
+                o = __builtin_amdgcn_update_dpp(o, (int)own, 0x104, 0xF, 0x5, false);
+                return __builtin_amdgcn_perm((uint32_t)o, own, take);
+            };
+            w[0] = halves(a);
+            w[1] = halves(b);
+        } else if constexpr (DH == 128) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = x[t][i];
+            cross4(w[0], w[1]);
+            cross4(w[2], w[3]);
+            cross8(w[0], w[2]);
+            cross8(w[1], w[3]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {  // rows 2 j and 2 j + 1
+                uint32_t a[4] = {x[2 * t + j][0], x[2 * t + j][1], x[2 * t + j][2], x[2 * t + j][3]};
+                cross8(a[0], a[2]);
+                cross8(a[1], a[3]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[4 * j + e] = a[2 * (e >> 1) + (e & 1)];
+            }
+        }
+    }
+    // V's scale of row 8 q4 + E, turned.
+    template <int E>
+    __device__ __forceinline__ uint32_t scale_of_v(const uint32_t (&two)[2], int set) const {
+        if constexpr (DH == 128) return turned(un[set].vs[E], v_turn);
+        else return turned(of_quad_lane<(E >> 1)>(two[E & 1]), v_turn);
     }
 
     // Has the sums finished here rather than behind the next loads, which would
@@ -415,7 +523,7 @@ struct Walk4 {
             }
         float top = rounded_product(fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
                                           fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))), f);
-        const auto live = [&](int e) { return (e >> 2) * 16 + 4 * q4 + (e & 3) < n; };
+        const auto live = [&](int e) { return v_row(e) < n; };
         if (__builtin_expect(n < kUnit4, 0)) {
             top = made_here(kNoMax);
 #pragma unroll
@@ -482,11 +590,21 @@ struct Walk4 {
         }
         constexpr uint32_t one = 0x3f803f80u;
         const uint4 ones = make_uint4(one, one, one, one);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            uint32_t s[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[i] = turned(un[set].vs[4 * t + i], v_turn);
+        uint32_t two[2] = {};  // the scales of rows 2 (r16 % 4) and the next, of the lane's dims
+        if constexpr (DH == 64) {
+            two[0] = un[set].vs[0];
+            two[1] = un[set].vs[1];
+        } else if constexpr (DH == 256) {
+            const uint32_t w0 = un[set].vs[0], w1 = un[set].vs[1], w2 = un[set].vs[2], w3 = un[set].vs[3];
+            two[0] = r16 & 4 ? w1 : w0;
+            two[1] = r16 & 4 ? w3 : w2;
+        }
+        const auto tile = [&](auto which) {
+            constexpr int t = decltype(which)::value;
+            const uint32_t s[4] = {scale_of_v<4 * t>(two, set), scale_of_v<4 * t + 1>(two, set), scale_of_v<4 * t + 2>(two, set),
+                                   scale_of_v<4 * t + 3>(two, set)};
+            uint32_t v[DH == 256 ? 8 : DH == 128 ? 4 : 2];
+            rows_of_v(set, t, v);
 #pragma unroll
             for (int h = 0; h < PP; ++h) {
                 const uint4 p = make_uint4(P[h][4 * t], P[h][4 * t + 1], P[h][4 * t + 2], P[h][4 * t + 3]);
@@ -494,10 +612,16 @@ struct Walk4 {
             }
             const auto product = [&](auto byte) {
                 constexpr int J = decltype(byte)::value;
-                const uint4 y = make_uint4(bf16_pair4<J & 3>(un[set].v[4 * t][J >> 2], s[0]),
-                                           bf16_pair4<J & 3>(un[set].v[4 * t + 1][J >> 2], s[1]),
-                                           bf16_pair4<J & 3>(un[set].v[4 * t + 2][J >> 2], s[2]),
-                                           bf16_pair4<J & 3>(un[set].v[4 * t + 3][J >> 2], s[3]));
+                uint4 y;
+                if constexpr (DH == 64)
+                    y = make_uint4(bf16_pair4<J>(v[0], s[0]), bf16_pair4<2 + J>(v[0], s[1]), bf16_pair4<J>(v[1], s[2]),
+                                   bf16_pair4<2 + J>(v[1], s[3]));
+                else if constexpr (DH == 128)
+                    y = make_uint4(bf16_pair4<J>(v[0], s[0]), bf16_pair4<J>(v[1], s[1]), bf16_pair4<J>(v[2], s[2]),
+                                   bf16_pair4<J>(v[3], s[3]));
+                else
+                    y = make_uint4(bf16_pair4<J & 3>(v[J >> 2], s[0]), bf16_pair4<J & 3>(v[2 + (J >> 2)], s[1]),
+                                   bf16_pair4<J & 3>(v[4 + (J >> 2)], s[2]), bf16_pair4<J & 3>(v[6 + (J >> 2)], s[3]));
 #pragma unroll
                 for (int h = 0; h < PP; ++h) {
                     const uint4 p = make_uint4(P[h][4 * t], P[h][4 * t + 1], P[h][4 * t + 2], P[h][4 * t + 3]);
@@ -516,7 +640,9 @@ struct Walk4 {
                 product(std::integral_constant<int, 6>{});
                 product(std::integral_constant<int, 7>{});
             }
-        }
+        };
+        tile(std::integral_constant<int, 0>{});
+        tile(std::integral_constant<int, 1>{});
     }
 
     // A row-tile value (rows 4 q4 + i) summed over the parts: put(g, parity, value)
@@ -691,7 +817,7 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
     st.load_vs(0, a, at);
     fresh.request(early, T_new, pair);
     in_order();  // before q, whose wait so covers the scales' and the new rows' too
-    st.request_q(early, b, kvh);
+    st.request_q(early, b, kvh, wave);
     cnt.load(W > 0 ? early.win_count : nullptr, b);
     n[0] = u < end ? min(kUnit4, rows - at * kUnit4) : 0;
     mine[0] = u;
@@ -713,7 +839,8 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
         st.load_v(i, a, at);
         st.load_vs(i, a, at);
     }
-    st.split_q(early);
+    __shared__ Queries<DH, G> s_q;
+    st.split_q(early, wave, s_q);
     // What follows from the count: the ring slots that hold a key of this step, and the
     // units that take appended rows.
     const int count = cnt.value();
@@ -749,8 +876,9 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
             s_new.codes[v][row][word] = w;
             if ((word & 3) == 0) s_new.scales[v][row][word >> 2] = (uint8_t)byte;
         }
-        lds_barrier();
     }
+    lds_barrier();
+    st.take_q(s_q);
     const auto amend = [&](int i) {
         if (__builtin_expect(amends[i], 0))
             st.amend(i, s_new, (mine[i] - pool_units) * kUnit4, slot0, T_new, W, n[i]);
@@ -818,7 +946,7 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
     __shared__ int s_cnt[NW];
 #pragma unroll
     for (int j = 0; j < DH / 32; ++j)
-        st.over_parts(st.acc[j], [&](int g, int odd, float x) { s_acc[wave][g][DH / 16 * st.r16 + 2 * j + odd] = x; });
+        st.over_parts(st.acc[j], [&](int g, int odd, float x) { s_acc[wave][g][st.v_dim() + 2 * j + odd] = x; });
     st.over_parts(st.l, [&](int g, int odd, float x) {
         if (st.r16 == 0 && odd == 0) s_l[wave][g] = x;
     });
