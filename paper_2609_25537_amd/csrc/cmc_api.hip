@@ -265,15 +265,18 @@ DecodePlan plan_decode8(int B, int Hq, int Hkv, int Dh, int k, int W, bool appen
 // 0.65 us, more than its bytes do, so a long axis is split over all CUs; a join costs
 // about 1.7 us and 0.06 us per split that the last workgroup reads.
 //
-// - Up to 12 units, or from 160 pairs on, no split: 8 pairs of 7 units 6.8 us in one
-//   workgroup each and 8.2 in two; 160 pairs of 24 units 11.8 and 13.2.
+// - Up to 12 units, or from 160 pairs on, no split: 8 pairs of 7 units 6.2 us in one
+//   workgroup each and 7.2 in two; 160 pairs of 24 units 10.8 and 11.9.
 // - Else a wave's units and the number of splits grow alike, as the root of the length,
-//   with one workgroup per CU at most.  8 pairs: 24 units 8.2 us in 6 splits (3: 8.9),
-//   130 units 9.7 in 11 (17: 10.0, 7: 10.7), 1026 units 16.7 in 29 (43: 18.6, 20: 18.5);
-//   64 pairs: 24 units 10.1 in 3 (6: 10.7), 136 units 15.6 in 4 (7: 15.8, 3: 17.3).
-// - Eight waves only for a pair's whole axis, where a CU has one workgroup and each wave
-//   enough to walk: 256 pairs of 144 units 30.8 us (4 waves 32.9), of 48 units 17.3 (16.6);
-//   eight query heads, 192 pairs of 50 units, 16.9 (18.0).
+//   with one workgroup per CU at most.  8 pairs: 24 units 7.1 us in 6 splits (3: 7.9),
+//   130 units 8.7 in 11 (17: 9.0, 7: 9.7), 1026 units 15.8 in 29 (43: 17.8, 20: 17.7);
+//   64 pairs: 24 units 9.0 in 3 (2: 9.6), 136 units 14.7 in 4 (7: 14.7, 3: 16.6).
+// - Eight waves for a pair's whole axis where a CU has one workgroup at most: 256 pairs of
+//   144 units 30.1 us (4 waves 34.0), 192 of 38 units 13.3 (13.9), 8 of 12 units 5.6 (6.0), of 7
+//   units 6.2 (6.2).  Split axes leave half of the CUs to others only where pairs are few
+//   and long: one of 1026 units 15.7 us in 33 splits (4 waves 18.9); 8 pairs of 1026 units
+//   fill the card with four waves (26 splits of eight 16.9), and of 130 units a wave of eight
+//   has too little (9.4).
 constexpr long long kMaxSplits4 = 127;
 DecodePlan plan_decode4(int B, int Hq, int Hkv, int Dh, int k, int W) {
     const long long pairs = (long long)B * Hkv;
@@ -283,11 +286,17 @@ DecodePlan plan_decode4(int B, int Hq, int Hkv, int Dh, int k, int W) {
     long long S = 1, chunk = std::max(1LL, units);
     if (units > 12 && pairs > 0 && pairs < 160) {
         const long long most = std::min(256 / pairs, kMaxSplits4);
-        const long long share = (long long)(sqrt((double)units) / 4), least = (units + 4 * most - 1) / (4 * most);
-        chunk = 4 * std::max(std::max(1LL, share), least);
+        const long long share = std::max(1L, lround(sqrt((double)units) / 4)), least = (units + 4 * most - 1) / (4 * most);
+        chunk = 4 * std::max(share, least);
         S = (units + chunk - 1) / chunk;
+        if (pairs * S <= 128 && share >= 6) {
+            pl.waves = 8;
+            chunk = (chunk + 7) / 8 * 8;
+            S = (units + chunk - 1) / chunk;
+        }
+    } else if (pairs <= 256 && units >= 12) {
+        pl.waves = 8;
     }
-    pl.waves = S == 1 && pairs <= 256 && units >= (Dh == 64 || G == 8 ? 48 : 64) ? 8 : 4;
     pl.S = (int)S;
     pl.chunk = (int)((chunk + pl.waves - 1) / pl.waves * pl.waves);
     pl.counter_bytes = align256((size_t)(B + pairs) * sizeof(unsigned));
