@@ -31,18 +31,19 @@
 // Fused append: every workgroup requests the appended rows with its first unit; those
 // whose part of the ring takes some of them quantise them before their walk, to memory
 // and to LDS, and take them from there in the units that hold them: nothing waits for a
-// store, and no unit is read twice.  Publication, merge and the count's advance are
-// decode_finish.hpp's.
+// store, and no unit is read twice.
 //
-// Bound, at 8 kv heads of 128 and 32 heads: full batches by memory over the launch's own
-// 7 us (64 sequences of 1536 keys, 109 MB, 25.0 us; of 4608 keys 59.7, 6.2 TB/s at the
-// slope; 16 x 16 heads of 256 over 3048 keys, 212 MB, 37.4 us, 5.7 TB/s), few sequences
-// by the chain of one unit's instructions, about 0.65 us for a wave alone on its SIMD
-// and 0.47 a unit for two (one sequence of 768 keys 8.3 us, of 32808 keys 16.1; 24
-// ragged sequences of 64 heads 16.0).  Measured and slower: more units in flight than two,
-// 12 waves, the next unit's scores between this one's (one workgroup's 32768 keys 135 us
-// against 126), and K multiplied as codes and scales with q in five parts of 6 bits (64
-// sequences 25.7 us, with heads of 64 20.1 against 18.0).
+// Bound, at 8 kv heads of 128 and 32 heads: full batches by memory between the launch's
+// start and end, which take 7 us (64 sequences of 1536 keys, 109 MB, 23.4 to 24 us; of 4608
+// keys 59.8, 6.2 TB/s at the slope; 16 x 16 heads of 256 over 3048 keys, 212 MB, 35.5 us, 6.0
+// TB/s), few sequences by the chain of one unit's instructions, about 0.65 us for a wave
+// alone on its SIMD, and the join of their splits (one sequence of 768 keys 7.4 us, of
+// 32808 keys 15.1; 24 ragged sequences of 64 heads 15.3).  Measured and slower: more units
+// in flight than two, 12 waves, the next unit's scores between this one's (one workgroup's
+// 32768 keys 135 us against 126), K multiplied as codes and scales with q in five parts of 6
+// bits (64 sequences 25.7 us against 25.1, with heads of 64 20.1 against 18.0), q split by every
+// wave for itself (21 keys of one sequence 5.2 us, 4.2 shared; with heads of 256 7.4 and 5.3).
+#include <algorithm>
 #include <type_traits>
 
 #include "cache4.hpp"
@@ -674,6 +675,147 @@ struct Walk4 {
     }
 };
 
+// Two dims of head g over the waves' (m, l, acc); returns the joint maximum.  Without a
+// key in any wave (m = kNoMax) the weights are 1 against zeros.
+template <int NW, int DH, int G>
+__device__ __forceinline__ float joined(const float (&sm)[NW][G], const float (&sl)[NW][G], const float (&sa)[NW][G][DH],
+                                        int g, int d, float2 &num, float &den) {
+    float mw[NW], lw[NW];
+    float2 aw[NW];
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        mw[w] = sm[w][g];
+        lw[w] = sl[w][g];
+        aw[w] = *reinterpret_cast<const float2 *>(&sa[w][g][d]);
+    }
+    float M = mw[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) M = fmaxf(M, mw[w]);
+    num = make_float2(0.f, 0.f);
+    den = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        const float f = fast_exp2(mw[w] - M);
+        num.x = fmaf(f, aw[w].x, num.x);
+        num.y = fmaf(f, aw[w].y, num.y);
+        den = fmaf(f, lw[w], den);
+    }
+    return M;
+}
+
+// The partials of a pair's S splits into the waves' (m, l, acc), as if each wave had
+// walked every NW-th split's rows (with fewer than 256 sums a split, groups of its lanes
+// every NW-th or so): each split is read by one wave, 16 bytes a lane, all of them
+// requested at once for up to 8 NW splits.  Loads are coherent across the XCDs, and
+// bounded: splits past the last come as zeros, with kNoMax for m.  Against each thread
+// reading two dims of every split: 8 pairs in 29 splits of four heads of 128 15.3 -> 15.1
+// us, one of eight heads in 33 15.7 -> 14.7, one of two pairs of a head of 64 in 59 14.6 -> 11.7;
+// 8 pairs in 6 splits 7.4 both.
+template <int NW, int DH, int G, int MOST, class Arrive>
+__device__ __forceinline__ void merge_splits(const float *part_ml, const float *part_acc, int S, int wave, int lane,
+                                             float (&s_m)[NW][G], float (&s_l)[NW][G], float (&s_acc)[NW][G][DH], Arrive arrive) {
+    constexpr int kWords = G * DH / 4;                        // of 16 bytes, a split's sums
+    constexpr int L = kWords < 64 ? kWords : 64, NG = 64 / L;  // lanes to a split, splits at a time
+    constexpr int NV = kWords / L;                            // words a lane
+    constexpr int NJ = std::min(MOST, NV >= 8 ? 2 : NV >= 4 ? 4 : 8);  // turns requested at a time
+    constexpr int kCoherent = 16;                             // sc1
+    const __amdgpu_buffer_rsrc_t ml = buffer_of(part_ml, S * G * 8), ac = buffer_of(part_acc, S * G * DH * 4);
+    const int turns = (S + NW * NG - 1) / (NW * NG), group = lane / L;
+    // The wave's i-th split is wave + NW i; in turn j a group takes i = group + NG j.
+    float *const own = &s_acc[wave][0][0];  // (m, l) of its splits: 2 G turns NG <= G DH floats
+    const int mls = turns * NG * G;
+    const auto ml_at = [&](int x) {
+        const auto v = __builtin_amdgcn_raw_buffer_load_b64(ml, ((wave + NW * (x / G)) * G + x % G) * 8, 0, kCoherent);
+        return make_uint2(v[0], v[1]);
+    };
+    const auto keep = [&](int x, const uint2 &v) {
+        const bool in = wave + NW * (x / G) < S;
+        *reinterpret_cast<float2 *>(own + 2 * x) = make_float2(in ? __uint_as_float(v.x) : kNoMax, in ? __uint_as_float(v.y) : 0.f);
+    };
+    const uint2 first = ml_at(lane);
+    u32x4 a[NJ][NV];
+    const auto request = [&](int j0) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+                a[j][v] = __builtin_amdgcn_raw_buffer_load_b128(
+                    ac, (wave + NW * (group + NG * (j0 + j))) * (G * DH * 4) + 16 * (lane % L + L * v), 0, kCoherent);
+    };
+    in_order();  // (m, l) first: the weights need only them
+    request(0);
+    in_order();
+    if (lane < mls) keep(lane, first);
+    for (int x = lane + 64; x < mls; x += 64) keep(x, ml_at(x));
+    arrive();
+    int g[NV];
+    float M[NV], den[NV], sum[NV][4];
+    float2 x[NV][NJ];
+    const auto take = [&](int v, int j0) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)  // past the last turn that one again
+            x[v][j] = *reinterpret_cast<const float2 *>(own + 2 * ((group + NG * min(j0 + j, turns - 1)) * G + g[v]));
+    };
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        g[v] = 4 * (lane % L + L * v) / DH;
+        take(v, 0);
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        M[v] = kNoMax;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) M[v] = fmaxf(M[v], x[v][j].x);
+        for (int j = NJ; j < turns; ++j) M[v] = fmaxf(M[v], own[2 * ((group + NG * j) * G + g[v])]);
+        if constexpr (L <= 16) M[v] = combine_xor16<OpMax>(M[v]);
+        if constexpr (L <= 32) M[v] = combine_xor32<OpMax>(M[v]);
+        den[v] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[v][e] = 0.f;
+    }
+    for (int j0 = 0;;) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            if (j0 + j < turns) {  // wave-uniform
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    const float f = fast_exp2(x[v][j].x - M[v]);
+                    den[v] = fmaf(f, x[v][j].y, den[v]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[v][e] = fmaf(f, __uint_as_float(a[j][v][e]), sum[v][e]);
+                }
+            }
+        }
+        j0 += NJ;
+        if (j0 >= turns) break;
+        request(j0);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) take(v, j0);
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const auto over_groups = [&](float x) {
+            if constexpr (L <= 16) x = combine_xor16<OpSum>(x);
+            if constexpr (L <= 32) x = combine_xor32<OpSum>(x);
+            return x;
+        };
+        den[v] = over_groups(den[v]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[v][e] = over_groups(sum[v][e]);
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int at = 4 * (lane % L + L * v);
+        if (group == 0) {
+            *reinterpret_cast<float4 *>(own + at) = make_float4(sum[v][0], sum[v][1], sum[v][2], sum[v][3]);
+            if (at % DH == 0) {
+                s_m[wave][g[v]] = M[v];
+                s_l[wave][g[v]] = den[v];
+            }
+        }
+    }
+}
+
 template <int DH, int G>
 constexpr int kMinWaves4 = 2;
 
@@ -939,7 +1081,6 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
     p.Hkv = Hkv;
     p.S = S;
     p.T_new = T_new;
-    const int cnt_now = count;
 
     __shared__ __attribute__((aligned(16))) float s_acc[NW][G][DH];
     __shared__ float s_m[NW][G], s_l[NW][G];
@@ -954,10 +1095,59 @@ __global__ __launch_bounds__(NW * kWave, (kMinWaves4<DH, G>)) void decode4_kerne
     if (st.lane == 0) s_cnt[wave] = cnt.raw;  // stored once the wave's count read has returned
     __syncthreads();
     constexpr int kThreads = NW * kWave;
-    constexpr bool kKeepNaN = true, kBySplits = true;
     const bool bump = p.T_new > 0 && W > 0;
-    unsigned prev = ~0u;  // the sequence counter before this workgroup's arrival (one lane)
-#include "decode_finish.hpp"
+    unsigned prev = ~0u;  // the sequence counter before this pair's arrival (one lane)
+    // A pair arrives for its sequence once all of its waves have read the count: each stored
+    // what it read before the barrier above.
+    const auto arrive = [&] {
+        if (bump && threadIdx.x == 0) prev = arrive_once(p.seq_counter, b, (unsigned)(s_cnt[NW - 1] != INT_MIN));
+    };
+    float *const outp = p.out + ((size_t)b * p.Hq + (size_t)kvh * G) * DH;
+    const auto output = [&] {
+        for (int t = threadIdx.x; t < G * DH / 2; t += kThreads) {
+            float2 num;
+            float den;
+            joined<NW, DH, G>(s_m, s_l, s_acc, 2 * t / DH, 2 * t % DH, num, den);
+            const float inv = den == 0.f ? 0.f : __builtin_amdgcn_rcpf(den);  // a NaN stays one
+            *reinterpret_cast<float2 *>(outp + 2 * t) = make_float2(num.x * inv, num.y * inv);
+        }
+    };
+    if (S == 1) {
+        arrive();
+        output();
+    } else {
+        // Publication: the split's partial by coherent stores, which have completed when it
+        // arrives on the pair's counter; the last one to arrive merges them all.
+        __shared__ int s_last;
+        const size_t part = (pair * S + s) * G;
+        for (int t = threadIdx.x; t < G * DH / 2; t += kThreads) {
+            const int g = 2 * t / DH, d = 2 * t % DH;
+            float2 num;
+            float den;
+            const float M = joined<NW, DH, G>(s_m, s_l, s_acc, g, d, num, den);
+            coherent_store2(&p.part_acc[part * DH + 2 * t], num.x, num.y);
+            if (d == 0) coherent_store2(&p.part_ml[(part + g) * 2], M, den);
+        }
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        if (threadIdx.x == 0)
+            s_last = __hip_atomic_fetch_add(&p.pair_counter[pair], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)(S - 1);
+        __syncthreads();
+        if (!s_last) return;  // workgroup-uniform
+        const auto merge = [&](auto most) {
+            merge_splits<NW, DH, G, decltype(most)::value>(p.part_ml + pair * S * G * 2, p.part_acc + pair * S * G * DH, S, wave,
+                                                           st.lane, s_m, s_l, s_acc, arrive);
+        };
+        if (S <= 2 * NW) merge(std::integral_constant<int, 2>{});
+        else merge(std::integral_constant<int, 8>{});
+        lds_barrier();
+        output();
+        if (threadIdx.x == 0) __hip_atomic_store(&p.pair_counter[pair], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (bump && prev == (unsigned)(p.Hkv - 1)) {  // one lane of the sequence's last pair
+        p.win_count[b] = count + p.T_new;
+        __hip_atomic_store(&p.seq_counter[b], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
 }
 
 template <int DH, int G>

@@ -342,6 +342,7 @@ def test_attend_counts(k, W, counts, k_len):
     (20, 8, 4, 64, 120, 300), (33, 8, 4, 128, 40, 130), (50, 8, 2, 128, 64, 64), (70, 8, 1, 64, 33, 95), (5, 13, 8, 256, 200, 700),
     (2, 4, 8, 256, 1000, 2000), (40, 1, 8, 256, 33, 500), (1, 1, 8, 128, 5000, 9000), (1, 1, 2, 64, 3, 20000), (1, 1, 1, 256, 200, 184),
     (1, 1, 1, 128, 0, 385), (20, 8, 8, 128, 500, 1100), (19, 8, 4, 64, 300, 700), (32, 8, 1, 256, 100, 2000), (33, 8, 4, 128, 100, 2000),
+    (3, 1, 4, 64, 40, 120000), (1, 1, 8, 256, 0, 70000), (3, 1, 1, 64, 5000, 60000), (2, 2, 1, 128, 0, 40000),
 ])
 def test_attend_plans(B, Hkv, G, Dh, k, W):
     rng = np.random.default_rng(B * Hkv)
