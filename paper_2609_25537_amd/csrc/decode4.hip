@@ -19,8 +19,8 @@
 // p crosses no lane.  A code byte holds two dims of one row, and widens to the two k
 // slots of a B word: with p in one slot and 0 in the other, a product gives one of
 // the two dims.  So rows are (head, dim parity, part), one MFMA takes 16 keys x 32
-// dims, and no code moves between lanes or bytes.  V's rows are loaded to match: lane
-// (c, q4) takes Dh / 16 consecutive dims of rows 4 q4 .. 4 q4 + 3 and 16 + 4 q4 ..
+// dims, and no code moves between bytes.  Lane (c, q4) multiplies Dh / 16 dims of rows 8 q4
+// .. 8 q4 + 7, which four lanes exchange from whole 16-byte loads (rows_of_v).
 // The same rows against ones give l, from the p that V was multiplied with.
 //
 // The maximum is moved only when a score passes it by more than 2 (p <= 4), which
