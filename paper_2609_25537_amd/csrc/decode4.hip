@@ -38,7 +38,7 @@
 // keys 59.8, 6.2 TB/s at the slope; 16 x 16 heads of 256 over 3048 keys, 212 MB, 35.5 us, 6.0
 // TB/s), few sequences by the chain of one unit's instructions, about 0.65 us for a wave
 // alone on its SIMD, and the join of their splits (one sequence of 768 keys 7.4 us, of
-// 32808 keys 15.1; 24 ragged sequences of 64 heads 15.3).  Measured and slower: more units
+// 32808 keys 14.8; 24 ragged sequences of 64 heads 15.3).  Measured and slower: more units
 // in flight than two, 12 waves, the next unit's scores between this one's (one workgroup's
 // 32768 keys 135 us against 126), K multiplied as codes and scales with q in five parts of 6
 // bits (64 sequences 25.7 us against 25.1, with heads of 64 20.1 against 18.0), q split by every
@@ -569,7 +569,7 @@ struct Walk4 {
         // row's dim parity has, or nothing.
         const int part = r16 / (2 * G);
         const uint32_t half = (r16 / G) & 1 ? 0x03020c0cu : 0x0c0c0302u;
-        const uint32_t take = part < 3 ? half : kNone, take_lo = part == 0 ? half : kNone;
+        const uint32_t take = part < 3 ? half : kNone, take_lo = part == 1 ? half : kNone;
         const float less1 = part >= 1 ? 1.f : 0.f, less2 = part >= 2 ? 1.f : 0.f;
         const auto slot = [](float y, uint32_t take) { return __builtin_amdgcn_perm(0u, __float_as_uint(y), take); };
         uint32_t P[PP][8];
@@ -580,9 +580,9 @@ struct Walk4 {
                 P[0][e] = slot(w[e], half);
                 P[1][e] = slot(r, half);
                 P[2][e] = slot(r - cut(r), half);
-            } else if constexpr (G == 4) {
-                const float r = w[e] - cut(w[e]);
-                P[0][e] = slot(part ? r : w[e], half);
+            } else if constexpr (G == 4) {  // the second part's rows take the third too
+                const float r = fmaf(-less1, cut(w[e]), w[e]);
+                P[0][e] = slot(r, half);
                 P[1][e] = slot(r - cut(r), take_lo);
             } else {
                 const float r = fmaf(-less1, cut(w[e]), w[e]);
