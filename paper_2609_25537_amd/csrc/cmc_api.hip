@@ -271,9 +271,14 @@ DecodePlan plan_decode8(int B, int Hq, int Hkv, int Dh, int k, int W, bool appen
 //   with one workgroup per CU at most.  8 pairs: 24 units 7.1 us in 6 splits (3: 7.9),
 //   130 units 8.7 in 11 (17: 9.0, 7: 9.7), 1026 units 15.8 in 29 (43: 17.8, 20: 17.7);
 //   64 pairs: 24 units 9.0 in 3 (2: 9.6), 136 units 14.7 in 4 (7: 14.7, 3: 16.6).
-// - Eight waves for a pair's whole axis where a CU has one workgroup at most: 256 pairs of
-//   144 units 30.1 us (4 waves 34.0), 192 of 38 units 13.3 (13.9), 8 of 12 units 5.6 (6.0), of 7
-//   units 6.2 (6.2).  Split axes leave half of the CUs to others only where pairs are few
+// - Eight waves for a pair's whole axis of 12 units and more where a CU has one workgroup
+//   at most: 256 pairs of 144 units 28.3 us (4 waves 30.0), 192 of 38 units 11.3 (11.9), 8 of
+//   12 units 5.2 (5.7).  Their start and sums cost more, so not for short lists of heads of
+//   256 (160 pairs of four query heads, 28 units 13.9 against 13.1, 48 units 18.3 both, 64 units
+//   21.9 against 22.6; of eight, 20 units 14.2 against 13.2, 48 units 21.1 against 22.1), nor of
+//   heads of 128 where nearly every CU has a workgroup (256 pairs, 28 units 10.2 against
+//   10.0, one query head 9.3 against 8.9; 40 units the same).
+// - Split axes leave half of the CUs to others only where pairs are few
 //   and long: one of 1026 units 15.7 us in 33 splits (4 waves 18.9); 8 pairs of 1026 units
 //   fill the card with four waves (26 splits of eight 16.9), and of 130 units a wave of eight
 //   has too little (9.4).
@@ -282,6 +287,7 @@ DecodePlan plan_decode4(int B, int Hq, int Hkv, int Dh, int k, int W) {
     const long long pairs = (long long)B * Hkv;
     const long long units = ((long long)k + kUnit4 - 1) / kUnit4 + ((long long)W + kUnit4 - 1) / kUnit4;
     const int G = Hq / Hkv;
+    const int from8 = Dh == 256 ? (G == 8 ? 48 : 64) : Dh == 128 && G < 8 && pairs > 208 ? 40 : 12;
     DecodePlan pl;
     long long S = 1, chunk = std::max(1LL, units);
     if (units > 12 && pairs > 0 && pairs < 160) {
@@ -294,7 +300,7 @@ DecodePlan plan_decode4(int B, int Hq, int Hkv, int Dh, int k, int W) {
             chunk = (chunk + 7) / 8 * 8;
             S = (units + chunk - 1) / chunk;
         }
-    } else if (pairs <= 256 && units >= 12) {
+    } else if (pairs <= 256 && units >= from8) {
         pl.waves = 8;
     }
     pl.S = (int)S;
