@@ -265,15 +265,15 @@ DecodePlan plan_decode8(int B, int Hq, int Hkv, int Dh, int k, int W, bool appen
 // 0.65 us, more than its bytes do, so a long axis is split over all CUs; a join costs
 // about 1.7 us and 0.06 us per split that the last workgroup reads.
 //
-// - Up to 12 units, or from 160 pairs on, no split: 8 pairs of 7 units 6.2 us in one
+// - Up to 12 units, or from 129 pairs on, no split: 8 pairs of 7 units 6.2 us in one
 //   workgroup each and 7.2 in two; 160 pairs of 24 units 10.8 and 11.9.
 // - Else a wave's units and the number of splits grow alike, as the root of the length,
 //   with one workgroup per CU at most.  8 pairs: 24 units 7.1 us in 6 splits (3: 7.9),
 //   130 units 8.7 in 11 (17: 9.0, 7: 9.7), 1026 units 15.8 in 29 (43: 17.8, 20: 17.7);
 //   64 pairs: 24 units 9.0 in 3 (2: 9.6), 136 units 14.7 in 4 (7: 14.7, 3: 16.6).
 // - Eight waves for a pair's whole axis of 12 units and more where a CU has one workgroup
-//   at most: 256 pairs of 144 units 28.3 us (4 waves 30.0), 192 of 38 units 11.3 (11.9), 8 of
-//   12 units 5.2 (5.7).  Their start and sums cost more, so not for short lists of heads of
+//   at most: 256 pairs of 144 units 28.3 us (4 waves 30.0), 192 of 38 units 11.3 (11.9),
+//   136 of 144 units 26.0 (29.9), 8 of 12 units 5.2 (5.7).  Their start and sums cost more, so not for short lists of heads of
 //   256 (160 pairs of four query heads, 28 units 13.9 against 13.1, 48 units 18.3 both, 64 units
 //   21.9 against 22.6; of eight, 20 units 14.2 against 13.2, 48 units 21.1 against 22.1), nor of
 //   heads of 128 where nearly every CU has a workgroup (256 pairs, 28 units 10.2 against
@@ -290,7 +290,7 @@ DecodePlan plan_decode4(int B, int Hq, int Hkv, int Dh, int k, int W) {
     const int from8 = Dh == 256 ? (G == 8 ? 48 : 64) : Dh == 128 && G < 8 && pairs > 208 ? 40 : 12;
     DecodePlan pl;
     long long S = 1, chunk = std::max(1LL, units);
-    if (units > 12 && pairs > 0 && pairs < 160) {
+    if (units > 12 && pairs > 0 && pairs <= 128) {
         const long long most = std::min(256 / pairs, kMaxSplits4);
         const long long share = std::max(1L, lround(sqrt((double)units) / 4)), least = (units + 4 * most - 1) / (4 * most);
         chunk = 4 * std::max(share, least);
@@ -300,9 +300,8 @@ DecodePlan plan_decode4(int B, int Hq, int Hkv, int Dh, int k, int W) {
             chunk = (chunk + 7) / 8 * 8;
             S = (units + chunk - 1) / chunk;
         }
-    } else if (pairs <= 256 && units >= from8) {
-        pl.waves = 8;
     }
+    if (S == 1 && pairs <= 256 && units >= from8) pl.waves = 8;
     pl.S = (int)S;
     pl.chunk = (int)((chunk + pl.waves - 1) / pl.waves * pl.waves);
     pl.counter_bytes = align256((size_t)(B + pairs) * sizeof(unsigned));

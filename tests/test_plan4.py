@@ -46,6 +46,15 @@ def test_waves_of_whole_axes(Dh, G):
                 assert p.waves == waves(pairs, units, G, Dh), (pairs, units)
 
 
+@pytest.mark.parametrize("Dh,G", HEADS)
+def test_waves_of_batches_too_large_to_split(Dh, G):
+    """129 pairs and more have one workgroup each: the same waves as 160 have."""
+    for units in (12, 13, 14, 40, 48, 64, 144, 500):
+        for pairs in range(129, 161):
+            p = plan(pairs, units, G, Dh)
+            assert (p.S, p.waves) == (1, waves(pairs, units, G, Dh)), (pairs, units)
+
+
 @pytest.mark.parametrize("units", [1, 2, 11, 12, 13, 14, 24, 25, 48, 144, 145, 500, 1026, 4096])
 def test_plans_cover_the_axis(units):
     """Splits of whole turns of their waves, every one with units, the partials within what the
