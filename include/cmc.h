@@ -597,7 +597,7 @@ cmc_status cmc_two_tier_decode_q8(const float *q, const void *cme_k, const void 
 
 /*
  * One decode step: cmc_window_append_q8, then cmc_two_tier_decode_q8 over the
- * updated cache; in a single launch for up to 1024 / Dh rows.  The ring's codes, scales
+ * updated cache; in a single launch for up to 16 rows.  The ring's codes, scales
  * and counts are those of the two calls; out is the same attention over the
  * same keys, up to the order of the sums.  With W == 0 there is no Tier-2 and the
  * new rows are ignored.
