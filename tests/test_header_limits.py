@@ -21,5 +21,5 @@ def test_rows_that_a_step_appends_in_its_launch():
     k = _read(build.CSRC, "kernels.hpp")
     rows8 = re.search(r"constexpr int kFusedRows8 = (\d+);", k)[1]
     assert f"in a single launch for up to {rows8} rows." in _comment_of("cmc_decode_step_q8")
-    rows4 = re.search(r"constexpr int fused_rows4\(int Dh\) \{ return ([\d */]+) / Dh; \}", k)[1]
-    assert f"in a single launch for up to {eval(rows4.replace("/", "//"))} / Dh rows." in _comment_of("cmc_decode_step_q4")
+    rows4 = re.search(r"constexpr int fused_rows4\(int Dh\) \{ return 4 \* 64 / 2 \* (\d+) / Dh; \}", k)[1]
+    assert f"in a single launch for up to {4 * 64 // 2 * int(rows4)} / Dh rows." in _comment_of("cmc_decode_step_q4")
