@@ -769,7 +769,7 @@ cmc_status cmc_decode_step_q4(const float *q, const uint8_t *cme_k, const uint8_
  * multiple of 16, strides at least a token's elements and multiples of 16 bytes, eps
  * >= 0 and finite.  No output may overlap an input.
  * Arithmetic: fp32, rounded once to the outputs; angles in fp64 (pos * inv_freq to
- * 2^-52 of itself), their sines and cosines to fp32's accuracy.  A head with an
+ * 2^-51 of itself), their sines and cosines to fp32's accuracy.  A head with an
  * infinity or a NaN is NaN where the formula gives one.
  */
 cmc_status cmc_norm_rope(const void *q, long long q_stride, const void *k, long long k_stride,

@@ -9,7 +9,8 @@
 // A workgroup takes one token, every head of it up to 512 threads.  The heads are
 // requested first; while they come, the first waves take one sine and cosine each to LDS,
 // which all heads then share: t in turns is reduced in fp64 (pos * inv_freq is right to
-// 2^-53 of itself; fp32 would be off by 0.06 radians at a million), the rest in fp32.
+// 2^-51 of itself, three roundings; fp32 would be off by 0.06 radians at a million), the
+// rest in fp32.
 //
 // Bound by memory for prompts: 8192 tokens of 32 + 16 heads of 128, bf16 to fp32 queries
 // and bf16 keys and values, 268 MB in 49.7 us, 5.4 TB/s (four tokens to a workgroup in
