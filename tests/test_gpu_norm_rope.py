@@ -142,6 +142,33 @@ def test_not_finite(value, norm):
     assert torch.equal(oq, want[0])
 
 
+@pytest.mark.parametrize("value", [math.inf, -math.inf])
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved,dim,pair", [(False, 5, [5, 37]), (False, 37, [5, 37]), (False, 100, [100]), (True, 5, [4, 5]),
+                                                  (True, 62, [62, 63]), (True, 64, [64])])
+def test_an_infinity_under_a_norm(value, kind, interleaved, dim, pair):
+    """x / sqrt(infinity): NaN where the infinity was, 0 elsewhere in its head, and the NaN
+    in both dims of its pair where that one turns; no other head changes."""
+    say("rope infinity", value, kind, interleaved, dim)
+    rng = np.random.default_rng(16)
+    q, k, v = (x.clone() for x in projection(rng, 2, 3, 4, 2, 128, kind))
+    f, tf = freqs(64)
+    pos = torch.from_numpy(rng.integers(1, 40000, (2, 3)).astype(np.int32)).to(DEV)
+    how = dict(q_weight=torch.from_numpy((1 + 0.3 * rng.standard_normal(128)).astype(np.float32)).to(DEV),
+               k_weight=torch.from_numpy((1 + 0.3 * rng.standard_normal(128)).astype(np.float32)).to(DEV), interleaved=interleaved,
+               kv_dtype=FLOAT[kind])
+    want = cmc.cmc_norm_rope(q, k, v, pos, tf, **how)
+    q[1, 2, 3, dim] = k[1, 2, 1, dim] = value
+    got = cmc.cmc_norm_rope(q, k, v, pos, tf, **how)
+    for y, w, at in ((got[0], want[0], (1, 2, 3)), (got[1], want[1], (1, 1, 2))):
+        head = y[at]
+        assert head.isnan().nonzero().flatten().tolist() == pair
+        assert (head[~head.isnan()] == 0).all()
+        y[at] = w[at]
+        assert torch.equal(y, w)
+    assert torch.equal(got[2], want[2])
+
+
 def test_parts_left_out():
     rng = np.random.default_rng(7)
     q, k, v = projection(rng, 2, 3, 4, 2, 64, "bf16")
