@@ -132,9 +132,14 @@ __global__ __launch_bounds__(256) void read_rows4_kernel(Read4Params p) {
     out(static_cast<T *>(p.out_v) + to, v, vs);
 }
 
+// Words of one (sequence, kv head)'s rows of 256: 2^29.  The kernels number words, and those
+// of a last trip past them, in 32 bits, and a grid dimension holds less than 2^32 threads.
+constexpr long long kMostWords = (long long)kCache4MaxRows * (256 / 8);
+static_assert(kMostWords + 256 * kWriteTrip<true> <= 1LL << 31, "32-bit word numbers");
+
 template <typename T, bool RING>
 hipError_t launch_rows(const Write4Params &p, int rows, hipStream_t stream) {
-    const long long words = (long long)rows << p.row_shift;  // 2^31 at most
+    const long long words = (long long)rows << p.row_shift;  // kMostWords at most
     const dim3 grid((unsigned)((words + 256 * kWriteTrip<RING> - 1) / (256 * kWriteTrip<RING>)), p.Hkv, p.B);
     write_rows4_kernel<T, RING><<<grid, 256, 0, stream>>>(p);
     return hipGetLastError();
@@ -163,7 +168,7 @@ hipError_t launch_append4(const Write4Params &p, bool bf16, hipStream_t stream) 
 }
 
 hipError_t launch_read4(const Read4Params &p, bool bf16, hipStream_t stream) {
-    const long long words = (long long)p.rows << p.row_shift;  // 2^31 at most, so less than 2^32 threads
+    const long long words = (long long)p.rows << p.row_shift;  // kMostWords at most
     const dim3 grid((unsigned)((words + 255) / 256), p.Hkv, p.B);
     if (bf16) read_rows4_kernel<uint16_t><<<grid, 256, 0, stream>>>(p);
     else read_rows4_kernel<float><<<grid, 256, 0, stream>>>(p);

@@ -1,6 +1,8 @@
 // What the decode kernels share (decode.hip: fp32 and bf16 caches, decode8.hip:
-// the 8-bit cache): the ring count's fetch, the combination of a workgroup's
-// waves, the publication and merge of the splits, and the count's advance.
+// the 8-bit cache, decode4.hip: the 4-bit cache): the ring count's fetch, an
+// arrival on a counter, the coherent stores of the partials; and, for the first
+// two, the combination of a workgroup's waves and how the splits' merge is cut
+// (decode4.hip joins both its own way).
 #pragma once
 
 #include <float.h>
