@@ -261,27 +261,31 @@ DecodePlan plan_decode8(int B, int Hq, int Hkv, int Dh, int k, int W, bool appen
     return pl;
 }
 
-// Decode over the 4-bit cache.  A unit of 32 rows costs a wave alone on its SIMD about
-// 0.65 us, more than its bytes do, so a long axis is split over all CUs; a join costs
-// about 1.7 us and 0.06 us per split that the last workgroup reads.
+// Decode over the 4-bit cache; times in us of the attention alone, 32/8 heads of 128 unless
+// said otherwise.  A unit of 32 rows costs a wave alone on its SIMD about 0.65 us, more than
+// its bytes do, so a long axis is split over all CUs; a join costs about 1.8 us, and every
+// further split 0.03 us where there is one pair, 0.12 of eight.
 //
-// - Up to 12 units, or from 129 pairs on, no split: 8 pairs of 7 units 6.2 us in one
-//   workgroup each and 7.2 in two; 160 pairs of 24 units 10.8 and 11.9.
+// - Up to 12 units, or from 129 pairs on, no split: 8 pairs of 7 units 4.6 us in one
+//   workgroup each and 5.8 in two; 160 pairs of 24 units 8.7 and 10.6.  (Three splits of long
+//   lists up to 170 pairs would be quicker, 136 pairs of 144 units 21.2 against 25.7; two
+//   would not, 27.4.)
 // - Else a wave's units and the number of splits grow alike, as the root of the length,
-//   with one workgroup per CU at most.  8 pairs: 24 units 7.1 us in 6 splits (3: 7.9),
-//   130 units 8.7 in 11 (17: 9.0, 7: 9.7), 1026 units 15.8 in 29 (43: 17.8, 20: 17.7);
-//   64 pairs: 24 units 9.0 in 3 (2: 9.6), 136 units 14.7 in 4 (7: 14.7, 3: 16.6).
+//   with one workgroup per CU at most.  8 pairs: 24 units 6.1 us in 6 splits (3: 6.6),
+//   130 units 8.9 in 11 (17: 8.4, 7: 9.6), 1026 units 15.4 in 29 (43: 16.5, 20: 17.1);
+//   64 pairs: 24 units 7.6 in 3 (2: 8.3), 136 units 13.4 in 4 (7: 13.7, 3: 15.2).
 // - Eight waves for a pair's whole axis of 12 units and more where a CU has one workgroup
-//   at most: 256 pairs of 144 units 28.3 us (4 waves 30.0), 192 of 38 units 11.3 (11.9),
-//   136 of 144 units 26.0 (29.9), 8 of 12 units 5.2 (5.7).  Their start and sums cost more, so not for short lists of heads of
-//   256 (160 pairs of four query heads, 28 units 13.9 against 13.1, 48 units 18.3 both, 64 units
-//   21.9 against 22.6; of eight, 20 units 14.2 against 13.2, 48 units 21.1 against 22.1), nor of
-//   heads of 128 where nearly every CU has a workgroup (256 pairs, 28 units 10.2 against
-//   10.0, one query head 9.3 against 8.9; 40 units the same).
-// - Split axes leave half of the CUs to others only where pairs are few
-//   and long: one of 1026 units 15.7 us in 33 splits (4 waves 18.9); 8 pairs of 1026 units
-//   fill the card with four waves (26 splits of eight 16.9), and of 130 units a wave of eight
-//   has too little (9.4).
+//   at most: 256 pairs of 144 units 28.9 us (4 waves 30.3), 192 of 38 units 11.3 (12.0),
+//   136 of 144 units 25.7 (29.8), 8 of 12 units 5.2 (5.7).  Their start and sums cost more, so
+//   not for short lists of heads of 256 (160 pairs of four query heads, 28 units 13.9 against
+//   13.1, 48 units 18.3 both, 64 units 21.9 against 22.6; of eight, 20 units 14.2 against
+//   13.2, 48 units 21.1 against 22.1), nor of heads of 128 where nearly every CU has a
+//   workgroup (256 pairs, 28 units 10.2 against 10.0, one query head 9.3 against 8.9; 40
+//   units the same).
+// - Split axes leave half of the CUs to others only where pairs are few and long: one of
+//   1026 units 12.1 us in 33 splits (4 waves 12.9; in 65 splits 10.5, of 4 waves 11.5); 8
+//   pairs of 1026 units fill the card with four waves (26 splits of eight 15.7), and of 130
+//   units eight gain nothing (8.9).
 constexpr long long kMaxSplits4 = 127;
 DecodePlan plan_decode4(int B, int Hq, int Hkv, int Dh, int k, int W) {
     const long long pairs = (long long)B * Hkv;
